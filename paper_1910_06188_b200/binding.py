@@ -14,7 +14,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import warnings
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -24,6 +24,7 @@ LIB_PATH = os.path.join(_PKG, "libq8.so")
 Q8_OK, Q8_ERR_NULL, Q8_ERR_SHAPE, Q8_ERR_ALIGN, Q8_ERR_SCALE, Q8_ERR_INDEX = 0, 1, 2, 3, 4, 5
 Q8_ERR_OVERFLOW, Q8_ERR_WORKSPACE, Q8_ERR_TIMEOUT, Q8_ERR_CUDA, Q8_ERR_ARG = 6, 7, 8, 9, 10
 Q8_ACT_NONE, Q8_ACT_GELU = 0, 1
+Q8_F32, Q8_F16, Q8_BF16 = 0, 1, 2
 Q8_MAX_K = 133144
 
 # name -> (restype, argtypes); mirrors include/q8.h and include/q8_tools.h one to one.
@@ -55,6 +56,17 @@ SIGNATURES = {
     "q8_linear_q_requant": (_int, [_vp, _vp, _vp, _vp, _vp, _int, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp]),
     "q8_add_layernorm_quant": (_int, [_vp, _vp, _vp, _vp, _vp, _f, _i64, _i64, _vp, _vp, _vp, _vp]),
     "q8_attention_quant": (_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "q8_mx4_codes_bytes": (_sz, [_i64, _i64]),
+    "q8_mx4_scales_bytes": (_sz, [_i64, _i64, _i64]),
+    "q8_mx4_quantize": (_int, [_vp, _int, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "q8_mx4_dequantize": (_int, [_vp, _vp, _i64, _i64, _i64, _vp, _int, _i64, _vp]),
+    "q8_mx4_fake_quantize": (_int, [_vp, _int, _i64, _i64, _i64, _vp, _i64, _vp, _vp]),
+    "q8_mx4_linear_workspace_bytes": (_sz, [_i64, _i64]),
+    "q8_mx4_linear": (_int, [_vp, _int, _i64, _vp, _vp, _vp, _int, _vp, _int, _i64, _i64, _i64, _i64, _vp, _sz, _vp, _vp]),
+    "q8_mx4_linear_q": (_int, [_vp, _vp, _vp, _vp, _vp, _int, _vp, _int, _i64, _i64, _i64, _i64, _vp, _vp]),
+    "q8_mx4_linear_grouped_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "q8_mx4_linear_grouped": (_int, [_vp, _int, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _int, _vp, _int, _i64, _i64, _i64, _i64,
+                                     _vp, _sz, _vp, _vp]),
     "q8_poll_status": (_int, [_vp, C.POINTER(C.c_uint32), _vp]),
     "q8_status_string": (C.c_char_p, [_int]),
     "q8_last_launch_info": (None, [C.POINTER(_int)] * 5),
@@ -617,6 +629,200 @@ def q8_attention_quant(qkv, B: int, S: int, heads: int, S_q, ctx_q=None, ctx=Non
                                    _ptr(S_q, torch.float32, "S_q"), _ptr(ctx_q, torch.int8, "ctx_q"), _stream(stream))
     _check(st, "q8_attention_quant")
     return ctx_q
+
+
+# ---------------------------------------------------------------- MXFP4
+_MX4_DTYPES = {torch.float32: Q8_F32, torch.float16: Q8_F16, torch.bfloat16: Q8_BF16}
+
+
+class Mx4(NamedTuple):
+    """A tensor in microscaled 4-bit floating point; include/q8.h has the layout of its parts."""
+
+    codes: torch.Tensor  # uint8 [..., rows, 16 ceil(K / 32)]
+    scales: torch.Tensor  # uint8, one row of atoms after the other
+    K: int
+
+
+def _mx4_matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
+    """(pointer, type, row stride) of values in rows: [rows, K] with any distance of rows, or a contiguous [groups, rows, K]."""
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype not in _MX4_DTYPES:
+        raise TypeError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
+    K = t.shape[-1]
+    if t.dim() == 2 and (t.stride(1) == 1 or K == 1):
+        ld = t.stride(0) if t.shape[0] > 1 else K
+        if ld < K:
+            raise TypeError(f"the rows of {name} overlap")
+    elif t.is_contiguous():
+        ld = K
+    else:
+        raise TypeError(f"{name} must have its values side by side in rows" + (" and be contiguous" if t.dim() > 2 else ""))
+    return t.data_ptr(), _MX4_DTYPES[t.dtype], ld
+
+
+def _mx4_parts(t: Mx4, name: str, dims: int) -> Tuple[int, int, int, int, int]:
+    """(codes, scales, groups, rows, K) of a quantised tensor of `dims` dimensions; groups is 1 for a matrix."""
+    codes, scales, K = t
+    if codes.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions, its codes are {tuple(codes.shape)}")
+    groups, rows = (codes.shape[0] if dims == 3 else 1), codes.shape[-2]
+    if K < 1 or codes.shape[-1] != 16 * -(-K // 32):
+        raise ValueError(f"{name}: rows of {codes.shape[-1]} bytes do not hold {K} codes")
+    need = int(load().q8_mx4_scales_bytes(groups, rows, K))
+    if scales.numel() < need:
+        raise ValueError(f"{name} has {scales.numel()} bytes of scales, {need} are read")
+    return _ptr(codes, torch.uint8, name), _ptr(scales, torch.uint8, name), groups, rows, K
+
+
+def _mx4_same_device(*tensors) -> None:
+    """Kernels run on the current device: all tensors are there."""
+    current = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != current:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{current}")
+
+
+def _mx4_empty(shape, dtype, device, stream):
+    """A new tensor that belongs to the stream that the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _mx4_output(Y, shape, dtype, like, stream, name: str = "Y"):
+    if Y is None:
+        Y = _mx4_empty(shape, dtype, like.device, stream)
+    elif tuple(Y.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(Y.shape)}")
+    elif dtype is not None and Y.dtype != dtype:
+        raise TypeError(f"{name} is {Y.dtype}, {dtype} was asked for")
+    return Y
+
+
+def q8_mx4_codes_bytes(rows: int, K: int) -> int:
+    return int(load().q8_mx4_codes_bytes(rows, K))
+
+
+def q8_mx4_scales_bytes(groups: int, rows: int, K: int) -> int:
+    return int(load().q8_mx4_scales_bytes(groups, rows, K))
+
+
+def q8_mx4_quantize(X, dev_status=None, stream=None) -> Mx4:
+    """X [rows, K], or [experts, rows, K] for the weights of q8_mx4_linear_grouped, in MXFP4."""
+    if X.dim() not in (2, 3):
+        raise ValueError(f"X must have 2 or 3 dimensions, got {tuple(X.shape)}")
+    x, dtype, ld = _mx4_matrix(X, "X")
+    _mx4_same_device(X, dev_status)
+    groups, (rows, K) = (X.shape[0] if X.dim() == 3 else 1), X.shape[-2:]
+    codes = _mx4_empty((*X.shape[:-1], 16 * -(-K // 32)), torch.uint8, X.device, stream)
+    scales = _mx4_empty(q8_mx4_scales_bytes(groups, rows, K), torch.uint8, X.device, stream)
+    st = load().q8_mx4_quantize(x, dtype, groups, rows, K, ld, _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales"),
+                                _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check(st, "q8_mx4_quantize")
+    return Mx4(codes, scales, K)
+
+
+def q8_mx4_dequantize(T: Mx4, dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
+    """The values that the codes and scales of T stand for."""
+    codes, scales, groups, rows, K = _mx4_parts(T, "T", T.codes.dim() if T.codes.dim() == 3 else 2)
+    _mx4_same_device(T.codes, T.scales)
+    Y = _mx4_empty((*T.codes.shape[:-1], K), dtype, T.codes.device, stream)
+    y, y_dtype, ldy = _mx4_matrix(Y, "Y")
+    _check(load().q8_mx4_dequantize(codes, scales, groups, rows, K, y, y_dtype, ldy, _stream(stream)), "q8_mx4_dequantize")
+    return Y
+
+
+def q8_mx4_fake_quantize(X, Xhat=None, dev_status=None, stream=None) -> torch.Tensor:
+    """Training-mode MXFP4: the values that the codes of X [rows, K] stand for, in X's type; q8_ste_backward is its gradient."""
+    if X.dim() != 2:
+        raise ValueError(f"X must have 2 dimensions, got {tuple(X.shape)}")
+    x, dtype, ld = _mx4_matrix(X, "X")
+    Xhat = _mx4_output(Xhat, X.shape, X.dtype, X, stream, "Xhat")
+    out, _, ldo = _mx4_matrix(Xhat, "Xhat")
+    _mx4_same_device(X, Xhat, dev_status)
+    st = load().q8_mx4_fake_quantize(x, dtype, X.shape[0], X.shape[1], ld, out, ldo, _ptr(dev_status, torch.int32, "dev_status"),
+                                     _stream(stream))
+    _check(st, "q8_mx4_fake_quantize")
+    return Xhat
+
+
+def q8_mx4_linear_workspace_bytes(M: int, K: int) -> int:
+    return int(load().q8_mx4_linear_workspace_bytes(M, K))
+
+
+def q8_mx4_linear_grouped_workspace_bytes(T: int, experts: int, K: int) -> int:
+    return int(load().q8_mx4_linear_grouped_workspace_bytes(T, experts, K))
+
+
+def _mx4_bias(bias, values: int):
+    if bias is not None and bias.numel() != values:
+        raise ValueError(f"bias has {bias.numel()} values, {values} are read")
+    return _ptr(bias, torch.float32, "bias")
+
+
+def q8_mx4_linear(X, W: Mx4, bias=None, act: int = Q8_ACT_NONE, Y=None, dtype: Optional[torch.dtype] = None, workspace=None,
+                  dev_status=None, stream=None) -> torch.Tensor:
+    """act(X_hat W_hat^T + b) with X [M, K] quantised on its way in; Y in X's type unless `dtype` or Y says otherwise."""
+    wq, ws, _, N, K = _mx4_parts(W, "W", 2)
+    if X.dim() != 2 or X.shape[1] != K:
+        raise ValueError(f"X is {tuple(X.shape)} but W has rows of {K}")
+    x, x_dtype, ldx = _mx4_matrix(X, "X")
+    M = X.shape[0]
+    Y = _mx4_output(Y, (M, N), dtype if dtype is not None or Y is not None else X.dtype, X, stream)
+    y, y_dtype, ldy = _mx4_matrix(Y, "Y")
+    if workspace is None:
+        workspace = _mx4_empty(q8_mx4_linear_workspace_bytes(M, K), torch.uint8, X.device, stream)
+    _mx4_same_device(X, *W[:2], bias, Y, workspace, dev_status)
+    st = load().q8_mx4_linear(x, x_dtype, ldx, wq, ws, _mx4_bias(bias, N), int(act), y, y_dtype, ldy, M, N, K,
+                              _any_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+                              _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check(st, "q8_mx4_linear")
+    return Y
+
+
+def q8_mx4_linear_q(Xq: Mx4, W: Mx4, bias=None, act: int = Q8_ACT_NONE, Y=None, dtype: Optional[torch.dtype] = None,
+                    dev_status=None, stream=None) -> torch.Tensor:
+    """q8_mx4_linear on an activation that is quantised already; Y is fp32 unless `dtype` or Y says otherwise."""
+    wq, ws, _, N, K = _mx4_parts(W, "W", 2)
+    xq, xs, _, M, K2 = _mx4_parts(Xq, "Xq", 2)
+    if K2 != K:
+        raise ValueError(f"Xq has rows of {K2}, W of {K}")
+    Y = _mx4_output(Y, (M, N), dtype if dtype is not None or Y is not None else torch.float32, Xq.codes, stream)
+    y, y_dtype, ldy = _mx4_matrix(Y, "Y")
+    _mx4_same_device(*Xq[:2], *W[:2], bias, Y, dev_status)
+    st = load().q8_mx4_linear_q(xq, xs, wq, ws, _mx4_bias(bias, N), int(act), y, y_dtype, ldy, M, N, K,
+                                _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check(st, "q8_mx4_linear_q")
+    return Y
+
+
+def q8_mx4_linear_grouped(X, offsets, W: Mx4, bias=None, act: int = Q8_ACT_NONE, rows=None, Y=None,
+                          dtype: Optional[torch.dtype] = None, workspace=None, dev_status=None, stream=None) -> torch.Tensor:
+    """The layer with one weight matrix per expert (W from a [experts, N, K] tensor, bias [experts, N]): Y[t] =
+    act(X_hat[rows[t]] W_hat[e]^T + b[e]) for the slots offsets[e] <= t < offsets[e + 1]; without `rows` slot t takes row t.
+    Rows of Y that no expert owns stay as they were (are uninitialised in a Y that this call makes)."""
+    wq, ws, E, N, K = _mx4_parts(W, "W", 3)
+    if X.dim() != 2 or X.shape[1] != K:
+        raise ValueError(f"X is {tuple(X.shape)} but W has rows of {K}")
+    if offsets.numel() != E + 1:
+        raise ValueError(f"offsets has {offsets.numel()} values for {E} experts")
+    x, x_dtype, ldx = _mx4_matrix(X, "X")
+    T = X.shape[0] if rows is None else rows.numel()
+    Y = _mx4_output(Y, (T, N), dtype if dtype is not None or Y is not None else X.dtype, X, stream)
+    y, y_dtype, ldy = _mx4_matrix(Y, "Y")
+    if workspace is None:
+        workspace = _mx4_empty(q8_mx4_linear_grouped_workspace_bytes(T, E, K), torch.uint8, X.device, stream)
+    _mx4_same_device(X, offsets, *W[:2], bias, rows, Y, workspace, dev_status)
+    st = load().q8_mx4_linear_grouped(x, x_dtype, ldx, X.shape[0], _ptr(rows, torch.int32, "rows"), _ptr(offsets, torch.int32, "offsets"),
+                                      E, wq, ws, _mx4_bias(bias, E * N), int(act), y, y_dtype, ldy, T, N, K,
+                                      _any_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+                                      _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    _check(st, "q8_mx4_linear_grouped")
+    return Y
 
 
 def q8_poll_status(dev_status: torch.Tensor, stream=None) -> Tuple[int, int]:

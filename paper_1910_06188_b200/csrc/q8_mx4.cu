@@ -1,0 +1,299 @@
+// Quantisation to microscaled 4-bit floating point, back, and both at once (training), streaming passes bound by HBM.
+//
+// A lane takes 8 neighbouring values of a row, so four lanes share a block: its maximum is an integer maximum of the lanes'
+// magnitude bits and two shuffles, the scale an exponent, the codes four conversions of two values each.  A warp takes 256 columns of
+// up to four rows, whose loads are all issued before the first is used.  For a plain matrix these are the rows r, r + 32,
+// r + 64 and r + 96 that lie side by side in an atom of scales: the four bytes of each leave as one 16-byte store.
+
+#include "q8_mx4.cuh"
+
+namespace q8 {
+
+namespace {
+
+using namespace mx4;
+
+constexpr int kThreads = 128;
+constexpr int kWarps = kThreads / 32;
+constexpr int kChunk = 256;  // columns of a warp
+
+enum Kind { kMatrix, kFake, kSlots1, kSlots4 };
+template <int KIND>
+constexpr int kRows = KIND == kSlots1 ? 1 : 4;
+
+// Eight values from column k0 on; those at or behind `valid` are 0.
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, int valid, bool vec, float (&v)[8])
+{
+    if (vec && valid >= 8) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 a = __ldcs(reinterpret_cast<const float4 *>(p)), b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+            const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(p));
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                T h[2];
+                memcpy(h, &w[i], 4);
+                v[2 * i] = to_float(h[0]);
+                v[2 * i + 1] = to_float(h[1]);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < valid ? to_float(p[i]) : 0.0f;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T *p, int valid, bool vec, const float (&v)[8])
+{
+    if (vec && valid >= 8) {
+        if constexpr (sizeof(T) == 4) {
+            __stcs(reinterpret_cast<float4 *>(p), make_float4(v[0], v[1], v[2], v[3]));
+            __stcs(reinterpret_cast<float4 *>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+        } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const T h[2] = {from_float<T>(v[2 * i]), from_float<T>(v[2 * i + 1])};
+                memcpy(&w[i], h, 4);
+            }
+            __stcs(reinterpret_cast<uint4 *>(p), make_uint4(w[0], w[1], w[2], w[3]));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) p[i] = from_float<T>(v[i]);
+    }
+}
+
+// E of the block that this lane and its three neighbours hold, and the lane's codes.  NaN becomes 0; neither NaN nor an infinity is
+// in the maximum (`odd` says that there was one).
+__device__ __forceinline__ uint32_t quantize8(float (&v)[8], uint32_t &E, bool &odd)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t bits = __float_as_uint(v[i]) & 0x7fffffffu;
+        if (bits >= 0x7f800000u) {
+            odd = true;
+            if (bits > 0x7f800000u) v[i] = 0.0f;
+        } else {
+            top = max(top, bits);
+        }
+    }
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const uint32_t field = top >> 23;
+    E = field > 2 ? field - 2 : 0;
+    const float inv = inverse_scale(E);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], inv);
+    return pack_e2m1(v);
+}
+
+template <typename T, int KIND>
+__global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs a, int64_t tasks, int row_lanes, int vec, int vec_out)
+{
+    constexpr int R = kRows<KIND>;
+    constexpr bool kSlots = KIND == kSlots1 || KIND == kSlots4;
+    __shared__ int32_t table_words[kSlots ? 2 * (kMaxExperts + 1) : 1];
+    grid_dependency_wait();
+    grid_dependency_release_next(true);
+    const int lane = threadIdx.x & 31;
+    const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const int64_t chunks = ceil_div(a.K, kChunk);
+    ExpertTable table{table_words, table_words + kMaxExperts + 1};
+    bool bad_index = false;
+    if (kSlots) {
+        if (threadIdx.x < 32) bad_index = build_expert_table(table, a.offsets, a.E, (int32_t)a.rows);
+        __syncthreads();
+    }
+    if (task >= tasks) return;
+    int64_t first, row_step, end, scale_row0 = 0;
+    int64_t chunk;
+    if (KIND == kMatrix) {  // row_lanes of the 32 rows r, with r + 32, ... each, of a block of 128
+        const int64_t blocks = ceil_div(a.rows, kAtomRows);
+        const int64_t block = task / row_lanes / chunks, group = block / blocks;
+        chunk = task / row_lanes % chunks;
+        first = group * a.rows + (block - group * blocks) * kAtomRows + task % row_lanes;
+        end = (group + 1) * a.rows;
+        scale_row0 = block * kAtomRows + task % row_lanes;
+        row_step = 32;
+    } else {
+        chunk = task % chunks;
+        first = task / chunks * R;
+        end = a.rows;
+        row_step = 1;
+    }
+    const int64_t k0 = chunk * kChunk + lane * 8;
+    const int valid = (int)max((int64_t)0, min((int64_t)8, a.K - k0));
+    const int64_t pitch = code_pitch(a.K), atoms = scale_atoms(a.K);
+    bool odd = false;
+    float v[R][8];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int64_t row = first + j * row_step;
+        int64_t from = row;
+        bool there = row < end;
+        if (kSlots && there && a.index != nullptr) {
+            from = __ldg(a.index + row);
+            if (from < 0 || from >= a.x_rows) {  // counts as a row of zeros
+                const bool owned = row >= table.start[0] && row < table.start[a.E];
+                bad_index |= owned;
+                there = false;
+            }
+        }
+        load8(reinterpret_cast<const T *>(a.X) + from * a.ld + k0, there ? valid : 0, vec != 0, v[j]);
+    }
+    uint32_t words[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int64_t row = first + j * row_step;
+        uint32_t E;
+        const uint32_t codes = quantize8(v[j], E, odd);
+        if (KIND == kFake) {
+            if (row < end) {
+                float back[8];
+                unpack_e2m1(codes, back);
+                const float s = scale_value(E);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) back[i] = __fmul_rn(back[i], s);
+                store8(reinterpret_cast<T *>(a.Xhat) + row * a.ldo + k0, valid, vec_out != 0, back);
+            }
+            continue;
+        }
+        // the bytes of four blocks, gathered from every fourth of 16 lanes
+        uint32_t w = E << (8 * ((lane >> 2) & 3));
+        w |= __shfl_xor_sync(0xffffffffu, w, 4);
+        w |= __shfl_xor_sync(0xffffffffu, w, 8);
+        words[j] = w;
+        if (row < end && (k0 >> 1) < pitch) *reinterpret_cast<uint32_t *>(a.codes + row * pitch + (k0 >> 1)) = codes;
+        if (kSlots && row < end && (lane & 15) == 0) {
+            // the expert that owns the slot: the last one that starts at or before it
+            int lo = 0, hi = a.E;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (table.start[mid + 1] <= row) lo = mid + 1;
+                else hi = mid;
+            }
+            const int64_t atom = chunk * 2 + (lane >> 4);
+            if (lo < a.E && row >= table.start[lo] && atom < atoms) {
+                const int64_t in_expert = row - table.start[lo], block = table.block[lo] + in_expert / kAtomRows;
+                const int r = (int)(in_expert % kAtomRows);
+                *reinterpret_cast<uint32_t *>(a.scales + (block * atoms + atom) * kAtomBytes + (r & 31) * 16 + (r >> 5) * 4) = w;
+            }
+        }
+    }
+    if constexpr (KIND == kMatrix) {
+        const int64_t atom = chunk * 2 + (lane >> 4);
+        if ((lane & 15) == 0 && atom < atoms)
+            *reinterpret_cast<uint4 *>(a.scales + (scale_row0 / kAtomRows * atoms + atom) * kAtomBytes + (scale_row0 & 31) * 16) =
+                make_uint4(words[0], words[1], words[2], words[3]);
+    }
+    if (a.status != nullptr) {
+        const uint32_t flags = (odd ? 1u << Q8_ERR_SCALE : 0u) | (bad_index ? 1u << Q8_ERR_INDEX : 0u);
+        if (flags != 0) atomicOr(a.status, (int32_t)flags);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+mx4_dequantize_kernel(const uint8_t *codes, const uint8_t *scales, int64_t groups, int64_t rows, int64_t K, T *Y, int64_t ldy, int64_t tasks, int vec)
+{
+    grid_dependency_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    if (task >= tasks) return;
+    const int64_t chunks = ceil_div(K, kChunk), chunk = task % chunks, first = task / chunks * 4;
+    const int64_t k0 = chunk * kChunk + lane * 8;
+    if (k0 >= K) return;
+    const int valid = (int)min((int64_t)8, K - k0);
+    const int64_t pitch = code_pitch(K), atoms = scale_atoms(K), blocks = ceil_div(rows, kAtomRows);
+    uint32_t c[4], E[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t row = first + j;
+        c[j] = E[j] = 0;
+        if (row >= groups * rows) continue;
+        const int64_t group = row / rows, r = row - group * rows;
+        c[j] = __ldcs(reinterpret_cast<const uint32_t *>(codes + row * pitch + (k0 >> 1)));
+        E[j] = __ldg(scales + ((group * blocks + r / kAtomRows) * atoms + k0 / kAtomK) * kAtomBytes + (r & 31) * 16 +
+                     ((r % kAtomRows) >> 5) * 4 + (k0 % kAtomK) / kBlock);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (first + j >= groups * rows) continue;
+        float v[8];
+        unpack_e2m1(c[j], v);
+        const float s = E[j] == 255 ? __uint_as_float(0x7fc00000u) : scale_value(E[j]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], s);
+        store8(Y + (first + j) * ldy + k0, valid, vec != 0, v);
+    }
+}
+
+bool rows_aligned(const void *p, int64_t ld, int size) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0; }
+
+cudaError_t grid_of(int64_t tasks, dim3 *grid)
+{
+    const int64_t ctas = ceil_div(tasks, kWarps);
+    if (ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    *grid = dim3((unsigned)ctas);
+    return cudaSuccess;
+}
+
+template <typename T, int KIND>
+cudaError_t launch_kind(const Mx4QuantizeArgs &a, cudaStream_t s)
+{
+    const int64_t chunks = ceil_div(a.K, kChunk);
+    const int row_lanes = (int)(a.rows < 32 ? a.rows : 32);
+    const int64_t tasks = KIND == kMatrix ? a.groups * ceil_div(a.rows, kAtomRows) * chunks * row_lanes : ceil_div(a.rows, kRows<KIND>) * chunks;
+    dim3 grid;
+    cudaError_t e = grid_of(tasks, &grid);
+    if (e != cudaSuccess) return e;
+    return launch_overlapping_tail(mx4_quantize_kernel<T, KIND>, grid, dim3(kThreads), 0, s, a, tasks, row_lanes,
+                                   (int)rows_aligned(a.X, a.ld, sizeof(T)), (int)rows_aligned(a.Xhat, a.ldo, sizeof(T)));
+}
+
+template <typename T>
+cudaError_t launch_type(const Mx4QuantizeArgs &a, cudaStream_t s)
+{
+    if (a.Xhat != nullptr) return launch_kind<T, kFake>(a, s);
+    if (a.offsets == nullptr) return launch_kind<T, kMatrix>(a, s);
+    // one row to a warp while that leaves room for every warp at once
+    return a.rows * ceil_div(a.K, kChunk) <= 16 * sm_count() ? launch_kind<T, kSlots1>(a, s) : launch_kind<T, kSlots4>(a, s);
+}
+
+}  // namespace
+
+cudaError_t launch_mx4_quantize(const Mx4QuantizeArgs &a, int dtype, cudaStream_t s)
+{
+    last_launch_info().launches += 1;
+    switch (dtype) {
+        case Q8_F32: return launch_type<float>(a, s);
+        case Q8_F16: return launch_type<__half>(a, s);
+        default: return launch_type<__nv_bfloat16>(a, s);
+    }
+}
+
+cudaError_t launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t groups, int64_t rows, int64_t K, void *Y,
+                                  int dtype, int64_t ldy, cudaStream_t s)
+{
+    last_launch_info().launches += 1;
+    const int64_t tasks = ceil_div(groups * rows, 4) * ceil_div(K, kChunk);
+    dim3 grid;
+    cudaError_t e = grid_of(tasks, &grid);
+    if (e != cudaSuccess) return e;
+    const int vec = rows_aligned(Y, ldy, dtype == Q8_F32 ? 4 : 2);
+    switch (dtype) {
+        case Q8_F32: return launch_overlapping_tail(mx4_dequantize_kernel<float>, grid, dim3(kThreads), 0, s, codes, scales, groups, rows, K, static_cast<float *>(Y), ldy, tasks, vec);
+        case Q8_F16: return launch_overlapping_tail(mx4_dequantize_kernel<__half>, grid, dim3(kThreads), 0, s, codes, scales, groups, rows, K, static_cast<__half *>(Y), ldy, tasks, vec);
+        default: return launch_overlapping_tail(mx4_dequantize_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, s, codes, scales, groups, rows, K, static_cast<__nv_bfloat16 *>(Y), ldy, tasks, vec);
+    }
+}
+
+}  // namespace q8

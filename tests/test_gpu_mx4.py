@@ -1,0 +1,459 @@
+"""The MXFP4 operators on the GPU against their definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_1910_06188_b200 import binding as q8
+from tests import mx4_reference as ref
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+NAMES = {torch.float32: "fp32", torch.float16: "fp16", torch.bfloat16: "bf16"}
+
+
+def values(shape, seed, dtype=torch.float32, spread=2.0):
+    """Blocks of very different magnitude, an outlier here and there."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=g)
+    x = x * torch.exp(spread * torch.randn((*shape[:-1], 1), generator=g)).clamp(1e-2, 1e2)
+    x = x * (1 + 7 * (torch.rand(shape, generator=g) < 0.02))
+    return x.to(dtype).cuda()
+
+
+def weights(shape, seed):
+    g = torch.Generator().manual_seed(seed)
+    return (0.02 * torch.randn(shape, generator=g)).cuda()
+
+
+def status_word():
+    return torch.zeros(1, dtype=torch.int32, device="cuda")
+
+
+def check_codes(t, x, group=0):
+    code, E, blocks = ref.unpack(t, group)
+    want_code, want_E = ref.quantize(ref.as_numpy(x))
+    assert np.array_equal(E[:, :blocks], want_E)
+    assert not E[:, blocks:].any(), "scales behind the last block"
+    assert np.array_equal(code, want_code)
+
+
+# ---------------------------------------------------------------- quantisation
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("rows,K", [(1, 1), (1, 32), (3, 33), (31, 256), (33, 257), (100, 31), (128, 128), (129, 1000), (300, 4104)])
+def test_quantize(rows, K, dtype):
+    x = values((rows, K), rows + K, dtype)
+    word = status_word()
+    t = q8.q8_mx4_quantize(x, dev_status=word)
+    assert t.codes.shape == (rows, 16 * -(-K // 32)) and t.K == K
+    check_codes(t, x)
+    assert word.item() == 0
+    for out in TYPES:
+        got = q8.q8_mx4_dequantize(t, out)
+        assert got.dtype == out and torch.equal(got.double().cpu(), torch.from_numpy(ref.rounded(x)).to(out).double())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("offset,ld", [(0, 600), (8, 616), (1, 601), (3, 640)])
+def test_quantize_rows_of_a_wider_tensor(offset, ld, dtype):
+    x = values((70, ld), ld, dtype)[:, offset:offset + 520]
+    check_codes(q8.q8_mx4_quantize(x), x)
+
+
+@pytest.mark.parametrize("shape", [(3, 5, 40), (2, 128, 256), (4, 200, 130)])
+def test_quantize_groups(shape):
+    x = values(shape, 7)
+    t = q8.q8_mx4_quantize(x)
+    back = q8.q8_mx4_dequantize(t)
+    for g in range(shape[0]):
+        check_codes(t, x[g], g)
+        assert np.array_equal(ref.as_numpy(back[g]), ref.rounded(x[g]))
+
+
+def test_quantize_ties_and_borders():
+    steps = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, 7.9999995])
+    rows = []
+    for s in (1.0, 2.0 ** -20, 2.0 ** 90):
+        for sign in (1, -1):
+            row = torch.zeros(32)
+            row[:10], row[10:20], row[20:30] = steps, torch.nextafter(steps, torch.tensor(9.0)), torch.nextafter(steps, torch.tensor(0.0))
+            row[30], row[31] = 4.0, -4.0
+            rows.append(sign * s * row.clamp(max=7.9999995))
+    x = torch.stack(rows).cuda()
+    t = q8.q8_mx4_quantize(x)
+    check_codes(t, x)
+    E = ref.unpack(t)[1][:, 0]
+    assert E.tolist() == [127, 127, 107, 107, 217, 217]
+
+
+def test_quantize_smallest_and_largest():
+    top, tiny = torch.finfo(torch.float32).max, 2.0 ** -149
+    x = torch.zeros(6, 64)
+    x[0, :32] = torch.linspace(-top, top, 32)
+    x[1, 3], x[1, 40] = tiny, -3 * tiny
+    x[2, :32] = torch.linspace(0, 2.0 ** -126, 32)
+    x[3, :32] = torch.linspace(0, 2.0 ** -123, 32)
+    x[4, 0], x[4, 1] = 2.0 ** -125, 2.0 ** 100
+    x = x.cuda()
+    check_codes(q8.q8_mx4_quantize(x), x)
+    assert np.array_equal(ref.as_numpy(q8.q8_mx4_fake_quantize(x)), ref.rounded(x))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_quantize_what_is_not_a_number(dtype):
+    x = values((40, 96), 3, dtype, 0.0)
+    x[0, 5], x[1, 40], x[2, 70] = float("nan"), float("inf"), -float("inf")
+    x[3, :32], x[4, 32:64], x[5] = float("nan"), float("inf"), 0
+    word = status_word()
+    t = q8.q8_mx4_quantize(x, dev_status=word)
+    check_codes(t, x)
+    assert word.item() == 1 << q8.Q8_ERR_SCALE
+    code, E, _ = ref.unpack(t)
+    assert code[0, 5] == 0 and code[1, 40] == 7 and code[2, 70] == 15
+    assert not code[3, :32].any() and E[3, 0] == 0 and (code[4, 32:64] == 7).all() and E[4, 1] == 0 and not E[5].any()
+    word.zero_()
+    q8.q8_mx4_fake_quantize(x[6:], dev_status=word)
+    assert word.item() == 0
+    y = q8.q8_mx4_fake_quantize(x, dev_status=word)
+    assert word.item() == 1 << q8.Q8_ERR_SCALE and torch.isfinite(y).all()
+
+
+# ---------------------------------------------------------------- training
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("rows,K", [(1, 1), (5, 33), (64, 768), (33, 1001)])
+def test_fake_quantize(rows, K, dtype):
+    x = values((rows, K), K, dtype)
+    before = x.clone()
+    y = q8.q8_mx4_fake_quantize(x)
+    want = torch.from_numpy(ref.rounded(x)).to(dtype)
+    assert y.dtype == dtype and torch.equal(y.cpu(), want) and torch.equal(x, before)
+    wide = torch.full((rows, K + 9), 3.0, dtype=dtype, device="cuda")
+    q8.q8_mx4_fake_quantize(x, wide[:, 4:4 + K])
+    assert torch.equal(wide[:, 4:4 + K].cpu(), want) and (wide[:, :4] == 3).all() and (wide[:, 4 + K:] == 3).all()
+    assert q8.q8_mx4_fake_quantize(x, x) is x and torch.equal(x.cpu(), want)
+    assert torch.equal(q8.q8_mx4_fake_quantize(x.clone()), x), "values on the grid stay"
+
+
+class FakeQuantized(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x):
+        return q8.q8_mx4_fake_quantize(x)
+
+    @staticmethod
+    def backward(ctx, g):
+        return q8.q8_ste_backward(g.contiguous())
+
+
+def test_training_step():
+    """A fake-quantised layer's gradients are those of the layer on the rounded values (Eq. 5: the rounding has slope 1)."""
+    x, w = values((48, 96), 1, spread=0.5).requires_grad_(), weights((80, 96), 2).requires_grad_()
+    g = values((48, 80), 3, spread=0.0)
+    (FakeQuantized.apply(x) @ FakeQuantized.apply(w).t()).backward(g)
+    x_hat, w_hat, g64 = ref.rounded(x), ref.rounded(w), ref.as_numpy(g)
+    for got, want, size in ((x.grad, g64 @ w_hat, np.abs(g64) @ np.abs(w_hat)), (w.grad, g64.T @ x_hat, np.abs(g64).T @ np.abs(x_hat))):
+        assert (np.abs(ref.as_numpy(got) - want) <= 100 * 2.0 ** -24 * size).all()  # up to 96 fp32 additions
+
+
+def test_slope_of_the_rounding():
+    """Differences over whole steps: from one end of the grid to the other the rounded values rise as the values do."""
+    t = torch.linspace(-6, 6, 961)[:, None].expand(-1, 32).contiguous()
+    t[:, 31] = 6.0
+    y = q8.q8_mx4_fake_quantize(t.cuda())[:, 0].cpu()
+    assert (y[1:] >= y[:-1]).all() and y[0] == -6 and y[-1] == 6
+    assert (y[-1] - y[0]) / (t[-1, 0] - t[0, 0]) == 1
+
+
+# ---------------------------------------------------------------- the layer
+def run_layer(M, N, K, dtype, act, with_bias, seed=0, ld=None, out=None):
+    x = values((M, ld or K), seed, dtype, 0.5)[:, :K]
+    w, b = weights((N, K), seed + 1), weights((N,), seed + 2) if with_bias else None
+    W = q8.q8_mx4_quantize(w)
+    word = status_word()
+    pad, out = 7, out or dtype
+    whole = torch.full((M + 2, N + pad), 77.0, dtype=out, device="cuda")
+    Y = whole[1:-1, :N]
+    got = q8.q8_mx4_linear(x, W, b, act, Y=Y, dev_status=word)
+    assert got is Y and word.item() == 0
+    ref.assert_layer(Y, ref.rounded(x), ref.rounded(w), b, act)
+    assert (whole[:, N:] == 77).all() and (whole[0] == 77).all() and (whole[-1] == 77).all()
+    plain = q8.q8_mx4_linear(x, W, b, act, dtype=out)
+    assert torch.equal(plain, Y)
+    assert torch.equal(q8.q8_mx4_linear_q(q8.q8_mx4_quantize(x), W, b, act, dtype=out), Y)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 8, 32), (1, 1000, 33), (2, 129, 64), (3, 128, 96), (15, 200, 130), (16, 256, 256),
+                                   (17, 127, 257), (33, 384, 512), (64, 128, 1000), (65, 300, 777), (127, 130, 2000), (128, 512, 160)])
+def test_linear_few_tokens(M, N, K):
+    run_layer(M, N, K, torch.float32, q8.Q8_ACT_NONE, True, seed=M)
+
+
+@pytest.mark.parametrize("M,N,K", [(129, 128, 128), (191, 256, 300), (192, 640, 512), (193, 1000, 1024), (320, 4096, 256), (500, 777, 1000),
+                                   (1000, 1024, 520), (2100, 2048, 264), (1500, 4100, 96)])
+@pytest.mark.parametrize("act", [q8.Q8_ACT_NONE, q8.Q8_ACT_GELU], ids=["none", "gelu"])
+def test_linear(M, N, K, act):
+    run_layer(M, N, K, torch.float32, act, act == q8.Q8_ACT_GELU, seed=M)
+
+
+@pytest.mark.parametrize("M", [1, 24, 200, 1300])
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("out", TYPES, ids=NAMES.get)
+def test_linear_types(M, dtype, out):
+    run_layer(M, 333, 700, dtype, q8.Q8_ACT_GELU, True, seed=5, out=out)
+    run_layer(M, 256, 512, dtype, q8.Q8_ACT_NONE, False, seed=6, out=out)
+
+
+@pytest.mark.parametrize("ld", [1000, 1008, 1001])
+def test_linear_rows_of_a_wider_tensor(ld):
+    run_layer(100, 256, 1000, torch.bfloat16, q8.Q8_ACT_NONE, True, ld=ld)
+
+
+def test_linear_long_rows():
+    run_layer(5, 130, 30000, torch.float32, q8.Q8_ACT_NONE, False)
+    run_layer(200, 300, 20001, torch.bfloat16, q8.Q8_ACT_NONE, True)
+
+
+def test_linear_scales_of_all_sizes():
+    """Scales from the smallest to the largest exponent; products outside fp32's range are left to it."""
+    x, w = values((70, 256), 1, spread=0.0), weights((160, 256), 2)
+    x = x * torch.pow(2.0, torch.arange(70).cuda().float()[:, None] - 35)
+    w = w * torch.pow(2.0, 40 - torch.arange(160).cuda().float()[:, None] / 2)
+    Y = q8.q8_mx4_linear(x, q8.q8_mx4_quantize(w))
+    ref.assert_layer(Y, ref.rounded(x), ref.rounded(w), None, q8.Q8_ACT_NONE)
+
+
+def test_linear_zero_rows_and_infinities():
+    x, w = values((40, 192), 1, spread=0.0), weights((130, 192), 2)
+    x[3], x[4, 64:96] = 0, 0
+    x[7, 10], x[8, 100] = float("inf"), float("nan")
+    w[5] = 0
+    word = status_word()
+    Y = q8.q8_mx4_linear(x, q8.q8_mx4_quantize(w), dev_status=word)
+    assert word.item() == 1 << q8.Q8_ERR_SCALE
+    assert (Y[3] == 0).all() and (Y[:, 5] == 0).all()
+    ref.assert_layer(Y, ref.rounded(x), ref.rounded(w), None, q8.Q8_ACT_NONE)
+
+
+def test_linear_nothing_to_do():
+    W = q8.q8_mx4_quantize(weights((16, 64), 1))
+    assert q8.q8_mx4_linear(torch.empty(0, 64, device="cuda"), W).shape == (0, 16)
+    none = q8.q8_mx4_quantize(torch.empty(0, 64, device="cuda"))
+    assert q8.q8_mx4_linear(values((3, 64), 1), none).shape == (3, 0)
+    assert q8.q8_mx4_dequantize(none).shape == (0, 64)
+
+
+# ---------------------------------------------------------------- grouped by expert
+def run_grouped(offsets, T, N, K, dtype=torch.float32, act=q8.Q8_ACT_NONE, with_bias=True, tokens=None, seed=0):
+    E = len(offsets) - 1
+    g = torch.Generator().manual_seed(seed)
+    x = values((tokens or T, K), seed, dtype, 0.5)
+    w, b = weights((E, N, K), seed + 1), weights((E, N), seed + 2) if with_bias else None
+    rows = torch.randint(0, tokens, (T,), generator=g, dtype=torch.int32).cuda() if tokens else None
+    W = q8.q8_mx4_quantize(w)
+    word = status_word()
+    whole = torch.full((T + 2, N), 55.0, dtype=dtype, device="cuda")
+    Y = whole[1:-1]
+    q8.q8_mx4_linear_grouped(x, torch.tensor(offsets, dtype=torch.int32).cuda(), W, b, act, rows, Y, dev_status=word)
+    assert word.item() == 0 and (whole[0] == 55).all() and (whole[-1] == 55).all()
+    taken = x if rows is None else x[rows.long()]
+    assert (Y[:offsets[0]] == 55).all() and (Y[offsets[-1]:] == 55).all()
+    for e, (lo, hi) in enumerate(zip(offsets, offsets[1:])):
+        if hi > lo:
+            ref.assert_layer(Y[lo:hi], ref.rounded(taken[lo:hi]), ref.rounded(w[e]), None if b is None else b[e], act)
+
+
+@pytest.mark.parametrize("offsets,T", [
+    ([0, 1], 1), ([0, 0, 1, 1], 1), ([0, 5, 5, 12], 12), ([0, 16, 32, 48, 64], 64), ([3, 10, 40], 50), ([0, 0, 0, 0], 9),
+    ([0, 130, 131, 400], 400), ([0, 127, 255, 384, 513], 600), ([0, 500, 500, 517, 1000], 1000)])
+@pytest.mark.parametrize("N,K", [(128, 128), (300, 520), (65, 33)])
+def test_grouped(offsets, T, N, K):
+    run_grouped(offsets, T, N, K)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("E,T", [(7, 20), (64, 40), (64, 3000), (5, 4000), (1, 100)])
+def test_grouped_routed(E, T, dtype):
+    cuts = np.sort(np.random.RandomState(E).randint(0, T + 1, E - 1)).tolist()
+    run_grouped([0, *cuts, T], T, 200, 264, dtype, q8.Q8_ACT_GELU, tokens=T // 2 + 1, seed=T)
+
+
+def test_grouped_many_experts():
+    for E in (31, 32, 33, 1000, 1024):
+        cuts = np.sort(np.random.RandomState(E).randint(0, 701, E - 1)).tolist()
+        run_grouped([0, *cuts, 700], 700, 40, 64, with_bias=E != 33)
+
+
+def test_grouped_is_the_plain_layer_for_one_expert():
+    x, w = values((300, 512), 1, torch.bfloat16), weights((1, 384, 512), 2)
+    W = q8.q8_mx4_quantize(w)
+    one = q8.Mx4(W.codes[0], W.scales, W.K)
+    offsets = torch.tensor([0, 300], dtype=torch.int32).cuda()
+    assert torch.equal(q8.q8_mx4_linear_grouped(x, offsets, W), q8.q8_mx4_linear(x, one))
+
+
+@pytest.mark.parametrize("offsets", [[0, 30, 20, 50], [0, -5, 30, 50], [0, 20, 70, 50], [60, 10, 20, 30], [0, 2 ** 31 - 1, -2 ** 31, 7]])
+def test_grouped_bad_offsets(offsets):
+    """Moved to the nearest offsets that rise from 0 to T, and flagged."""
+    T, N, K = 50, 140, 96
+    x, w = values((T, K), 1), weights((3, N, K), 2)
+    word = status_word()
+    whole = torch.full((T + 2, N), 55.0, device="cuda")
+    Y = whole[1:-1]
+    q8.q8_mx4_linear_grouped(x, torch.tensor(offsets, dtype=torch.int64).to(torch.int32).cuda(), q8.q8_mx4_quantize(w), Y=Y, dev_status=word)
+    assert word.item() == 1 << q8.Q8_ERR_INDEX and (whole[0] == 55).all() and (whole[-1] == 55).all()
+    ends = np.maximum.accumulate(np.clip(offsets, 0, T))
+    for e in range(3):
+        lo, hi = ends[e], ends[e + 1]
+        if hi > lo:
+            ref.assert_layer(Y[lo:hi], ref.rounded(x[lo:hi]), ref.rounded(w[e]), None, q8.Q8_ACT_NONE)
+    assert (Y[:ends[0]] == 55).all() and (Y[ends[-1]:] == 55).all()
+
+
+def test_grouped_bad_rows():
+    x, w = values((10, 96), 1), weights((2, 60, 96), 2)
+    rows = torch.tensor([0, 9, 10, -1, 3, 3, 2 ** 31 - 1, 5], dtype=torch.int32).cuda()
+    offsets = torch.tensor([0, 5, 7], dtype=torch.int32).cuda()
+    word = status_word()
+    Y = torch.full((8, 60), 55.0, device="cuda")
+    q8.q8_mx4_linear_grouped(x, offsets, q8.q8_mx4_quantize(w), rows=rows, Y=Y, dev_status=word)
+    assert word.item() == 1 << q8.Q8_ERR_INDEX
+    assert (Y[[2, 3, 6]] == 0).all() and (Y[7] == 55).all()
+    taken = x[rows.long().clamp(0, 9)].clone()
+    taken[[2, 3, 6]] = 0
+    ref.assert_layer(Y[:5], ref.rounded(taken[:5]), ref.rounded(w[0]), None, 0)
+    ref.assert_layer(Y[5:7], ref.rounded(taken[5:7]), ref.rounded(w[1]), None, 0)
+    word.zero_()
+    rows[:7] = 0
+    rows[7] = 99  # of a slot that no expert owns
+    q8.q8_mx4_linear_grouped(x, offsets, q8.q8_mx4_quantize(w), rows=rows, Y=Y, dev_status=word)
+    assert word.item() == 0
+
+
+# ---------------------------------------------------------------- as they are used
+def test_feed_forward_of_experts():
+    """Top-2 routing, two grouped layers with GELU between them, and the tokens put together again."""
+    tokens, E, H, F = 150, 6, 256, 520
+    g = torch.Generator().manual_seed(0)
+    x = values((tokens, H), 1, torch.bfloat16, 0.0)
+    choice = torch.rand(tokens, E, generator=g).topk(2, dim=1)
+    expert = choice.indices.flatten()
+    order = expert.argsort(stable=True)
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64), expert.bincount(minlength=E).cumsum(0)]).to(torch.int32).cuda()
+    rows = (order // 2).to(torch.int32).cuda()
+    w1, w2 = weights((E, F, H), 2), weights((E, H, F), 3)
+    h = q8.q8_mx4_linear_grouped(x, offsets, q8.q8_mx4_quantize(w1), None, q8.Q8_ACT_GELU, rows)
+    y = q8.q8_mx4_linear_grouped(h, offsets, q8.q8_mx4_quantize(w2))
+    out = torch.zeros(tokens, H, device="cuda").index_add_(0, rows.long(), y.float() * choice.values.flatten()[order].cuda()[:, None])
+    want, size = np.zeros((tokens, H)), np.zeros((tokens, H))
+    ends = offsets.tolist()
+    for e in range(E):
+        lo, hi = ends[e], ends[e + 1]
+        if lo == hi:
+            continue
+        taken = rows[lo:hi].long().cpu()
+        ref.assert_layer(h[lo:hi], ref.rounded(x[taken]), ref.rounded(w1[e]), None, q8.Q8_ACT_GELU)
+        ref.assert_layer(y[lo:hi], ref.rounded(h[lo:hi]), ref.rounded(w2[e]), None, q8.Q8_ACT_NONE)
+        part = ref.as_numpy(y[lo:hi]) * choice.values.flatten()[order][lo:hi, None].double().numpy()
+        np.add.at(want, taken.numpy(), part)
+        np.add.at(size, taken.numpy(), np.abs(part))
+    assert (np.abs(ref.as_numpy(out) - want) <= 4 * 2.0 ** -24 * size).all()  # a product and up to two additions in fp32
+
+
+def test_captured_and_replayed():
+    """Two layers and a grouped one in a graph, replayed on new inputs, one workspace for all of them."""
+    M, H, F, E = 70, 256, 384, 3
+    x = values((M, H), 1, torch.bfloat16, 0.0)
+    W1, W2, W3 = q8.q8_mx4_quantize(weights((F, H), 2)), q8.q8_mx4_quantize(weights((H, F), 3)), q8.q8_mx4_quantize(weights((E, F, H), 4))
+    offsets = torch.tensor([0, 20, 20, 65], dtype=torch.int32).cuda()
+    ws = torch.empty(max(q8.q8_mx4_linear_workspace_bytes(M, F), q8.q8_mx4_linear_grouped_workspace_bytes(M, E, H)), dtype=torch.uint8, device="cuda")
+    Y = torch.full((M, F), 9.0, dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        h = q8.q8_mx4_linear(x, W1, None, q8.Q8_ACT_GELU, workspace=ws)
+        y = q8.q8_mx4_linear(h, W2, workspace=ws)
+        q8.q8_mx4_linear_grouped(y, offsets, W3, Y=Y, workspace=ws)
+        return y
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = step()
+    for seed in (5, 6):
+        x.copy_(values((M, H), seed, torch.bfloat16, 0.0))
+        offsets.copy_(torch.tensor([0, 20, 20, 65] if seed == 5 else [0, 0, 50, 60], dtype=torch.int32))
+        Y.fill_(9.0)
+        graph.replay()
+        replayed = (y.clone(), Y.clone())
+        Y.fill_(9.0)
+        assert torch.equal(step(), replayed[0]) and torch.equal(Y, replayed[1])
+
+
+def test_other_streams_and_repeated_calls():
+    x, w = values((200, 512), 1), weights((640, 512), 2)
+    W = q8.q8_mx4_quantize(w)
+    want = q8.q8_mx4_linear(x, W)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    results = [q8.q8_mx4_linear(x, W, stream=side) for _ in range(20)] + [q8.q8_mx4_linear(x, W) for _ in range(20)]
+    with torch.cuda.stream(side):
+        results.append(q8.q8_mx4_linear(x, q8.q8_mx4_quantize(w)))
+        results.append(q8.q8_mx4_linear_q(q8.q8_mx4_quantize(x), q8.q8_mx4_quantize(w)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(r, want) for r in results)
+
+
+def test_weights_made_right_before_the_layer():
+    """The layer starts while the kernel before it still runs; weights and offsets that earlier kernels write are there in time."""
+    x = values((64, 1024), 1)
+    ws = [weights((2048, 1024), s) for s in range(6)]
+    want = []
+    for w in ws:
+        W = q8.q8_mx4_quantize(w)
+        torch.cuda.synchronize()
+        want.append(q8.q8_mx4_linear(x, W))
+        torch.cuda.synchronize()
+    W = q8.q8_mx4_quantize(ws[0])
+    got = []
+    for w in ws:
+        fresh = q8.q8_mx4_quantize(w)
+        W.codes.copy_(fresh.codes)
+        W.scales.copy_(fresh.scales)
+        got.append(q8.q8_mx4_linear(x, W))
+        fresh = q8.q8_mx4_quantize(w)
+        got.append(q8.q8_mx4_linear(x, fresh))
+    assert all(torch.equal(a, b) for a, b in zip(got, [v for v in want for _ in range(2)]))
+
+
+def test_refusals_on_the_device():
+    x, w = values((4, 64), 1), weights((8, 64), 2)
+    W = q8.q8_mx4_quantize(w)
+    with pytest.raises(ValueError, match="rows of 64"):
+        q8.q8_mx4_linear(values((4, 65), 1), W)
+    with pytest.raises(ValueError, match="bias has 7"):
+        q8.q8_mx4_linear(x, W, weights((7,), 1))
+    with pytest.raises(ValueError, match="Y must be"):
+        q8.q8_mx4_linear(x, W, Y=torch.empty(4, 9, device="cuda"))
+    with pytest.raises(TypeError, match="asked for"):
+        q8.q8_mx4_linear(x, W, Y=torch.empty(4, 8, device="cuda"), dtype=torch.float16)
+    with pytest.raises(TypeError, match="float32, float16 or bfloat16"):
+        q8.q8_mx4_linear(x.double(), W)
+    with pytest.raises(TypeError, match="side by side"):
+        q8.q8_mx4_linear(values((64, 4), 1).t(), W)
+    with pytest.raises(TypeError, match="overlap"):
+        q8.q8_mx4_linear(values((1, 64), 1).expand(4, 64), W)
+    with pytest.raises(ValueError, match="bytes of scales"):
+        q8.q8_mx4_linear(x, q8.Mx4(W.codes, W.scales[:100], W.K))
+    with pytest.raises(ValueError, match="do not hold"):
+        q8.q8_mx4_linear(x, q8.Mx4(W.codes, W.scales, 65))
+    with pytest.raises(q8.Q8Error) as e:
+        q8.q8_mx4_linear(x, W, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == q8.Q8_ERR_WORKSPACE
+    with pytest.raises(q8.Q8Error) as e:
+        q8.q8_mx4_linear(x, W, act=3)
+    assert e.value.status == q8.Q8_ERR_ARG
+    G = q8.q8_mx4_quantize(weights((2, 8, 64), 2))
+    with pytest.raises(ValueError, match="dimensions"):
+        q8.q8_mx4_linear(x, G)
+    with pytest.raises(ValueError, match="for 2 experts"):
+        q8.q8_mx4_linear_grouped(x, torch.zeros(2, dtype=torch.int32, device="cuda"), G)
+    with pytest.raises(TypeError, match="offsets must be torch.int32"):
+        q8.q8_mx4_linear_grouped(x, torch.zeros(3, dtype=torch.int64, device="cuda"), G)
+    torch.cuda.synchronize()

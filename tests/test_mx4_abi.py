@@ -1,0 +1,123 @@
+"""Host-only checks of the MXFP4 entry points: sizes, refusals before anything touches the device, and what the reference itself does."""
+import numpy as np
+import pytest
+import torch
+
+from paper_1910_06188_b200 import binding as q8
+from paper_1910_06188_b200 import build
+from tests import mx4_reference as ref
+
+FAKE = 0x10000  # never dereferenced
+MANY = 1 << 60
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return q8.load()
+
+
+def test_sizes(lib):
+    assert [q8.q8_mx4_codes_bytes(5, K) for K in (1, 32, 33, 1000)] == [80, 80, 160, 2560]
+    assert [q8.q8_mx4_scales_bytes(1, r, K) for r, K in ((1, 1), (128, 128), (129, 128), (128, 129), (0, 5))] == [512, 512, 1024, 1024, 0]
+    assert q8.q8_mx4_scales_bytes(3, 130, 300) == 3 * 2 * 3 * 512
+    assert q8.q8_mx4_codes_bytes(-1, 4) == q8.q8_mx4_codes_bytes(4, 0) == q8.q8_mx4_scales_bytes(1 << 30, 4, 4) == 0
+    assert q8.q8_mx4_linear_workspace_bytes(3, 64) == 256 + 512
+    assert q8.q8_mx4_linear_grouped_workspace_bytes(300, 7, 64) == 9728 + (2 + 7) * 512
+    assert q8.q8_mx4_linear_grouped_workspace_bytes(4, 1000, 64) == 256 + 4 * 512
+    assert q8.q8_mx4_linear_grouped_workspace_bytes(4, 1025, 64) == 0
+
+
+def linear(lib, X=FAKE, xt=0, ldx=64, Wq=FAKE, Ws=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, M=4, N=8, K=64, ws=FAKE, size=MANY, word=None):
+    return lib.q8_mx4_linear(X, xt, ldx, Wq, Ws, bias, act, Y, yt, ldy, M, N, K, ws, size, word, None)
+
+
+def linear_q(lib, Xq=FAKE, Xs=FAKE, Wq=FAKE, Ws=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, M=4, N=8, K=64, word=None):
+    return lib.q8_mx4_linear_q(Xq, Xs, Wq, Ws, bias, act, Y, yt, ldy, M, N, K, word, None)
+
+
+def grouped(lib, X=FAKE, xt=0, ldx=64, x_rows=4, rows=None, offsets=FAKE, E=3, Wq=FAKE, Ws=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, T=4, N=8, K=64,
+            ws=FAKE, size=MANY, word=None):
+    return lib.q8_mx4_linear_grouped(X, xt, ldx, x_rows, rows, offsets, E, Wq, Ws, bias, act, Y, yt, ldy, T, N, K, ws, size, word, None)
+
+
+def quantize(lib, X=FAKE, t=0, G=1, R=4, K=64, ld=64, codes=FAKE, scales=FAKE, word=None):
+    return lib.q8_mx4_quantize(X, t, G, R, K, ld, codes, scales, word, None)
+
+
+def dequantize(lib, codes=FAKE, scales=FAKE, G=1, R=4, K=64, Y=FAKE, t=0, ld=64):
+    return lib.q8_mx4_dequantize(codes, scales, G, R, K, Y, t, ld, None)
+
+
+def fake(lib, X=FAKE, t=0, R=4, K=64, ld=64, out=FAKE, ldo=64, word=None):
+    return lib.q8_mx4_fake_quantize(X, t, R, K, ld, out, ldo, word, None)
+
+
+@pytest.mark.parametrize("call,arguments,status", [
+    *[(linear, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "Wq", "Ws", "Y", "ws")],
+    *[(linear_q, {k: None}, q8.Q8_ERR_NULL) for k in ("Xq", "Xs", "Wq", "Ws", "Y")],
+    *[(grouped, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "offsets", "Wq", "Ws", "Y", "ws")],
+    *[(quantize, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "codes", "scales")],
+    *[(dequantize, {k: None}, q8.Q8_ERR_NULL) for k in ("Y", "codes", "scales")],
+    *[(fake, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "out")],
+    *[(call, {k: 3}, q8.Q8_ERR_ARG) for call in (linear, grouped) for k in ("xt", "yt", "act")],
+    *[(call, {"t": 7}, q8.Q8_ERR_ARG) for call in (quantize, dequantize, fake)],
+    (linear_q, {"act": -1}, q8.Q8_ERR_ARG), (linear_q, {"yt": 3}, q8.Q8_ERR_ARG),
+    (fake, {"X": FAKE, "out": FAKE, "ldo": 65}, q8.Q8_ERR_ARG),
+    *[(call, bad, q8.Q8_ERR_SHAPE) for call in (linear, linear_q) for bad in (
+        {"M": -1}, {"N": -1}, {"K": 0}, {"K": -5}, {"K": (1 << 24) + 1, "ldx": 1 << 30} if call is linear else {"K": (1 << 24) + 1}, {"ldy": 7},
+        {"M": 1 << 31}, {"N": 1 << 31, "ldy": 1 << 32}, {"M": 1 << 30, "N": 1 << 30, "ldy": 1 << 30})],
+    (linear, {"ldx": 63}, q8.Q8_ERR_SHAPE),
+    *[(grouped, bad, q8.Q8_ERR_SHAPE) for bad in (
+        {"T": -1}, {"T": 5}, {"E": -1}, {"E": 1025}, {"x_rows": -1}, {"x_rows": 3}, {"K": 0}, {"ldx": 1}, {"ldy": 7}, {"N": 1 << 30, "ldy": 1 << 30})],
+    *[(quantize, bad, q8.Q8_ERR_SHAPE) for bad in ({"G": -1}, {"R": -1}, {"K": 0}, {"ld": 63}, {"G": 1 << 20, "R": 1 << 20})],
+    (dequantize, {"ld": 1}, q8.Q8_ERR_SHAPE), (fake, {"ld": 1}, q8.Q8_ERR_SHAPE), (fake, {"ldo": 1}, q8.Q8_ERR_SHAPE),
+    *[(linear, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("X", 2), ("Wq", 8), ("Ws", 8), ("bias", 2), ("Y", 2), ("ws", 128), ("word", 2))],
+    *[(linear_q, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("Xq", 8), ("Xs", 8), ("Wq", 8), ("Ws", 8), ("bias", 2), ("Y", 2), ("word", 2))],
+    *[(grouped, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("X", 2), ("rows", 2), ("offsets", 2), ("Wq", 8), ("Ws", 8), ("bias", 2), ("Y", 2), ("ws", 128))],
+    (linear, {"xt": 1, "X": FAKE + 1}, q8.Q8_ERR_ALIGN), (quantize, {"X": FAKE + 2}, q8.Q8_ERR_ALIGN), (quantize, {"codes": FAKE + 4}, q8.Q8_ERR_ALIGN),
+    (dequantize, {"scales": FAKE + 4}, q8.Q8_ERR_ALIGN), (fake, {"out": FAKE + 1}, q8.Q8_ERR_ALIGN),
+    (linear, {"size": 256 + 511}, q8.Q8_ERR_WORKSPACE), (grouped, {"size": 256 + 3 * 512 - 1}, q8.Q8_ERR_WORKSPACE),
+    # nothing to do: never reaches the device
+    *[(call, {k: 0}, q8.Q8_OK) for call in (linear, linear_q) for k in ("M", "N")], *[(grouped, {k: 0}, q8.Q8_OK) for k in ("T", "N", "E")],
+    *[(quantize, {k: 0, "X": None}, q8.Q8_OK) for k in ("G", "R")], (dequantize, {"R": 0}, q8.Q8_OK), (fake, {"R": 0, "X": None}, q8.Q8_OK)])
+def test_refusals(lib, call, arguments, status):
+    assert call(lib, **arguments) == status
+
+
+def test_tensors_of_the_host_are_refused(lib):
+    W = q8.Mx4(torch.zeros(8, 32, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8), 64)
+    with pytest.raises(TypeError, match="X must be a CUDA tensor"):
+        q8.q8_mx4_quantize(torch.zeros(4, 64))
+    with pytest.raises(TypeError, match="CUDA tensor"):
+        q8.q8_mx4_linear(torch.zeros(4, 64), W)
+    with pytest.raises(TypeError, match="CUDA tensor"):
+        q8.q8_mx4_dequantize(W)
+    with pytest.raises(TypeError, match="CUDA tensor"):
+        q8.q8_mx4_fake_quantize(torch.zeros(4, 64))
+    with pytest.raises(ValueError, match="2 or 3 dimensions"):
+        q8.q8_mx4_quantize(torch.zeros(64))
+
+
+# ---------------------------------------------------------------- the reference
+def test_reference_rounds_to_the_nearest_of_all_values():
+    r = np.random.RandomState(0)
+    x = r.standard_normal((200, 64)) * np.exp(r.standard_normal((200, 1)) * 20)
+    code, E = ref.quantize(x)
+    got = ref.values(code, E, 64).reshape(200, 2, 32)
+    every = np.concatenate([ref.GRID, -ref.GRID])[None, None, None, :] * 2.0 ** (E - 127.0)[..., None, None]
+    off = np.abs(x.reshape(200, 2, 32)[..., None] - every).min(-1)
+    assert np.array_equal(np.abs(x.reshape(200, 2, 32) - got), off)
+    top = np.abs(x).reshape(200, 2, 32).max(-1) / 2.0 ** (E - 127.0)
+    assert ((top >= 4) & (top < 8)).all()
+
+
+def test_reference_on_an_example_by_hand():
+    """max 5 -> s = 2^(2 - 2) = 1; 0.25, 2.5, 5 are ties and go to 0, 2, 4; 0.75 goes to 1, -3.5 to -4."""
+    x = np.zeros((1, 32))
+    x[0, :8] = [5, 0.25, 2.5, 0.75, -3.5, 0.3, -0.2, 1.6]
+    code, E = ref.quantize(x)
+    assert E.tolist() == [[127]]
+    assert ref.values(code, E, 8).tolist() == [[4, 0, 2, 1, -4, 0.5, 0, 1.5]]
+    assert code[0, :8].tolist() == [6, 0, 4, 2, 14, 1, 8, 3]
+    assert ref.values(*ref.quantize(x * 2.0 ** -30), 8).tolist() == (ref.values(code, E, 8) * 2.0 ** -30).tolist()
