@@ -93,7 +93,9 @@ _native_module = None
 _NATIVE_CALLS = ("q8_quantize_weight", "q8_fake_quantize", "q8_ste_backward", "q8_calibrate",
                  "q8_linear", "q8_linear_workspace_bytes", "q8_linear_q", "q8_linear_requant", "q8_linear_q_requant",
                  "q8_linear_dyn", "q8_embedding", "q8_add_layernorm", "q8_add_layernorm_quant", "q8_add_layernorm_absmax",
-                 "q8_attention", "q8_attention_quant", "q8_attention_absmax", "q8_embed_layernorm")
+                 "q8_attention", "q8_attention_quant", "q8_attention_absmax", "q8_embed_layernorm", "q8_mx4_quantize",
+                 "q8_mx4_dequantize", "q8_mx4_fake_quantize", "q8_mx4_scales_bytes", "q8_mx4_linear", "q8_mx4_linear_workspace_bytes",
+                 "q8_mx4_linear_q", "q8_mx4_linear_grouped", "q8_mx4_linear_grouped_workspace_bytes")
 
 
 class Q8Error(RuntimeError):
@@ -713,6 +715,10 @@ def q8_mx4_scales_bytes(groups: int, rows: int, K: int) -> int:
 
 def q8_mx4_quantize(X, dev_status=None, stream=None) -> Mx4:
     """X [rows, K], or [experts, rows, K] for the weights of q8_mx4_linear_grouped, in MXFP4."""
+    if stream is None:
+        r = (_native_module or _native()).mx4_quantize(X, dev_status)
+        if r is not NotImplemented:
+            return Mx4._make(r)
     if X.dim() not in (2, 3):
         raise ValueError(f"X must have 2 or 3 dimensions, got {tuple(X.shape)}")
     x, dtype, ld = _mx4_matrix(X, "X")
@@ -728,6 +734,10 @@ def q8_mx4_quantize(X, dev_status=None, stream=None) -> Mx4:
 
 def q8_mx4_dequantize(T: Mx4, dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
     """The values that the codes and scales of T stand for."""
+    if stream is None:
+        r = (_native_module or _native()).mx4_dequantize(T, dtype)
+        if r is not NotImplemented:
+            return r
     codes, scales, groups, rows, K = _mx4_parts(T, "T", T.codes.dim() if T.codes.dim() == 3 else 2)
     _mx4_same_device(T.codes, T.scales)
     Y = _mx4_empty((*T.codes.shape[:-1], K), dtype, T.codes.device, stream)
@@ -738,6 +748,10 @@ def q8_mx4_dequantize(T: Mx4, dtype: torch.dtype = torch.float32, stream=None) -
 
 def q8_mx4_fake_quantize(X, Xhat=None, dev_status=None, stream=None) -> torch.Tensor:
     """Training-mode MXFP4: the values that the codes of X [rows, K] stand for, in X's type; q8_ste_backward is its gradient."""
+    if stream is None:
+        r = (_native_module or _native()).mx4_fake_quantize(X, Xhat, dev_status)
+        if r is not NotImplemented:
+            return r
     if X.dim() != 2:
         raise ValueError(f"X must have 2 dimensions, got {tuple(X.shape)}")
     x, dtype, ld = _mx4_matrix(X, "X")
@@ -767,6 +781,10 @@ def _mx4_bias(bias, values: int):
 def q8_mx4_linear(X, W: Mx4, bias=None, act: int = Q8_ACT_NONE, Y=None, dtype: Optional[torch.dtype] = None, workspace=None,
                   dev_status=None, stream=None) -> torch.Tensor:
     """act(X_hat W_hat^T + b) with X [M, K] quantised on its way in; Y in X's type unless `dtype` or Y says otherwise."""
+    if stream is None:
+        r = (_native_module or _native()).mx4_linear(X, W, bias, act, Y, dtype, workspace, dev_status)
+        if r is not NotImplemented:
+            return r
     wq, ws, _, N, K = _mx4_parts(W, "W", 2)
     if X.dim() != 2 or X.shape[1] != K:
         raise ValueError(f"X is {tuple(X.shape)} but W has rows of {K}")
@@ -787,6 +805,10 @@ def q8_mx4_linear(X, W: Mx4, bias=None, act: int = Q8_ACT_NONE, Y=None, dtype: O
 def q8_mx4_linear_q(Xq: Mx4, W: Mx4, bias=None, act: int = Q8_ACT_NONE, Y=None, dtype: Optional[torch.dtype] = None,
                     dev_status=None, stream=None) -> torch.Tensor:
     """q8_mx4_linear on an activation that is quantised already; Y is fp32 unless `dtype` or Y says otherwise."""
+    if stream is None:
+        r = (_native_module or _native()).mx4_linear_q(Xq, W, bias, act, Y, dtype, dev_status)
+        if r is not NotImplemented:
+            return r
     wq, ws, _, N, K = _mx4_parts(W, "W", 2)
     xq, xs, _, M, K2 = _mx4_parts(Xq, "Xq", 2)
     if K2 != K:
@@ -805,6 +827,10 @@ def q8_mx4_linear_grouped(X, offsets, W: Mx4, bias=None, act: int = Q8_ACT_NONE,
     """The layer with one weight matrix per expert (W from a [experts, N, K] tensor, bias [experts, N]): Y[t] =
     act(X_hat[rows[t]] W_hat[e]^T + b[e]) for the slots offsets[e] <= t < offsets[e + 1]; without `rows` slot t takes row t.
     Rows of Y that no expert owns stay as they were (are uninitialised in a Y that this call makes)."""
+    if stream is None:
+        r = (_native_module or _native()).mx4_linear_grouped(X, offsets, W, bias, act, rows, Y, dtype, workspace, dev_status)
+        if r is not NotImplemented:
+            return r
     wq, ws, E, N, K = _mx4_parts(W, "W", 3)
     if X.dim() != 2 or X.shape[1] != K:
         raise ValueError(f"X is {tuple(X.shape)} but W has rows of {K}")

@@ -11,9 +11,11 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <limits>
+#include <vector>
 
 #include "q8.h"
 
@@ -24,7 +26,9 @@ namespace {
     X(q8_quantize_weight) X(q8_fake_quantize) X(q8_ste_backward) X(q8_calibrate) X(q8_linear)  \
     X(q8_linear_workspace_bytes) X(q8_linear_q) X(q8_linear_requant) X(q8_linear_q_requant) X(q8_linear_dyn)            \
     X(q8_embedding) X(q8_add_layernorm) X(q8_add_layernorm_quant) X(q8_add_layernorm_absmax) X(q8_attention)            \
-    X(q8_attention_quant) X(q8_attention_absmax) X(q8_embed_layernorm)
+    X(q8_attention_quant) X(q8_attention_absmax) X(q8_embed_layernorm)                                                  \
+    X(q8_mx4_quantize) X(q8_mx4_dequantize) X(q8_mx4_fake_quantize) X(q8_mx4_scales_bytes) X(q8_mx4_linear)             \
+    X(q8_mx4_linear_workspace_bytes) X(q8_mx4_linear_q) X(q8_mx4_linear_grouped) X(q8_mx4_linear_grouped_workspace_bytes)
 #define Q8_DECLARE(name) decltype(&::name) p_##name = nullptr;
 Q8_CALLS(Q8_DECLARE)
 PyObject *g_check = nullptr;  // binding._check(status, where): raises
@@ -466,6 +470,248 @@ PyObject *ste_backward(Args a)
     return out.result();
 }
 
+// ---- MXFP4
+// Values in rows: [rows, K] with any distance of rows, or a contiguous tensor of three dimensions, on the current device.
+struct Rows {
+    const at::Tensor *t = nullptr;
+    void *ptr = nullptr;
+    int dtype = 0;
+    int64_t ld = 0, groups = 1, rows = 0, K = 0;
+};
+bool same_device(const at::Tensor &t) { return t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
+int mx4_dtype(at::ScalarType t) { return t == at::kFloat ? Q8_F32 : t == at::kHalf ? Q8_F16 : t == at::kBFloat16 ? Q8_BF16 : -1; }
+bool rows_of(const at::Tensor &t, Rows *r)
+{
+    const int64_t dims = t.dim();
+    if ((dims != 2 && dims != 3) || !same_device(t)) return false;
+    r->t = &t;
+    r->dtype = mx4_dtype(t.scalar_type());
+    r->K = t.size(dims - 1);
+    r->rows = t.size(dims - 2);
+    if (r->dtype < 0) return false;
+    if (dims == 3) {
+        if (!t.is_contiguous()) return false;
+        r->groups = t.size(0);
+        r->ld = r->K;
+    } else {
+        if (t.stride(1) != 1 && r->K != 1) return false;
+        r->ld = r->rows > 1 ? t.stride(0) : r->K;
+        if (r->ld < r->K) return false;
+    }
+    r->ptr = t.data_ptr();
+    return true;
+}
+bool rows_of(Call &c, PyObject *o, int64_t dims, Rows *r)
+{
+    const at::Tensor *t = c.tensor(o);
+    if (t == nullptr || (dims != 0 && t->dim() != dims) || !rows_of(*t, r)) c.plain = false;
+    return c.plain;
+}
+// A contiguous tensor on the current device (nullptr for None), of exactly `values` values where that is not negative
+template <typename T>
+T *mx4_ptr(Call &c, PyObject *o, at::ScalarType type, int64_t values = -1)
+{
+    T *p = c.ptr<T>(o, type);
+    if (c.plain && o != Py_None) {
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!same_device(t) || (values >= 0 && t.numel() != values)) c.plain = false;
+    }
+    return p;
+}
+// The parts of a quantised tensor (codes, scales, K)
+struct Quantized {
+    const uint8_t *codes = nullptr, *scales = nullptr;
+    const at::Tensor *t = nullptr;
+    int64_t groups = 1, rows = 0, K = 0;
+    Quantized(Call &c, PyObject *o, int64_t dims)
+    {
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3) {
+            c.plain = false;
+            return;
+        }
+        codes = mx4_ptr<const uint8_t>(c, PyTuple_GET_ITEM(o, 0), at::kByte);
+        scales = mx4_ptr<const uint8_t>(c, PyTuple_GET_ITEM(o, 1), at::kByte);
+        K = c.integer(PyTuple_GET_ITEM(o, 2));
+        if (!c.plain || PyTuple_GET_ITEM(o, 0) == Py_None || PyTuple_GET_ITEM(o, 1) == Py_None || K < 1) {
+            c.plain = false;
+            return;
+        }
+        t = &THPVariable_Unpack(PyTuple_GET_ITEM(o, 0));
+        const int64_t d = t->dim();
+        if ((d != 2 && d != 3) || (dims != 0 && d != dims) || t->size(d - 1) != 16 * ((K - 1) / 32 + 1)) {
+            c.plain = false;
+            return;
+        }
+        groups = d == 3 ? t->size(0) : 1;
+        rows = t->size(d - 2);
+        if ((size_t)THPVariable_Unpack(PyTuple_GET_ITEM(o, 1)).numel() < p_q8_mx4_scales_bytes(groups, rows, K)) c.plain = false;
+    }
+};
+// None or a torch.dtype
+bool dtype_or(PyObject *o, at::ScalarType otherwise, at::ScalarType *out)
+{
+    *out = o == Py_None ? otherwise : THPDtype_Check(o) ? reinterpret_cast<THPDtype *>(o)->scalar_type : at::kByte;
+    return mx4_dtype(*out) >= 0;
+}
+// Y that the caller gave (which `dtype`, if given, has to agree with) or a new one
+struct Mx4Output {
+    PyObject *given;
+    at::Tensor made;
+    Rows r;
+    Mx4Output(Call &c, PyObject *o, PyObject *dtype, at::ScalarType otherwise, int64_t M, int64_t N, const at::Tensor &like) : given(o)
+    {
+        at::ScalarType type;
+        if (!c.plain) return;
+        if (o == Py_None) {
+            if (!dtype_or(dtype, otherwise, &type)) {
+                c.plain = false;
+                return;
+            }
+            made = at::empty({M, N}, at::TensorOptions().dtype(type).device(like.device()));
+            if (!rows_of(made, &r)) c.plain = false;
+        } else {
+            if (!rows_of(c, o, 2, &r)) return;
+            if (r.rows != M || r.K != N || (dtype != Py_None && (!dtype_or(dtype, otherwise, &type) || type != r.t->scalar_type()))) c.plain = false;
+        }
+    }
+    PyObject *result() { return given == Py_None ? THPVariable_Wrap(made) : Py_NewRef(given); }
+};
+struct Mx4Workspace {
+    at::Tensor made;
+    void *ptr = nullptr;
+    size_t bytes = 0;
+    Mx4Workspace(Call &c, PyObject *o, size_t need, const at::Tensor &like)
+    {
+        if (!c.plain) return;
+        if (o == Py_None) {
+            bytes = need;
+            made = at::empty({(int64_t)need}, at::TensorOptions().dtype(at::kByte).device(like.device()));
+            ptr = made.data_ptr();
+        } else {
+            ptr = c.any_ptr(o, &bytes);
+            if (c.plain && !same_device(THPVariable_Unpack(o))) c.plain = false;
+        }
+    }
+};
+
+// (X, dev_status) -> (codes, scales, K)
+PyObject *mx4_quantize(Args a)
+{
+    Call c;
+    Rows x;
+    if (!rows_of(c, a[0], 0, &x)) return other_form();
+    auto status = mx4_ptr<int32_t>(c, a[1], kI32);
+    if (!c.plain || x.K < 1) return other_form();
+    std::vector<int64_t> shape = x.t->sizes().vec();
+    shape.back() = 16 * ((x.K - 1) / 32 + 1);
+    const auto bytes = at::TensorOptions().dtype(at::kByte).device(x.t->device());
+    at::Tensor codes = at::empty(shape, bytes), scales = at::empty({(int64_t)p_q8_mx4_scales_bytes(x.groups, x.rows, x.K)}, bytes);
+    auto q = static_cast<uint8_t *>(codes.data_ptr()), w = static_cast<uint8_t *>(scales.data_ptr());
+    if (!run("q8_mx4_quantize", [&](void *s) { return p_q8_mx4_quantize(x.ptr, x.dtype, x.groups, x.rows, x.K, x.ld, q, w, status, s); })) return nullptr;
+    PyObject *r = PyTuple_New(3);
+    if (r == nullptr) return nullptr;
+    PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(codes));
+    PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(scales));
+    PyTuple_SET_ITEM(r, 2, PyLong_FromLongLong(x.K));
+    return r;
+}
+
+// (T, dtype)
+PyObject *mx4_dequantize(Args a)
+{
+    Call c;
+    Quantized t(c, a[0], 0);
+    at::ScalarType type;
+    if (!c.plain || !dtype_or(a[1], at::kFloat, &type)) return other_form();
+    std::vector<int64_t> shape = t.t->sizes().vec();
+    shape.back() = t.K;
+    at::Tensor y = at::empty(shape, at::TensorOptions().dtype(type).device(t.t->device()));
+    void *p = y.data_ptr();
+    if (!run("q8_mx4_dequantize", [&](void *s) { return p_q8_mx4_dequantize(t.codes, t.scales, t.groups, t.rows, t.K, p, mx4_dtype(type), t.K, s); }))
+        return nullptr;
+    return THPVariable_Wrap(y);
+}
+
+// (X, Xhat, dev_status)
+PyObject *mx4_fake_quantize(Args a)
+{
+    Call c;
+    Rows x;
+    if (!rows_of(c, a[0], 2, &x)) return other_form();
+    auto status = mx4_ptr<int32_t>(c, a[2], kI32);
+    Mx4Output out(c, a[1], Py_None, x.t->scalar_type(), x.rows, x.K, *x.t);
+    if (!c.plain || x.K < 1 || out.r.dtype != x.dtype) return other_form();
+    if (!run("q8_mx4_fake_quantize", [&](void *s) { return p_q8_mx4_fake_quantize(x.ptr, x.dtype, x.rows, x.K, x.ld, out.r.ptr, out.r.ld, status, s); }))
+        return nullptr;
+    return out.result();
+}
+
+// (X, W, bias, act, Y, dtype, workspace, dev_status)
+PyObject *mx4_linear(Args a)
+{
+    Call c;
+    Rows x;
+    if (!rows_of(c, a[0], 2, &x)) return other_form();
+    Quantized w(c, a[1], 2);
+    auto bias = mx4_ptr<const float>(c, a[2], kF32, w.rows);
+    const int act = c.small(a[3]);
+    auto status = mx4_ptr<int32_t>(c, a[7], kI32);
+    if (!c.plain || w.K != x.K) return other_form();
+    Mx4Output y(c, a[4], a[5], x.t->scalar_type(), x.rows, w.rows, *x.t);
+    Mx4Workspace ws(c, a[6], p_q8_mx4_linear_workspace_bytes(x.rows, x.K), *x.t);
+    if (!c.plain) return other_form();
+    if (!run("q8_mx4_linear", [&](void *s) {
+            return p_q8_mx4_linear(x.ptr, x.dtype, x.ld, w.codes, w.scales, bias, act, y.r.ptr, y.r.dtype, y.r.ld, x.rows, w.rows, x.K, ws.ptr, ws.bytes,
+                                   status, s);
+        }))
+        return nullptr;
+    return y.result();
+}
+
+// (Xq, W, bias, act, Y, dtype, dev_status)
+PyObject *mx4_linear_q(Args a)
+{
+    Call c;
+    Quantized x(c, a[0], 2), w(c, a[1], 2);
+    auto bias = mx4_ptr<const float>(c, a[2], kF32, w.rows);
+    const int act = c.small(a[3]);
+    auto status = mx4_ptr<int32_t>(c, a[6], kI32);
+    if (!c.plain || w.K != x.K) return other_form();
+    Mx4Output y(c, a[4], a[5], kF32, x.rows, w.rows, *x.t);
+    if (!c.plain) return other_form();
+    if (!run("q8_mx4_linear_q", [&](void *s) {
+            return p_q8_mx4_linear_q(x.codes, x.scales, w.codes, w.scales, bias, act, y.r.ptr, y.r.dtype, y.r.ld, x.rows, w.rows, x.K, status, s);
+        }))
+        return nullptr;
+    return y.result();
+}
+
+// (X, offsets, W, bias, act, rows, Y, dtype, workspace, dev_status)
+PyObject *mx4_linear_grouped(Args a)
+{
+    Call c;
+    Rows x;
+    if (!rows_of(c, a[0], 2, &x)) return other_form();
+    Quantized w(c, a[2], 3);
+    if (!c.plain || w.K != x.K || a[1] == Py_None) return other_form();
+    auto offsets = mx4_ptr<const int32_t>(c, a[1], kI32, w.groups + 1);
+    auto bias = mx4_ptr<const float>(c, a[3], kF32, w.groups * w.rows);
+    const int act = c.small(a[4]);
+    auto rows = mx4_ptr<const int32_t>(c, a[5], kI32);
+    auto status = mx4_ptr<int32_t>(c, a[9], kI32);
+    if (!c.plain) return other_form();
+    const int64_t T = a[5] == Py_None ? x.rows : THPVariable_Unpack(a[5]).numel();
+    Mx4Output y(c, a[6], a[7], x.t->scalar_type(), T, w.rows, *x.t);
+    Mx4Workspace ws(c, a[8], p_q8_mx4_linear_grouped_workspace_bytes(T, w.groups, x.K), *x.t);
+    if (!c.plain) return other_form();
+    if (!run("q8_mx4_linear_grouped", [&](void *s) {
+            return p_q8_mx4_linear_grouped(x.ptr, x.dtype, x.ld, x.rows, rows, offsets, w.groups, w.codes, w.scales, bias, act, y.r.ptr, y.r.dtype, y.r.ld, T,
+                                           w.rows, x.K, ws.ptr, ws.bytes, status, s);
+        }))
+        return nullptr;
+    return y.result();
+}
+
 // A C++ exception (a tensor without storage, an allocation that fails) leaves the call to its Python form.
 template <PyObject *(*F)(Args), int COUNT>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t count)
@@ -523,6 +769,12 @@ PyMethodDef kMethods[] = {
     Q8_ENTRY("calibrate", calibrate, 3),
     Q8_ENTRY("fake_quantize", fake_quantize, 3),
     Q8_ENTRY("ste_backward", ste_backward, 2),
+    Q8_ENTRY("mx4_quantize", mx4_quantize, 2),
+    Q8_ENTRY("mx4_dequantize", mx4_dequantize, 2),
+    Q8_ENTRY("mx4_fake_quantize", mx4_fake_quantize, 3),
+    Q8_ENTRY("mx4_linear", mx4_linear, 8),
+    Q8_ENTRY("mx4_linear_q", mx4_linear_q, 7),
+    Q8_ENTRY("mx4_linear_grouped", mx4_linear_grouped, 10),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_q8_native", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
