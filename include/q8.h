@@ -278,26 +278,26 @@ q8_status q8_attention_status_word(void **dev_status);
  * number among 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives that is nearest to x / s, ties to the even mantissa, 6 where x / s is
  * above it.  The last block of a row may be short.  A NaN is held as 0, an infinity as 6 s; neither enters max|x|, and either flags
  * Q8_ERR_SCALE in dev_status (the other values are as if it were not there).  A block of zeros is zeros, no condition.
- *   codes   q8_mx4_codes_bytes(rows, K) bytes: rows of 16 ceil(K / 32) bytes, two codes to a byte, the lower column in the lower
- *           four bits (bit 3 the sign, bits 2-1 the exponent, bit 0 the mantissa), 0 behind column K
- *   scales  q8_mx4_scales_bytes(groups, rows, K) bytes: the exponents E of s = 2^(E - 127) in atoms of 128 rows x 4 blocks, each
- *           512 bytes: row r, block b of an atom at byte 16 (r % 32) + 4 (r / 32) + b; atom (i, j) of ceil(rows / 128) x ceil(K /
- *           128) at 512 (i ceil(K / 128) + j); every group (the matrix of one expert) begins a row of atoms of its own
+ * In memory: q8_mx4_bytes(groups, rows, K) bytes of tiles of 128 rows x 256 columns, 17408 bytes each, tile (i, j) of
+ * ceil(rows / 128) x ceil(K / 256) at 17408 (i ceil(K / 256) + j); every group (the matrix of one expert) begins a row of tiles of its own.
+ *   16384 bytes of codes: row r at 128 r, block b (16 bytes) at place b ^ (r % 8) of it; two codes to a byte, the lower column in
+ *     the lower four bits (bit 3 the sign, bits 2-1 the exponent, bit 0 the mantissa); 0 behind column K
+ *   1024 bytes of scales, the exponents E of s = 2^(E - 127): row r, block b at byte 512 (b / 4) + 16 (r % 32) + 4 (r / 32) + b % 4;
+ *     0 behind the last block
  * Common to the calls below: dtype is one of Q8_F32, Q8_F16, Q8_BF16; ld* is the distance of two rows in values (at least their
- * length); codes and scales are 16-byte aligned, values aligned to their type; 1 <= K <= 2^24, rows below 2^31 - 512;
+ * length); tiles are 16-byte aligned, values aligned to their type; 1 <= K <= 2^24, rows below 2^31 - 512;
  * dev_status (may be NULL) is OR-ed into, never cleared; calls that share a workspace must be ordered on the stream.  Zero rows or
  * features are a no-op. */
 #define Q8_F32 0
 #define Q8_F16 1
 #define Q8_BF16 2
-size_t q8_mx4_codes_bytes(int64_t rows, int64_t K);
-size_t q8_mx4_scales_bytes(int64_t groups, int64_t rows, int64_t K);
+size_t q8_mx4_bytes(int64_t groups, int64_t rows, int64_t K);
 
-/* X [groups, rows, K] (group stride rows * ldx) into codes and scales, and back: Y [groups * rows, K] rounded once to its type. */
-q8_status q8_mx4_quantize(const void *X, int dtype, int64_t groups, int64_t rows, int64_t K, int64_t ldx, uint8_t *codes,
-                          uint8_t *scales, int32_t *dev_status, void *stream);
-q8_status q8_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t groups, int64_t rows, int64_t K, void *Y,
-                            int dtype, int64_t ldy, void *stream);
+/* X [groups, rows, K] (group stride rows * ldx) into the tiles T, and back: Y [groups * rows, K] rounded once to its type. */
+q8_status q8_mx4_quantize(const void *X, int dtype, int64_t groups, int64_t rows, int64_t K, int64_t ldx, uint8_t *T,
+                          int32_t *dev_status, void *stream);
+q8_status q8_mx4_dequantize(const uint8_t *T, int64_t groups, int64_t rows, int64_t K, void *Y, int dtype, int64_t ldy,
+                            void *stream);
 /* The same rounding in training: Xhat = the values that X's codes stand for, in X's type (Xhat may be X, with the same ld).  Its
  * gradient is Eq. 5's straight-through one: q8_ste_backward. */
 q8_status q8_mx4_fake_quantize(const void *X, int dtype, int64_t rows, int64_t K, int64_t ldx, void *Xhat, int64_t ldo,
@@ -308,10 +308,10 @@ q8_status q8_mx4_fake_quantize(const void *X, int dtype, int64_t rows, int64_t K
  *   workspace: >= q8_mx4_linear_workspace_bytes(M, K) bytes, 256-byte aligned, contents of no account.
  * Results are deterministic.  q8_mx4_linear_q: the same on an activation that is quantised already (no workspace). */
 size_t q8_mx4_linear_workspace_bytes(int64_t M, int64_t K);
-q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *Wq, const uint8_t *Ws, const float *bias, int act,
+q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *Wq, const float *bias, int act,
                         void *Y, int y_dtype, int64_t ldy, int64_t M, int64_t N, int64_t K, void *workspace,
                         size_t workspace_bytes, int32_t *dev_status, void *stream);
-q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Xs, const uint8_t *Wq, const uint8_t *Ws, const float *bias, int act,
+q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Wq, const float *bias, int act,
                           void *Y, int y_dtype, int64_t ldy, int64_t M, int64_t N, int64_t K, int32_t *dev_status, void *stream);
 
 /* The same with a weight matrix for each of up to 1024 experts: W [experts, N, K] (q8_mx4_quantize with groups = experts), bias
@@ -322,7 +322,7 @@ q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Xs, const uint8_t *W
  * Q8_ERR_INDEX in dev_status. */
 size_t q8_mx4_linear_grouped_workspace_bytes(int64_t T, int64_t experts, int64_t K);
 q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t x_rows, const int32_t *rows,
-                                const int32_t *offsets, int64_t experts, const uint8_t *Wq, const uint8_t *Ws, const float *bias,
+                                const int32_t *offsets, int64_t experts, const uint8_t *Wq, const float *bias,
                                 int act, void *Y, int y_dtype, int64_t ldy, int64_t T, int64_t N, int64_t K, void *workspace,
                                 size_t workspace_bytes, int32_t *dev_status, void *stream);
 

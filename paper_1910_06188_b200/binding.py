@@ -56,16 +56,15 @@ SIGNATURES = {
     "q8_linear_q_requant": (_int, [_vp, _vp, _vp, _vp, _vp, _int, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp]),
     "q8_add_layernorm_quant": (_int, [_vp, _vp, _vp, _vp, _vp, _f, _i64, _i64, _vp, _vp, _vp, _vp]),
     "q8_attention_quant": (_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp]),
-    "q8_mx4_codes_bytes": (_sz, [_i64, _i64]),
-    "q8_mx4_scales_bytes": (_sz, [_i64, _i64, _i64]),
-    "q8_mx4_quantize": (_int, [_vp, _int, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp]),
-    "q8_mx4_dequantize": (_int, [_vp, _vp, _i64, _i64, _i64, _vp, _int, _i64, _vp]),
+    "q8_mx4_bytes": (_sz, [_i64, _i64, _i64]),
+    "q8_mx4_quantize": (_int, [_vp, _int, _i64, _i64, _i64, _i64, _vp, _vp, _vp]),
+    "q8_mx4_dequantize": (_int, [_vp, _i64, _i64, _i64, _vp, _int, _i64, _vp]),
     "q8_mx4_fake_quantize": (_int, [_vp, _int, _i64, _i64, _i64, _vp, _i64, _vp, _vp]),
     "q8_mx4_linear_workspace_bytes": (_sz, [_i64, _i64]),
-    "q8_mx4_linear": (_int, [_vp, _int, _i64, _vp, _vp, _vp, _int, _vp, _int, _i64, _i64, _i64, _i64, _vp, _sz, _vp, _vp]),
-    "q8_mx4_linear_q": (_int, [_vp, _vp, _vp, _vp, _vp, _int, _vp, _int, _i64, _i64, _i64, _i64, _vp, _vp]),
+    "q8_mx4_linear": (_int, [_vp, _int, _i64, _vp, _vp, _int, _vp, _int, _i64, _i64, _i64, _i64, _vp, _sz, _vp, _vp]),
+    "q8_mx4_linear_q": (_int, [_vp, _vp, _vp, _int, _vp, _int, _i64, _i64, _i64, _i64, _vp, _vp]),
     "q8_mx4_linear_grouped_workspace_bytes": (_sz, [_i64, _i64, _i64]),
-    "q8_mx4_linear_grouped": (_int, [_vp, _int, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _int, _vp, _int, _i64, _i64, _i64, _i64,
+    "q8_mx4_linear_grouped": (_int, [_vp, _int, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _int, _vp, _int, _i64, _i64, _i64, _i64,
                                      _vp, _sz, _vp, _vp]),
     "q8_poll_status": (_int, [_vp, C.POINTER(C.c_uint32), _vp]),
     "q8_status_string": (C.c_char_p, [_int]),
@@ -94,7 +93,7 @@ _NATIVE_CALLS = ("q8_quantize_weight", "q8_fake_quantize", "q8_ste_backward", "q
                  "q8_linear", "q8_linear_workspace_bytes", "q8_linear_q", "q8_linear_requant", "q8_linear_q_requant",
                  "q8_linear_dyn", "q8_embedding", "q8_add_layernorm", "q8_add_layernorm_quant", "q8_add_layernorm_absmax",
                  "q8_attention", "q8_attention_quant", "q8_attention_absmax", "q8_embed_layernorm", "q8_mx4_quantize",
-                 "q8_mx4_dequantize", "q8_mx4_fake_quantize", "q8_mx4_scales_bytes", "q8_mx4_linear", "q8_mx4_linear_workspace_bytes",
+                 "q8_mx4_dequantize", "q8_mx4_fake_quantize", "q8_mx4_bytes", "q8_mx4_linear", "q8_mx4_linear_workspace_bytes",
                  "q8_mx4_linear_q", "q8_mx4_linear_grouped", "q8_mx4_linear_grouped_workspace_bytes")
 
 
@@ -638,11 +637,10 @@ _MX4_DTYPES = {torch.float32: Q8_F32, torch.float16: Q8_F16, torch.bfloat16: Q8_
 
 
 class Mx4(NamedTuple):
-    """A tensor in microscaled 4-bit floating point; include/q8.h has the layout of its parts."""
+    """A tensor [rows, K] or [groups, rows, K] in microscaled 4-bit floating point; include/q8.h has the layout of its tiles."""
 
-    codes: torch.Tensor  # uint8 [..., rows, 16 ceil(K / 32)]
-    scales: torch.Tensor  # uint8, one row of atoms after the other
-    K: int
+    tiles: torch.Tensor  # uint8
+    shape: Tuple[int, ...]
 
 
 def _mx4_matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
@@ -663,18 +661,16 @@ def _mx4_matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
     return t.data_ptr(), _MX4_DTYPES[t.dtype], ld
 
 
-def _mx4_parts(t: Mx4, name: str, dims: int) -> Tuple[int, int, int, int, int]:
-    """(codes, scales, groups, rows, K) of a quantised tensor of `dims` dimensions; groups is 1 for a matrix."""
-    codes, scales, K = t
-    if codes.dim() != dims:
-        raise ValueError(f"{name} must have {dims} dimensions, its codes are {tuple(codes.shape)}")
-    groups, rows = (codes.shape[0] if dims == 3 else 1), codes.shape[-2]
-    if K < 1 or codes.shape[-1] != 16 * -(-K // 32):
-        raise ValueError(f"{name}: rows of {codes.shape[-1]} bytes do not hold {K} codes")
-    need = int(load().q8_mx4_scales_bytes(groups, rows, K))
-    if scales.numel() < need:
-        raise ValueError(f"{name} has {scales.numel()} bytes of scales, {need} are read")
-    return _ptr(codes, torch.uint8, name), _ptr(scales, torch.uint8, name), groups, rows, K
+def _mx4_parts(t: Mx4, name: str, dims: int = 0) -> Tuple[int, int, int, int]:
+    """(tiles, groups, rows, K) of a quantised tensor of `dims` dimensions (0: two or three); groups is 1 for a matrix."""
+    tiles, shape = t
+    if len(shape) not in (2, 3) or (dims and len(shape) != dims):
+        raise ValueError(f"{name} must have {dims or '2 or 3'} dimensions, got {tuple(shape)}")
+    groups, rows, K = shape if len(shape) == 3 else (1, *shape)
+    need = q8_mx4_bytes(groups, rows, K)
+    if tiles.numel() < need:
+        raise ValueError(f"{name} has {tiles.numel()} bytes of tiles, {need} are read")
+    return _ptr(tiles, torch.uint8, name), groups, rows, K
 
 
 def _mx4_same_device(*tensors) -> None:
@@ -705,12 +701,8 @@ def _mx4_output(Y, shape, dtype, like, stream, name: str = "Y"):
     return Y
 
 
-def q8_mx4_codes_bytes(rows: int, K: int) -> int:
-    return int(load().q8_mx4_codes_bytes(rows, K))
-
-
-def q8_mx4_scales_bytes(groups: int, rows: int, K: int) -> int:
-    return int(load().q8_mx4_scales_bytes(groups, rows, K))
+def q8_mx4_bytes(groups: int, rows: int, K: int) -> int:
+    return int(load().q8_mx4_bytes(groups, rows, K))
 
 
 def q8_mx4_quantize(X, dev_status=None, stream=None) -> Mx4:
@@ -718,31 +710,30 @@ def q8_mx4_quantize(X, dev_status=None, stream=None) -> Mx4:
     if stream is None:
         r = (_native_module or _native()).mx4_quantize(X, dev_status)
         if r is not NotImplemented:
-            return Mx4._make(r)
+            return Mx4(r, tuple(X.shape))
     if X.dim() not in (2, 3):
         raise ValueError(f"X must have 2 or 3 dimensions, got {tuple(X.shape)}")
     x, dtype, ld = _mx4_matrix(X, "X")
     _mx4_same_device(X, dev_status)
-    groups, (rows, K) = (X.shape[0] if X.dim() == 3 else 1), X.shape[-2:]
-    codes = _mx4_empty((*X.shape[:-1], 16 * -(-K // 32)), torch.uint8, X.device, stream)
-    scales = _mx4_empty(q8_mx4_scales_bytes(groups, rows, K), torch.uint8, X.device, stream)
-    st = load().q8_mx4_quantize(x, dtype, groups, rows, K, ld, _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales"),
-                                _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
+    groups, rows, K = X.shape if X.dim() == 3 else (1, *X.shape)
+    tiles = _mx4_empty(q8_mx4_bytes(groups, rows, K), torch.uint8, X.device, stream)
+    st = load().q8_mx4_quantize(x, dtype, groups, rows, K, ld, _ptr(tiles, torch.uint8, "tiles"), _ptr(dev_status, torch.int32, "dev_status"),
+                                _stream(stream))
     _check(st, "q8_mx4_quantize")
-    return Mx4(codes, scales, K)
+    return Mx4(tiles, tuple(X.shape))
 
 
 def q8_mx4_dequantize(T: Mx4, dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
-    """The values that the codes and scales of T stand for."""
+    """The values that T stands for."""
     if stream is None:
         r = (_native_module or _native()).mx4_dequantize(T, dtype)
         if r is not NotImplemented:
             return r
-    codes, scales, groups, rows, K = _mx4_parts(T, "T", T.codes.dim() if T.codes.dim() == 3 else 2)
-    _mx4_same_device(T.codes, T.scales)
-    Y = _mx4_empty((*T.codes.shape[:-1], K), dtype, T.codes.device, stream)
+    tiles, groups, rows, K = _mx4_parts(T, "T")
+    _mx4_same_device(T.tiles)
+    Y = _mx4_empty(T.shape, dtype, T.tiles.device, stream)
     y, y_dtype, ldy = _mx4_matrix(Y, "Y")
-    _check(load().q8_mx4_dequantize(codes, scales, groups, rows, K, y, y_dtype, ldy, _stream(stream)), "q8_mx4_dequantize")
+    _check(load().q8_mx4_dequantize(tiles, groups, rows, K, y, y_dtype, ldy, _stream(stream)), "q8_mx4_dequantize")
     return Y
 
 
@@ -785,7 +776,7 @@ def q8_mx4_linear(X, W: Mx4, bias=None, act: int = Q8_ACT_NONE, Y=None, dtype: O
         r = (_native_module or _native()).mx4_linear(X, W, bias, act, Y, dtype, workspace, dev_status)
         if r is not NotImplemented:
             return r
-    wq, ws, _, N, K = _mx4_parts(W, "W", 2)
+    wq, _, N, K = _mx4_parts(W, "W", 2)
     if X.dim() != 2 or X.shape[1] != K:
         raise ValueError(f"X is {tuple(X.shape)} but W has rows of {K}")
     x, x_dtype, ldx = _mx4_matrix(X, "X")
@@ -794,8 +785,8 @@ def q8_mx4_linear(X, W: Mx4, bias=None, act: int = Q8_ACT_NONE, Y=None, dtype: O
     y, y_dtype, ldy = _mx4_matrix(Y, "Y")
     if workspace is None:
         workspace = _mx4_empty(q8_mx4_linear_workspace_bytes(M, K), torch.uint8, X.device, stream)
-    _mx4_same_device(X, *W[:2], bias, Y, workspace, dev_status)
-    st = load().q8_mx4_linear(x, x_dtype, ldx, wq, ws, _mx4_bias(bias, N), int(act), y, y_dtype, ldy, M, N, K,
+    _mx4_same_device(X, W.tiles, bias, Y, workspace, dev_status)
+    st = load().q8_mx4_linear(x, x_dtype, ldx, wq, _mx4_bias(bias, N), int(act), y, y_dtype, ldy, M, N, K,
                               _any_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
                               _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
     _check(st, "q8_mx4_linear")
@@ -809,14 +800,14 @@ def q8_mx4_linear_q(Xq: Mx4, W: Mx4, bias=None, act: int = Q8_ACT_NONE, Y=None, 
         r = (_native_module or _native()).mx4_linear_q(Xq, W, bias, act, Y, dtype, dev_status)
         if r is not NotImplemented:
             return r
-    wq, ws, _, N, K = _mx4_parts(W, "W", 2)
-    xq, xs, _, M, K2 = _mx4_parts(Xq, "Xq", 2)
+    wq, _, N, K = _mx4_parts(W, "W", 2)
+    xq, _, M, K2 = _mx4_parts(Xq, "Xq", 2)
     if K2 != K:
         raise ValueError(f"Xq has rows of {K2}, W of {K}")
-    Y = _mx4_output(Y, (M, N), dtype if dtype is not None or Y is not None else torch.float32, Xq.codes, stream)
+    Y = _mx4_output(Y, (M, N), dtype if dtype is not None or Y is not None else torch.float32, Xq.tiles, stream)
     y, y_dtype, ldy = _mx4_matrix(Y, "Y")
-    _mx4_same_device(*Xq[:2], *W[:2], bias, Y, dev_status)
-    st = load().q8_mx4_linear_q(xq, xs, wq, ws, _mx4_bias(bias, N), int(act), y, y_dtype, ldy, M, N, K,
+    _mx4_same_device(Xq.tiles, W.tiles, bias, Y, dev_status)
+    st = load().q8_mx4_linear_q(xq, wq, _mx4_bias(bias, N), int(act), y, y_dtype, ldy, M, N, K,
                                 _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
     _check(st, "q8_mx4_linear_q")
     return Y
@@ -831,7 +822,7 @@ def q8_mx4_linear_grouped(X, offsets, W: Mx4, bias=None, act: int = Q8_ACT_NONE,
         r = (_native_module or _native()).mx4_linear_grouped(X, offsets, W, bias, act, rows, Y, dtype, workspace, dev_status)
         if r is not NotImplemented:
             return r
-    wq, ws, E, N, K = _mx4_parts(W, "W", 3)
+    wq, E, N, K = _mx4_parts(W, "W", 3)
     if X.dim() != 2 or X.shape[1] != K:
         raise ValueError(f"X is {tuple(X.shape)} but W has rows of {K}")
     if offsets.numel() != E + 1:
@@ -842,9 +833,9 @@ def q8_mx4_linear_grouped(X, offsets, W: Mx4, bias=None, act: int = Q8_ACT_NONE,
     y, y_dtype, ldy = _mx4_matrix(Y, "Y")
     if workspace is None:
         workspace = _mx4_empty(q8_mx4_linear_grouped_workspace_bytes(T, E, K), torch.uint8, X.device, stream)
-    _mx4_same_device(X, offsets, *W[:2], bias, rows, Y, workspace, dev_status)
+    _mx4_same_device(X, offsets, W.tiles, bias, rows, Y, workspace, dev_status)
     st = load().q8_mx4_linear_grouped(x, x_dtype, ldx, X.shape[0], _ptr(rows, torch.int32, "rows"), _ptr(offsets, torch.int32, "offsets"),
-                                      E, wq, ws, _mx4_bias(bias, E * N), int(act), y, y_dtype, ldy, T, N, K,
+                                      E, wq, _mx4_bias(bias, E * N), int(act), y, y_dtype, ldy, T, N, K,
                                       _any_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
                                       _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
     _check(st, "q8_mx4_linear_grouped")

@@ -15,7 +15,7 @@ using namespace mx4;
 
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-constexpr int kChunk = 256;  // columns of a warp
+constexpr int kChunk = kTileK;  // columns of a warp
 
 enum Kind { kMatrix, kFake, kSlots1, kSlots4 };
 template <int KIND>
@@ -106,22 +106,22 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     const int lane = threadIdx.x & 31;
     const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
     const int64_t chunks = ceil_div(a.K, kChunk);
-    ExpertTable table{table_words, table_words + kMaxExperts + 1};
+    ExpertTable table{table_words, table_words + kMaxExperts + 1, nullptr};
     bool bad_index = false;
     if (kSlots) {
-        if (threadIdx.x < 32) bad_index = build_expert_table(table, a.offsets, a.E, (int32_t)a.rows);
+        if (threadIdx.x < 32) bad_index = build_expert_table(table, a.offsets, a.E, (int32_t)a.rows, 1, 1);
         __syncthreads();
     }
     if (task >= tasks) return;
-    int64_t first, row_step, end, scale_row0 = 0;
-    int64_t chunk;
+    int64_t first, row_step, end;
+    int64_t chunk, block = 0;
     if (KIND == kMatrix) {  // row_lanes of the 32 rows r, with r + 32, ... each, of a block of 128
-        const int64_t blocks = ceil_div(a.rows, kAtomRows);
-        const int64_t block = task / row_lanes / chunks, group = block / blocks;
+        const int64_t blocks = ceil_div(a.rows, kTileRows);
+        block = task / row_lanes / chunks;
+        const int64_t group = block / blocks;
         chunk = task / row_lanes % chunks;
-        first = group * a.rows + (block - group * blocks) * kAtomRows + task % row_lanes;
+        first = group * a.rows + (block - group * blocks) * kTileRows + task % row_lanes;
         end = (group + 1) * a.rows;
-        scale_row0 = block * kAtomRows + task % row_lanes;
         row_step = 32;
     } else {
         chunk = task % chunks;
@@ -131,7 +131,6 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     }
     const int64_t k0 = chunk * kChunk + lane * 8;
     const int valid = (int)max((int64_t)0, min((int64_t)8, a.K - k0));
-    const int64_t pitch = code_pitch(a.K), atoms = scale_atoms(a.K);
     bool odd = false;
     float v[R][8];
 #pragma unroll
@@ -171,8 +170,10 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
         w |= __shfl_xor_sync(0xffffffffu, w, 4);
         w |= __shfl_xor_sync(0xffffffffu, w, 8);
         words[j] = w;
-        if (row < end && (k0 >> 1) < pitch) *reinterpret_cast<uint32_t *>(a.codes + row * pitch + (k0 >> 1)) = codes;
-        if (kSlots && row < end && (lane & 15) == 0) {
+        if (KIND == kMatrix) {
+            const int r = (int)(task % row_lanes) + 32 * j;
+            if (row < end) *reinterpret_cast<uint32_t *>(a.out + (block * chunks + chunk) * kTileBytes + code_place(r, lane)) = codes;
+        } else if (row < end) {
             // the expert that owns the slot: the last one that starts at or before it
             int lo = 0, hi = a.E;
             while (lo < hi) {
@@ -180,18 +181,18 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
                 if (table.start[mid + 1] <= row) lo = mid + 1;
                 else hi = mid;
             }
-            const int64_t atom = chunk * 2 + (lane >> 4);
-            if (lo < a.E && row >= table.start[lo] && atom < atoms) {
-                const int64_t in_expert = row - table.start[lo], block = table.block[lo] + in_expert / kAtomRows;
-                const int r = (int)(in_expert % kAtomRows);
-                *reinterpret_cast<uint32_t *>(a.scales + (block * atoms + atom) * kAtomBytes + (r & 31) * 16 + (r >> 5) * 4) = w;
+            if (lo < a.E && row >= table.start[lo]) {
+                const int64_t in_expert = row - table.start[lo];
+                const int r = (int)(in_expert % kTileRows);
+                uint8_t *tile = a.out + ((table.block[lo] + in_expert / kTileRows) * chunks + chunk) * kTileBytes;
+                *reinterpret_cast<uint32_t *>(tile + code_place(r, lane)) = codes;
+                if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(tile + scale_place(r, lane >> 2)) = w;
             }
         }
     }
     if constexpr (KIND == kMatrix) {
-        const int64_t atom = chunk * 2 + (lane >> 4);
-        if ((lane & 15) == 0 && atom < atoms)
-            *reinterpret_cast<uint4 *>(a.scales + (scale_row0 / kAtomRows * atoms + atom) * kAtomBytes + (scale_row0 & 31) * 16) =
+        if ((lane & 15) == 0)
+            *reinterpret_cast<uint4 *>(a.out + (block * chunks + chunk) * kTileBytes + scale_place((int)(task % row_lanes), lane >> 2)) =
                 make_uint4(words[0], words[1], words[2], words[3]);
     }
     if (a.status != nullptr) {
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-mx4_dequantize_kernel(const uint8_t *codes, const uint8_t *scales, int64_t groups, int64_t rows, int64_t K, T *Y, int64_t ldy, int64_t tasks, int vec)
+mx4_dequantize_kernel(const uint8_t *tiles, int64_t groups, int64_t rows, int64_t K, T *Y, int64_t ldy, int64_t tasks, int vec)
 {
     grid_dependency_wait();
     const int lane = threadIdx.x & 31;
@@ -212,7 +213,7 @@ mx4_dequantize_kernel(const uint8_t *codes, const uint8_t *scales, int64_t group
     const int64_t k0 = chunk * kChunk + lane * 8;
     if (k0 >= K) return;
     const int valid = (int)min((int64_t)8, K - k0);
-    const int64_t pitch = code_pitch(K), atoms = scale_atoms(K), blocks = ceil_div(rows, kAtomRows);
+    const int64_t blocks = ceil_div(rows, kTileRows);
     uint32_t c[4], E[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -220,9 +221,9 @@ mx4_dequantize_kernel(const uint8_t *codes, const uint8_t *scales, int64_t group
         c[j] = E[j] = 0;
         if (row >= groups * rows) continue;
         const int64_t group = row / rows, r = row - group * rows;
-        c[j] = __ldcs(reinterpret_cast<const uint32_t *>(codes + row * pitch + (k0 >> 1)));
-        E[j] = __ldg(scales + ((group * blocks + r / kAtomRows) * atoms + k0 / kAtomK) * kAtomBytes + (r & 31) * 16 +
-                     ((r % kAtomRows) >> 5) * 4 + (k0 % kAtomK) / kBlock);
+        const uint8_t *tile = tiles + ((group * blocks + r / kTileRows) * chunks + chunk) * kTileBytes;
+        c[j] = __ldg(reinterpret_cast<const uint32_t *>(tile + code_place((int)(r % kTileRows), lane)));
+        E[j] = __ldg(tile + scale_place((int)(r % kTileRows), lane >> 2));
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -251,7 +252,7 @@ cudaError_t launch_kind(const Mx4QuantizeArgs &a, cudaStream_t s)
 {
     const int64_t chunks = ceil_div(a.K, kChunk);
     const int row_lanes = (int)(a.rows < 32 ? a.rows : 32);
-    const int64_t tasks = KIND == kMatrix ? a.groups * ceil_div(a.rows, kAtomRows) * chunks * row_lanes : ceil_div(a.rows, kRows<KIND>) * chunks;
+    const int64_t tasks = KIND == kMatrix ? a.groups * ceil_div(a.rows, kTileRows) * chunks * row_lanes : ceil_div(a.rows, kRows<KIND>) * chunks;
     dim3 grid;
     cudaError_t e = grid_of(tasks, &grid);
     if (e != cudaSuccess) return e;
@@ -280,8 +281,7 @@ cudaError_t launch_mx4_quantize(const Mx4QuantizeArgs &a, int dtype, cudaStream_
     }
 }
 
-cudaError_t launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t groups, int64_t rows, int64_t K, void *Y,
-                                  int dtype, int64_t ldy, cudaStream_t s)
+cudaError_t launch_mx4_dequantize(const uint8_t *tiles, int64_t groups, int64_t rows, int64_t K, void *Y, int dtype, int64_t ldy, cudaStream_t s)
 {
     last_launch_info().launches += 1;
     const int64_t tasks = ceil_div(groups * rows, 4) * ceil_div(K, kChunk);
@@ -290,9 +290,9 @@ cudaError_t launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, i
     if (e != cudaSuccess) return e;
     const int vec = rows_aligned(Y, ldy, dtype == Q8_F32 ? 4 : 2);
     switch (dtype) {
-        case Q8_F32: return launch_overlapping_tail(mx4_dequantize_kernel<float>, grid, dim3(kThreads), 0, s, codes, scales, groups, rows, K, static_cast<float *>(Y), ldy, tasks, vec);
-        case Q8_F16: return launch_overlapping_tail(mx4_dequantize_kernel<__half>, grid, dim3(kThreads), 0, s, codes, scales, groups, rows, K, static_cast<__half *>(Y), ldy, tasks, vec);
-        default: return launch_overlapping_tail(mx4_dequantize_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, s, codes, scales, groups, rows, K, static_cast<__nv_bfloat16 *>(Y), ldy, tasks, vec);
+        case Q8_F32: return launch_overlapping_tail(mx4_dequantize_kernel<float>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<float *>(Y), ldy, tasks, vec);
+        case Q8_F16: return launch_overlapping_tail(mx4_dequantize_kernel<__half>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<__half *>(Y), ldy, tasks, vec);
+        default: return launch_overlapping_tail(mx4_dequantize_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<__nv_bfloat16 *>(Y), ldy, tasks, vec);
     }
 }
 

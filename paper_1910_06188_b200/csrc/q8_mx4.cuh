@@ -5,12 +5,13 @@
 // and their negatives; ties to the even mantissa, 6 from there on).  x / s is a product with a power of two and exact wherever
 // the rounding depends on it, so the codes are the same whichever way they are computed.
 //
-// Layout of [rows, K]:
-//   codes   row-major, two to a byte (the lower index in the lower half), rows of 16 ceil(K / 32) bytes: whole blocks, 16-byte
-//           pitch; codes behind column K are 0
-//   scales  the order in which the tensor cores take them: atoms of 128 rows x 128 columns (4 blocks), 512 bytes each, atoms of
-//           a row of atoms one after the other; in an atom row r, block b is byte 16 (r % 32) + 4 (r / 32) + b.  Bytes of blocks
-//           behind the last one are 0; those of rows behind the last one are of no account.
+// Layout of [rows, K]: tiles of 128 rows x 256 columns, the tiles of a row of tiles one after the other, each as the tensor
+// cores take it from shared memory, so that a tile is one contiguous copy:
+//   16384 bytes of codes   row r at 128 r, in eight pieces of 16 bytes (32 codes, one block); piece p stands at place p ^ (r % 8); two
+//                          codes to a byte, the lower column in the lower half; codes behind column K are 0
+//   1024 bytes of scales   two atoms of 128 rows x 4 blocks: row r, block b of the atom is byte 16 (r % 32) + 4 (r / 32) + b;
+//                          scales of blocks behind the last one are 0
+// What rows behind the last one hold is of no account.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -21,75 +22,86 @@
 namespace q8 {
 namespace mx4 {
 
-constexpr int kBlock = 32;         // values that share a scale
-constexpr int kAtomRows = 128;     // rows, and
-constexpr int kAtomK = 128;        // columns of an atom of scales
-constexpr int kAtomBytes = 512;
+constexpr int kBlock = 32;       // values that share a scale
+constexpr int kTileRows = 128;   // rows, and
+constexpr int kTileK = 256;      // columns of a tile
+constexpr int kAtomBytes = 512;  // scales of 128 rows x 128 columns
+constexpr int kCodeBytes = kTileRows * kTileK / 2;
+constexpr int kTileBytes = kCodeBytes + 2 * kAtomBytes;
 constexpr int kMaxExperts = 1024;
 
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-__host__ __device__ inline int64_t code_pitch(int64_t K) { return 16 * ceil_div(K, kBlock); }
-__host__ __device__ inline int64_t scale_atoms(int64_t K) { return ceil_div(K, kAtomK); }
-// Row blocks of scales that T slots of E experts can need: every expert starts a block of its own.
-inline int64_t most_row_blocks(int64_t T, int64_t E) { return T / kAtomRows + (E < T ? E : T); }
+__host__ __device__ inline int64_t tiles_along(int64_t K) { return ceil_div(K, kTileK); }
+// Places in a tile: the 4 bytes with the codes of columns 8 i .. 8 i + 7, the scale of block b (0 .. 7), row r
+__host__ __device__ inline int code_place(int r, int i) { return r * 128 + ((((i >> 2) ^ r) & 7) << 4) + ((i & 3) << 2); }
+__host__ __device__ inline int scale_place(int r, int b) { return kCodeBytes + (b >> 2) * kAtomBytes + (r & 31) * 16 + (r >> 5) * 4 + (b & 3); }
+// Row blocks that T slots of E experts can need: every expert starts a block of its own.
+inline int64_t most_row_blocks(int64_t T, int64_t E) { return T / kTileRows + (E < T ? E : T); }
 
 // ---- experts
-// The slots [start[e], start[e + 1]) of each expert and the first of its row blocks of scales, in shared memory.
+// The slots [start[e], start[e + 1]) of each expert, the first of its row blocks and of its tiles, in shared memory.
 struct ExpertTable {
     int32_t *start;  // E + 1
     int32_t *block;  // E + 1
+    int32_t *tile;   // E + 1, or nullptr
 };
-// Written by one warp.  Offsets outside [0, T] or below an earlier one (a caller's mistake) are moved to the nearest allowed value, so that
-// every slot belongs to one expert at most and no access leaves the tensors; returns whether there were any.  A lane takes
-// neighbouring experts, so the 32 runs need one scan.  offsets == nullptr: one expert with all T slots.
-__device__ __forceinline__ bool build_expert_table(const ExpertTable &t, const int32_t *offsets, int E, int32_t T)
+__device__ __forceinline__ int32_t scan_max(int32_t v, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t o = __shfl_up_sync(0xffffffffu, v, d);
+        if (lane >= d) v = max(v, o);
+    }
+    return v;
+}
+__device__ __forceinline__ int32_t scan_sum(int32_t v, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t o = __shfl_up_sync(0xffffffffu, v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+// Written by one warp, 32 experts at a time.  Offsets outside [0, T] or below an earlier one (a caller's mistake) are moved to the
+// nearest allowed value, so that every slot belongs to one expert at most and no access leaves the tensors; returns whether there
+// were any.  An expert has ceil(slots / tile_n) tiles_m tiles.  offsets == nullptr: one expert with all T slots.
+__device__ __forceinline__ bool build_expert_table(const ExpertTable &t, const int32_t *offsets, int E, int32_t T, int32_t tile_n, int32_t tiles_m)
 {
     const int lane = threadIdx.x & 31;
     if (offsets == nullptr) {
-        if (lane == 0) {
-            t.start[0] = 0;
-            t.start[1] = T;
-            t.block[0] = 0;
-            t.block[1] = (T + kAtomRows - 1) / kAtomRows;
+        if (lane < 2) {
+            t.start[lane] = lane * T;
+            t.block[lane] = lane * ((T + kTileRows - 1) / kTileRows);
+            if (t.tile != nullptr) t.tile[lane] = lane * ((T + tile_n - 1) / tile_n * tiles_m);
         }
         __syncwarp();
         return false;
     }
-    const int run = (E + 32) / 32;  // ceil((E + 1) / 32)
-    const int lo = min(lane * run, E + 1), hi = min(lo + run, E + 1);
-    int32_t top = 0;
     bool bad = false;
-    for (int i = lo; i < hi; ++i) {
-        const int32_t v = __ldg(offsets + i);
-        bad |= v < 0 || v > T || v < top;
-        top = max(top, min(max(v, 0), T));
-        t.start[i] = top;
-    }
-    int32_t before = top;  // maximum over this and all lower lanes
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int32_t o = __shfl_up_sync(0xffffffffu, before, d);
-        if (lane >= d) before = max(before, o);
-    }
-    before = __shfl_up_sync(0xffffffffu, before, 1);
-    if (lane == 0) before = 0;
-    for (int i = lo; i < hi; ++i) {
-        bad |= t.start[i] < before;
-        t.start[i] = max(t.start[i], before);
-    }
-    __syncwarp();
-    int32_t sum = 0;
-    for (int i = lo; i < min(hi, E); ++i) sum += (t.start[i + 1] - t.start[i] + kAtomRows - 1) / kAtomRows;
-    int32_t at = sum;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int32_t o = __shfl_up_sync(0xffffffffu, at, d);
-        if (lane >= d) at += o;
-    }
-    at -= sum;
-    for (int i = lo; i < hi; ++i) {
-        t.block[i] = at;
-        if (i < E) at += (t.start[i + 1] - t.start[i] + kAtomRows - 1) / kAtomRows;
+    int32_t top = 0, blocks = 0, tiles = 0;
+    int32_t next = lane <= E ? __ldg(offsets + lane) : 0;
+    for (int e0 = 0; e0 <= E; e0 += 32) {
+        const int e = e0 + lane;
+        const int32_t raw = next;
+        next = e + 32 <= E ? __ldg(offsets + e + 32) : 0;  // on its way while this batch is scanned
+        const int32_t first_next = __shfl_sync(0xffffffffu, next, 0);
+        const int32_t v = e <= E ? min(max(raw, 0), T) : 0;
+        const int32_t begin = max(scan_max(v, lane), top);
+        bad |= e <= E && (raw != v || v < begin);
+        int32_t end = __shfl_down_sync(0xffffffffu, begin, 1);
+        if (lane == 31) end = max(begin, min(max(first_next, 0), T));
+        const int32_t count = e < E ? end - begin : 0;
+        const int32_t nb = (count + kTileRows - 1) / kTileRows, nt = t.tile != nullptr ? (count + tile_n - 1) / tile_n * tiles_m : 0;
+        const int32_t sb = scan_sum(nb, lane), st = scan_sum(nt, lane);
+        if (e <= E) {
+            t.start[e] = begin;
+            t.block[e] = blocks + sb - nb;
+            if (t.tile != nullptr) t.tile[e] = tiles + st - nt;
+        }
+        top = __shfl_sync(0xffffffffu, begin, 31);
+        blocks += __shfl_sync(0xffffffffu, sb, 31);
+        tiles += __shfl_sync(0xffffffffu, st, 31);
     }
     bad = __any_sync(0xffffffffu, bad);
     __syncwarp();
@@ -144,11 +156,11 @@ __device__ __forceinline__ float inverse_scale(uint32_t E) { return __uint_as_fl
 
 // ---- launchers (q8_mx4.cu, q8_mx4_gemm_sm100.cu); arguments are checked by the entry points
 struct Mx4QuantizeArgs {
-    const void *X;        // [groups, rows, K], rows ld values apart, groups rows * ld
+    const void *X;  // [groups, rows, K], rows ld values apart, groups rows * ld
     int64_t ld;
     int64_t groups, rows, K;
-    uint8_t *codes, *scales;
-    void *Xhat = nullptr;  // instead of codes and scales: the values, in X's type, rows ldo values apart
+    uint8_t *out;          // tiles
+    void *Xhat = nullptr;  // instead: the values, in X's type, rows ldo values apart
     int64_t ldo = 0;
     int32_t *status;
     // slots of experts: rows is the number of slots, groups 1
@@ -158,14 +170,13 @@ struct Mx4QuantizeArgs {
     int64_t x_rows = 0;              // rows that X has
 };
 cudaError_t launch_mx4_quantize(const Mx4QuantizeArgs &a, int dtype, cudaStream_t s);
-cudaError_t launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t groups, int64_t rows, int64_t K, void *Y,
-                                  int dtype, int64_t ldy, cudaStream_t s);
+cudaError_t launch_mx4_dequantize(const uint8_t *tiles, int64_t groups, int64_t rows, int64_t K, void *Y, int dtype, int64_t ldy, cudaStream_t s);
 
 struct Mx4GemmArgs {
-    const uint8_t *Xq, *Xs;  // activation codes [M, K] and scales
-    const uint8_t *Wq, *Ws;  // weights [E, N, K], scales of each expert in row blocks of its own
-    const float *bias;       // [E, N] or nullptr
-    void *Y;                 // [M, N], rows ldy values apart
+    const uint8_t *X;   // activation tiles, each expert's slots in row blocks of their own
+    const uint8_t *W;   // weight tiles, each expert's in row blocks of their own
+    const float *bias;  // [E, N] or nullptr
+    void *Y;            // [M, N], rows ldy values apart
     int64_t ldy;
     int y_dtype;
     int64_t M, N, K;

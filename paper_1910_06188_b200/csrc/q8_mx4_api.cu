@@ -12,7 +12,6 @@ constexpr int64_t kMaxK = int64_t(1) << 24;
 constexpr int64_t kMaxPitch = int64_t(1) << 40;  // in values; row * pitch fits 64 bits with room
 
 bool aligned_to(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
-size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 bool known_dtype(int d) { return d == Q8_F32 || d == Q8_F16 || d == Q8_BF16; }
 size_t dtype_bytes(int d) { return d == Q8_F32 ? 4 : 2; }
 q8_status cuda_status(cudaError_t e) { return e == cudaSuccess ? Q8_OK : Q8_ERR_CUDA; }
@@ -39,41 +38,34 @@ q8_status check_layer(int64_t M, int64_t N, int64_t K, int64_t E, int64_t ldy)
 
 extern "C" {
 
-size_t q8_mx4_codes_bytes(int64_t rows, int64_t K)
-{
-    if (rows < 0 || K <= 0 || rows > kMaxRows || K > kMaxK) return 0;
-    return (size_t)rows * (size_t)code_pitch(K);
-}
-
-size_t q8_mx4_scales_bytes(int64_t groups, int64_t rows, int64_t K)
+size_t q8_mx4_bytes(int64_t groups, int64_t rows, int64_t K)
 {
     if (check_matrix(groups, rows, K, K) != Q8_OK) return 0;
-    return (size_t)groups * (size_t)ceil_div(rows, kAtomRows) * (size_t)scale_atoms(K) * kAtomBytes;
+    return (size_t)groups * (size_t)ceil_div(rows, kTileRows) * (size_t)tiles_along(K) * kTileBytes;
 }
 
-q8_status q8_mx4_quantize(const void *X, int dtype, int64_t groups, int64_t rows, int64_t K, int64_t ldx, uint8_t *codes, uint8_t *scales,
-                          int32_t *dev_status, void *stream)
+q8_status q8_mx4_quantize(const void *X, int dtype, int64_t groups, int64_t rows, int64_t K, int64_t ldx, uint8_t *T, int32_t *dev_status,
+                          void *stream)
 {
     last_launch_info() = LaunchInfo();
     if (!known_dtype(dtype)) return Q8_ERR_ARG;
     const q8_status st = check_matrix(groups, rows, K, ldx);
     if (st != Q8_OK) return st;
     if (groups == 0 || rows == 0) return Q8_OK;
-    if (!X || !codes || !scales) return Q8_ERR_NULL;
-    if (!aligned_to(X, dtype_bytes(dtype)) || !aligned_to(codes, 16) || !aligned_to(scales, 16) || !aligned_to(dev_status, 4)) return Q8_ERR_ALIGN;
+    if (!X || !T) return Q8_ERR_NULL;
+    if (!aligned_to(X, dtype_bytes(dtype)) || !aligned_to(T, 16) || !aligned_to(dev_status, 4)) return Q8_ERR_ALIGN;
     Mx4QuantizeArgs a = {};
     a.X = X;
     a.ld = ldx;
     a.groups = groups;
     a.rows = rows;
     a.K = K;
-    a.codes = codes;
-    a.scales = scales;
+    a.out = T;
     a.status = dev_status;
     return cuda_status(launch_mx4_quantize(a, dtype, static_cast<cudaStream_t>(stream)));
 }
 
-q8_status q8_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t groups, int64_t rows, int64_t K, void *Y, int dtype, int64_t ldy,
+q8_status q8_mx4_dequantize(const uint8_t *T, int64_t groups, int64_t rows, int64_t K, void *Y, int dtype, int64_t ldy,
                             void *stream)
 {
     last_launch_info() = LaunchInfo();
@@ -81,9 +73,9 @@ q8_status q8_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t
     const q8_status st = check_matrix(groups, rows, K, ldy);
     if (st != Q8_OK) return st;
     if (groups == 0 || rows == 0) return Q8_OK;
-    if (!Y || !codes || !scales) return Q8_ERR_NULL;
-    if (!aligned_to(Y, dtype_bytes(dtype)) || !aligned_to(codes, 16) || !aligned_to(scales, 16)) return Q8_ERR_ALIGN;
-    return cuda_status(launch_mx4_dequantize(codes, scales, groups, rows, K, Y, dtype, ldy, static_cast<cudaStream_t>(stream)));
+    if (!Y || !T) return Q8_ERR_NULL;
+    if (!aligned_to(Y, dtype_bytes(dtype)) || !aligned_to(T, 16)) return Q8_ERR_ALIGN;
+    return cuda_status(launch_mx4_dequantize(T, groups, rows, K, Y, dtype, ldy, static_cast<cudaStream_t>(stream)));
 }
 
 q8_status q8_mx4_fake_quantize(const void *X, int dtype, int64_t rows, int64_t K, int64_t ldx, void *Xhat, int64_t ldo, int32_t *dev_status, void *stream)
@@ -109,18 +101,15 @@ q8_status q8_mx4_fake_quantize(const void *X, int dtype, int64_t rows, int64_t K
     return cuda_status(launch_mx4_quantize(a, dtype, static_cast<cudaStream_t>(stream)));
 }
 
-// The workspace of a layer: the activation's codes, then its scales.
-static size_t workspace_codes_bytes(int64_t M, int64_t K) { return round_up(q8_mx4_codes_bytes(M, K), 256); }
-
-size_t q8_mx4_linear_workspace_bytes(int64_t M, int64_t K) { return workspace_codes_bytes(M, K) + q8_mx4_scales_bytes(1, M, K); }
+size_t q8_mx4_linear_workspace_bytes(int64_t M, int64_t K) { return q8_mx4_bytes(1, M, K); }
 
 size_t q8_mx4_linear_grouped_workspace_bytes(int64_t T, int64_t experts, int64_t K)
 {
     if (T < 0 || T > kMaxRows || experts < 0 || experts > kMaxExperts || K <= 0 || K > kMaxK) return 0;
-    return workspace_codes_bytes(T, K) + (size_t)most_row_blocks(T, experts) * (size_t)scale_atoms(K) * kAtomBytes;
+    return (size_t)most_row_blocks(T, experts) * (size_t)tiles_along(K) * kTileBytes;
 }
 
-q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Xs, const uint8_t *Wq, const uint8_t *Ws, const float *bias, int act, void *Y, int y_dtype,
+q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Wq, const float *bias, int act, void *Y, int y_dtype,
                           int64_t ldy, int64_t M, int64_t N, int64_t K, int32_t *dev_status, void *stream)
 {
     last_launch_info() = LaunchInfo();
@@ -128,15 +117,13 @@ q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Xs, const uint8_t *W
     const q8_status st = check_layer(M, N, K, 1, ldy);
     if (st != Q8_OK) return st;
     if (M == 0 || N == 0) return Q8_OK;
-    if (!Xq || !Xs || !Wq || !Ws || !Y) return Q8_ERR_NULL;
-    if (!aligned_to(Xq, 16) || !aligned_to(Xs, 16) || !aligned_to(Wq, 16) || !aligned_to(Ws, 16) || !aligned_to(bias, 4) ||
+    if (!Xq || !Wq || !Y) return Q8_ERR_NULL;
+    if (!aligned_to(Xq, 16) || !aligned_to(Wq, 16) || !aligned_to(bias, 4) ||
         !aligned_to(Y, dtype_bytes(y_dtype)) || !aligned_to(dev_status, 4))
         return Q8_ERR_ALIGN;
     Mx4GemmArgs g = {};
-    g.Xq = Xq;
-    g.Xs = Xs;
-    g.Wq = Wq;
-    g.Ws = Ws;
+    g.X = Xq;
+    g.W = Wq;
     g.bias = bias;
     g.Y = Y;
     g.ldy = ldy;
@@ -150,7 +137,7 @@ q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Xs, const uint8_t *W
     return cuda_status(launch_mx4_gemm(g, static_cast<cudaStream_t>(stream)));
 }
 
-q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *Wq, const uint8_t *Ws, const float *bias, int act, void *Y, int y_dtype,
+q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *Wq, const float *bias, int act, void *Y, int y_dtype,
                         int64_t ldy, int64_t M, int64_t N, int64_t K, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream)
 {
     last_launch_info() = LaunchInfo();
@@ -159,8 +146,8 @@ q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *
     if (st == Q8_OK) st = check_matrix(1, M, K, ldx);
     if (st != Q8_OK) return st;
     if (M == 0 || N == 0) return Q8_OK;
-    if (!X || !Wq || !Ws || !Y || !workspace) return Q8_ERR_NULL;
-    if (!aligned_to(X, dtype_bytes(x_dtype)) || !aligned_to(Wq, 16) || !aligned_to(Ws, 16) || !aligned_to(bias, 4) ||
+    if (!X || !Wq || !Y || !workspace) return Q8_ERR_NULL;
+    if (!aligned_to(X, dtype_bytes(x_dtype)) || !aligned_to(Wq, 16) || !aligned_to(bias, 4) ||
         !aligned_to(Y, dtype_bytes(y_dtype)) || !aligned_to(dev_status, 4) || !aligned_to(workspace, 256))
         return Q8_ERR_ALIGN;
     if (workspace_bytes < q8_mx4_linear_workspace_bytes(M, K)) return Q8_ERR_WORKSPACE;
@@ -170,17 +157,14 @@ q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *
     a.groups = 1;
     a.rows = M;
     a.K = K;
-    a.codes = static_cast<uint8_t *>(workspace);
-    a.scales = a.codes + workspace_codes_bytes(M, K);
+    a.out = static_cast<uint8_t *>(workspace);
     a.status = dev_status;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t e = launch_mx4_quantize(a, x_dtype, s);
     if (e != cudaSuccess) return Q8_ERR_CUDA;
     Mx4GemmArgs g = {};
-    g.Xq = a.codes;
-    g.Xs = a.scales;
-    g.Wq = Wq;
-    g.Ws = Ws;
+    g.X = a.out;
+    g.W = Wq;
     g.bias = bias;
     g.Y = Y;
     g.ldy = ldy;
@@ -196,7 +180,7 @@ q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *
 }
 
 q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t x_rows, const int32_t *rows, const int32_t *offsets, int64_t experts,
-                                const uint8_t *Wq, const uint8_t *Ws, const float *bias, int act, void *Y, int y_dtype, int64_t ldy, int64_t T, int64_t N,
+                                const uint8_t *Wq, const float *bias, int act, void *Y, int y_dtype, int64_t ldy, int64_t T, int64_t N,
                                 int64_t K, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream)
 {
     last_launch_info() = LaunchInfo();
@@ -206,8 +190,8 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
     if (st != Q8_OK) return st;
     if (!rows && x_rows < T) return Q8_ERR_SHAPE;
     if (T == 0 || N == 0 || experts == 0) return Q8_OK;
-    if ((!X && x_rows > 0) || !offsets || !Wq || !Ws || !Y || !workspace) return Q8_ERR_NULL;
-    if (!aligned_to(X, dtype_bytes(x_dtype)) || !aligned_to(rows, 4) || !aligned_to(offsets, 4) || !aligned_to(Wq, 16) || !aligned_to(Ws, 16) ||
+    if ((!X && x_rows > 0) || !offsets || !Wq || !Y || !workspace) return Q8_ERR_NULL;
+    if (!aligned_to(X, dtype_bytes(x_dtype)) || !aligned_to(rows, 4) || !aligned_to(offsets, 4) || !aligned_to(Wq, 16) ||
         !aligned_to(bias, 4) || !aligned_to(Y, dtype_bytes(y_dtype)) || !aligned_to(dev_status, 4) || !aligned_to(workspace, 256))
         return Q8_ERR_ALIGN;
     if (workspace_bytes < q8_mx4_linear_grouped_workspace_bytes(T, experts, K)) return Q8_ERR_WORKSPACE;
@@ -217,8 +201,7 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
     a.groups = 1;
     a.rows = T;
     a.K = K;
-    a.codes = static_cast<uint8_t *>(workspace);
-    a.scales = a.codes + workspace_codes_bytes(T, K);
+    a.out = static_cast<uint8_t *>(workspace);
     a.status = dev_status;
     a.offsets = offsets;
     a.E = (int)experts;
@@ -228,10 +211,8 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
     const cudaError_t e = launch_mx4_quantize(a, x_dtype, s);
     if (e != cudaSuccess) return Q8_ERR_CUDA;
     Mx4GemmArgs g = {};
-    g.Xq = a.codes;
-    g.Xs = a.scales;
-    g.Wq = Wq;
-    g.Ws = Ws;
+    g.X = a.out;
+    g.W = Wq;
     g.bias = bias;
     g.Y = Y;
     g.ldy = ldy;

@@ -4,17 +4,18 @@
 //
 // The weights are the A operand (accumulator rows = TMEM lanes = output features), the tokens the B operand (accumulator columns).
 // So a tile is as narrow as its tokens are few, an expert with three rows costs 16 columns, a lane of the epilogue has one bias
-// value for the whole tile, and a warp's store of one column is 32 neighbouring features of a token: whole sectors of Y without any
-// staging.
+// value for the whole tile, and what a warp stores of one column is 32 neighbouring features of a token.
 //
-//   warp 0      TMA producer of the weights: 128-byte-swizzled boxes of 128 rows x 256 codes, and their scales
-//   warp 2      the same for the tokens
+//   warp 0      producer of the weights: a tile of 128 rows x 256 codes with its scales is one contiguous copy
+//   warp 2      producer of the tokens: rows of such tiles, and their scales
 //   warp 1      MMA issuer: copies the scales to TMEM (tcgen05.cp), issues tcgen05.mma kind::mxf4 (64 codes a time, one scale per
 //               32), fp32 accumulators in TMEM, double buffered
 //   warps 3..   epilogue: tcgen05.ld, bias, GELU, conversion, store
 //
-// A plain product is the grouped one with a single expert.  Every wait on an mbarrier is bounded: after ~2 s the CTA raises
-// Q8_ERR_TIMEOUT in the status word, all roles leave their loops, copies and products in flight are waited for (bounded), TMEM is freed.
+// CTAS = 2 (cta_group::2): a pair of SMs shares a tile of 256 features; each loads its own 128 rows of weights, half of the tokens and the
+// scales of all of them.  A plain product is the grouped one with a single expert.  Every wait on an mbarrier is bounded: after
+// ~2 s the CTA raises Q8_ERR_TIMEOUT in the status word, all roles leave their loops, copies and products in flight are waited for
+// (bounded), TMEM is freed.  No copy is multicast.
 
 #include <cuda.h>
 
@@ -30,58 +31,74 @@ using namespace mx4;
 using gemm_detail::encode_tiled_fn;
 using gemm_detail::gelu_fast_x2;
 
-constexpr int kTileM = 128;           // weight rows of a tile
-constexpr int kStageK = 256;          // codes of a stage row: one 128-byte swizzle span
-constexpr int kStageRowBytes = 128;
 constexpr int kMmaK = 64;
 constexpr int kAccStages = 2;
-constexpr int kBoxRows = 32;          // tokens of the small box, for tiles that are not full
-constexpr int kScaleCols = 4 * 2 + 8 * 2;  // TMEM columns of a stage's scales: 128 weight rows, 256 token rows, two atoms each
+constexpr int kScaleBytes = 2 * kAtomBytes;  // of a tile
+constexpr int kScaleCols = 4 * 2 + 8 * 2;    // TMEM columns of a stage's scales: 128 weight rows, 256 token rows, two atoms each
+constexpr int kStoreRows = 32;               // tokens of a staged block of 32 features
 
-template <int BN, int EW>
+template <int CTAS, int BN, int EW, bool STAGED, int SIZE>
 struct Cfg {
     static constexpr int kThreads = 96 + 32 * EW;
-    static constexpr int kABytes = kTileM * kStageRowBytes;
-    static constexpr int kBBytes = BN * kStageRowBytes;
-    static constexpr int kSaBytes = 2 * kAtomBytes;
-    static constexpr int kSbBytes = 4 * kAtomBytes;  // two row blocks: a tile of 192 may start in the middle of one
-    static constexpr int kStageBytes = kABytes + kBBytes + kSaBytes + kSbBytes;
-    static constexpr int kTableBytes = 2 * (kMaxExperts + 1) * 4 + 8;
-    static constexpr int kBudget = 227 * 1024 - 1024 - kTableBytes - 512;
+    static constexpr int kBBytes = BN / CTAS * 128;
+    static constexpr int kSbBytes = 2 * kScaleBytes;  // two row blocks: a tile of 192 may start in the middle of one
+    static constexpr int kStageBytes = kTileBytes + kBBytes + kSbBytes;
+    static constexpr int kStagingBytes = STAGED ? EW * kStoreRows * 32 * SIZE : 0;
+    static constexpr int kTableBytes = 3 * (kMaxExperts + 1) * 4 + 4;
+    static constexpr int kBudget = 227 * 1024 - 1024 - kTableBytes - kStagingBytes - 512;
     static constexpr int kStages = kBudget / kStageBytes > 8 ? 8 : kBudget / kStageBytes;
     static constexpr int kScaleCol0 = kAccStages * BN;
     static constexpr int kTmemCols = kScaleCol0 + 2 * kScaleCols <= 128 ? 128 : kScaleCol0 + 2 * kScaleCols <= 256 ? 256 : 512;
     static constexpr int kBarrierBytes = (2 * kStages + 2 * kAccStages + 1) * 8 + 16;
-    static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kTableBytes + kBarrierBytes;
+    static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStagingBytes + kTableBytes + kBarrierBytes;
     static_assert(kScaleCol0 + 2 * kScaleCols <= 512, "TMEM columns");
     static_assert(kSmemBytes <= 232448 && kStages >= 3, "shared memory budget");
-    static_assert(BN % kBoxRows == 0 && BN <= 192, "tile width");
+    static_assert(BN % (32 * CTAS) == 0 && BN <= 192 && kBBytes % 1024 == 0, "tile width");
+    // Instruction descriptor of kind::mxf4: E2M1 operands, both K-major, UE8M0 scales, M = 128 or 256 for the pair; N / 8 in bits
+    // 17..22, which half of a scale word serves in bits 4..5 (B) and 29..30 (A).
+    static constexpr uint32_t kInstrDesc = (1u << 7) | (1u << 10) | (1u << 23) | ((uint32_t)CTAS << 27);
 };
 
-// Instruction descriptor of kind::mxf4: E2M1 operands, both K-major, UE8M0 scales, M = 128; N / 8 in bits 17..22, which half of a
-// scale word serves in bits 4..5 (B) and 29..30 (A).
-constexpr uint32_t kInstrDesc = (1u << 7) | (1u << 10) | (1u << 23) | ((uint32_t)(kTileM >> 7) << 27);
-
+template <int CTAS>
 __device__ __forceinline__ void mma_mxf4_elected(uint32_t elected, uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc,
                                                  uint32_t tmem_sa, uint32_t tmem_sb, uint32_t accumulate)
 {
-    asm volatile(
-        "{\n\t.reg .pred p, e;\n\t"
-        "setp.ne.b32 p, %6, 0;\n\t"
-        "setp.ne.b32 e, %7, 0;\n\t"
-        "@e tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate), "r"(elected)
-        : "memory");
+    if constexpr (CTAS == 2)
+        asm volatile(
+            "{\n\t.reg .pred p, e;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "setp.ne.b32 e, %7, 0;\n\t"
+            "@e tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate), "r"(elected)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p, e;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "setp.ne.b32 e, %7, 0;\n\t"
+            "@e tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate), "r"(elected)
+            : "memory");
 }
-// 512 bytes of shared memory (32 lanes x 16 bytes) to four columns of each of the four lane quarters
+// 512 bytes of shared memory (32 lanes x 16 bytes) to four columns of each of the four lane quarters; with CTAS = 2 in both CTAs, each from
+// its own shared memory
+template <int CTAS>
 __device__ __forceinline__ void copy_scales_elected(uint32_t elected, uint32_t tmem, uint64_t desc)
 {
-    asm volatile(
-        "{\n\t.reg .pred e;\n\t"
-        "setp.ne.b32 e, %2, 0;\n\t"
-        "@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}"
-        ::"r"(tmem), "l"(desc), "r"(elected)
-        : "memory");
+    if constexpr (CTAS == 2)
+        asm volatile(
+            "{\n\t.reg .pred e;\n\t"
+            "setp.ne.b32 e, %2, 0;\n\t"
+            "@e tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}"
+            ::"r"(tmem), "l"(desc), "r"(elected)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred e;\n\t"
+            "setp.ne.b32 e, %2, 0;\n\t"
+            "@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}"
+            ::"r"(tmem), "l"(desc), "r"(elected)
+            : "memory");
 }
 // Untiled copy global -> shared; both 16-byte aligned, bytes a multiple of 16.
 __device__ __forceinline__ void bulk_load_elected(uint32_t elected, uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
@@ -101,55 +118,56 @@ __device__ __forceinline__ uint64_t scale_desc(uint32_t saddr)
 
 struct Plan {
     int32_t tile_n;    // tokens of a full tile
-    int32_t tiles_m;   // tiles of weight rows
+    int32_t tiles_m;   // tiles of features
     int32_t num_kb;    // stages of a tile
     int32_t k_blocks;  // blocks of 32 along K
-    int32_t atoms;     // atoms of scales along K
-    int32_t w_row_blocks;  // row blocks of scales of one expert's weights
+    int32_t w_blocks;  // row blocks of one expert's weights
 };
 
-// A tile: expert, its first token (in the expert and as a row of X and Y), how many tokens it has, its first feature.
+// A tile: expert, its first token (in the expert and as a row of Y), how many tokens it has, its first feature.
 struct Tile {
     int32_t expert, first, row, count, feature;
-    __device__ __forceinline__ int width() const { return (count + 15) & ~15; }
 };
-// Walks the tiles that a CTA takes, in rising order; tiles of an expert are ordered features first.
+// Tiles in rising order, those of an expert features first.  A warp looks at 32 experts at a time.
+template <int TILE_M>
 struct TileWalk {
-    int32_t expert = 0, base = 0, next_base = 0;
+    int32_t base = 0;  // the batch of experts that the last tile was found in
     __device__ __forceinline__ bool find(int32_t t, const ExpertTable &table, int E, const Plan &p, Tile &out)
     {
+        const int lane = threadIdx.x & 31;
+        if (t >= table.tile[E]) return false;
         while (true) {
-            if (expert >= E) return false;
-            const int32_t count = table.start[expert + 1] - table.start[expert];
-            const int32_t tiles = (count + p.tile_n - 1) / p.tile_n * p.tiles_m;
-            if (t < base + tiles) {
-                const int32_t local = t - base, n = local / p.tiles_m;
-                out.expert = expert;
+            const uint32_t past = __ballot_sync(0xffffffffu, base + lane < E && table.tile[min(base + lane + 1, E)] > t);
+            if (past != 0) {
+                const int e = base + __ffs(past) - 1;
+                const int32_t local = t - table.tile[e], n = local / p.tiles_m;
+                out.expert = e;
                 out.first = n * p.tile_n;
-                out.row = table.start[expert] + out.first;
-                out.count = min(p.tile_n, count - out.first);
-                out.feature = (local - n * p.tiles_m) * kTileM;
+                out.row = table.start[e] + out.first;
+                out.count = min(p.tile_n, table.start[e + 1] - out.row);
+                out.feature = (local - n * p.tiles_m) * TILE_M;
                 return true;
             }
-            base += tiles;
-            ++expert;
+            base += 32;
         }
     }
 };
 
-template <int BN, int EW, typename T>
+template <int CTAS, int BN, int EW, bool STAGED, typename T>
 __global__ void __launch_bounds__(96 + 32 * EW, 1)
-mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                const __grid_constant__ CUtensorMap map_x32, Mx4GemmArgs a, Plan plan)
+mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x32, const __grid_constant__ CUtensorMap map_x16,
+                const __grid_constant__ CUtensorMap map_s, const __grid_constant__ CUtensorMap map_y, Mx4GemmArgs a, Plan plan)
 {
-    using C = Cfg<BN, EW>;
+    using C = Cfg<CTAS, BN, EW, STAGED, sizeof(T)>;
+    constexpr int TILE_M = kTileRows * CTAS;
+    constexpr int kStep = 16 * CTAS;  // widths of tiles are multiples of this
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t *smem_a = smem;
-    uint8_t *smem_b = smem_a + C::kStages * C::kABytes;
-    uint8_t *smem_sa = smem_b + C::kStages * C::kBBytes;
-    uint8_t *smem_sb = smem_sa + C::kStages * C::kSaBytes;
-    uint64_t *full_bar = reinterpret_cast<uint64_t *>(smem_sb + C::kStages * C::kSbBytes);
+    uint8_t *smem_a = smem;  // codes and scales of the weights
+    uint8_t *smem_b = smem_a + C::kStages * kTileBytes;
+    uint8_t *smem_sb = smem_b + C::kStages * C::kBBytes;
+    uint8_t *smem_stage = smem_sb + C::kStages * C::kSbBytes;
+    uint64_t *full_bar = reinterpret_cast<uint64_t *>(smem_stage + C::kStagingBytes);
     uint64_t *empty_bar = full_bar + C::kStages;
     uint64_t *tmem_full_bar = empty_bar + C::kStages;
     uint64_t *tmem_empty_bar = tmem_full_bar + kAccStages;
@@ -159,40 +177,50 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     ExpertTable table;
     table.start = reinterpret_cast<int32_t *>(tmem_slot + 4);
     table.block = table.start + kMaxExperts + 1;
+    table.tile = table.block + kMaxExperts + 1;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;
+    const bool leader = rank == 0;
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kStages; ++s) {
-            mbar_init(smem_u32(full_bar + s), 2);  // both producers, with their byte counts
+            mbar_init(smem_u32(full_bar + s), 2);  // both producers (the leader's), with the byte counts
             mbar_init(smem_u32(empty_bar + s), 1);
         }
         for (int s = 0; s < kAccStages; ++s) {
             mbar_init(smem_u32(tmem_full_bar + s), 1);
-            mbar_init(smem_u32(tmem_empty_bar + s), EW);
+            mbar_init(smem_u32(tmem_empty_bar + s), EW * CTAS);
         }
         mbar_init(smem_u32(drain_bar), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
+    if (warp == 1) {
+        if (CTAS == 2) tmem_alloc_pair(smem_u32(tmem_slot), C::kTmemCols);
+        else tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
+    }
     // Offsets and weights are there already when the kernel before this one is the quantise pass of the same call; else that
     // kernel may have written them.
     if (!a.weights_early) grid_dependency_wait();
     if (warp == 2) {
-        const bool bad = build_expert_table(table, a.offsets, a.E, (int32_t)a.M);
+        const bool bad = build_expert_table(table, a.offsets, a.E, (int32_t)a.M, plan.tile_n, plan.tiles_m);
         if (bad && lane == 0 && blockIdx.x == 0 && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_INDEX);
     }
     tc_fence_before();
     __syncthreads();
+    if (CTAS == 2) cluster_sync_all();  // the peer's barriers exist before anything signals them
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     grid_dependency_release_next(true);
 
-    const int32_t first_tile = blockIdx.x, tile_step = gridDim.x;
-    TileWalk walk;
+    const int32_t first_tile = blockIdx.x / CTAS, tile_step = gridDim.x / CTAS;
+    TileWalk<TILE_M> walk;
     Tile tile;
+    auto width_of = [&](const Tile &t) { return (t.count + kStep - 1) / kStep * kStep; };
     if (warp == 0 || warp == 2) {
         // ---------------- producers ----------------
+        // A pair's loads all report to the leader's barrier, which its MMA warp waits on.  The tensor maps of the pair see tiles as rows of 128
+        // bytes: 136 of them to a tile, the last 8 its scales.
         const bool weights = warp == 0;
         if (!weights) grid_dependency_wait();
         const uint32_t elected = elect_one();
@@ -201,34 +229,48 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         int64_t issued = 0;
         bool ok = true;
         for (int32_t t = first_tile; ok && walk.find(t, table, a.E, plan, tile); t += tile_step) {
-            const int64_t atom_row = (int64_t)plan.atoms * kAtomBytes;
-            const int w_row = (int)((int64_t)tile.expert * a.N + tile.feature);
-            const uint8_t *sa = a.Ws + ((int64_t)tile.expert * plan.w_row_blocks + tile.feature / kAtomRows) * atom_row;
-            const uint8_t *sb = a.Xs + ((int64_t)table.block[tile.expert] + tile.first / kAtomRows) * atom_row;
-            const bool two_blocks = tile.first % kAtomRows + tile.width() > kAtomRows;
-            const bool whole = tile.width() > BN - kBoxRows;
-            const int boxes = (tile.width() + kBoxRows - 1) / kBoxRows;
+            const int width = width_of(tile), mine = width / CTAS;
+            const int64_t w_tile = ((int64_t)tile.expert * plan.w_blocks + tile.feature / kTileRows + rank) * plan.num_kb;
+            const int first = tile.first + (int)rank * mine, sub = first % kTileRows;
+            const int64_t x_tile = ((int64_t)table.block[tile.expert] + first / kTileRows) * plan.num_kb;
+            const int64_t s_tile = ((int64_t)table.block[tile.expert] + tile.first / kTileRows) * plan.num_kb;
+            const bool two_scales = tile.first % kTileRows + width > kTileRows;  // the tile's tokens lie in two row blocks
+            const int in_first = min(mine, kTileRows - sub);                     // of this CTA's tokens, those in the first row block
             for (int kb = 0; kb < plan.num_kb; ++kb) {
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(empty_bar + s), phase ^ 1u, abort_flag, a.status));
                 if (!ok) break;
                 const uint32_t fb = smem_u32(full_bar + s);
-                const uint32_t scale_bytes = (uint32_t)min(2, plan.atoms - 2 * kb) * kAtomBytes;
-                if (weights) {
-                    mbar_expect_tx_elected(elected, fb, C::kABytes + scale_bytes);
-                    tma_load_2d_elected(elected, smem_u32(smem_a + s * C::kABytes), &map_w, kb * kStageRowBytes, w_row, fb);
-                    bulk_load_elected(elected, smem_u32(smem_sa + s * C::kSaBytes), sa + kb * 2 * kAtomBytes, scale_bytes, fb);
-                } else {
-                    const uint32_t dst = smem_u32(smem_b + s * C::kBBytes), dst_s = smem_u32(smem_sb + s * C::kSbBytes);
-                    mbar_expect_tx_elected(elected, fb, (uint32_t)(whole ? C::kBBytes : boxes * kBoxRows * kStageRowBytes) +
-                                                            scale_bytes * (two_blocks ? 2 : 1));
-                    if (whole) {
-                        tma_load_2d_elected(elected, dst, &map_x, kb * kStageRowBytes, tile.row, fb);
+                const uint32_t dst_b = smem_u32(smem_b + s * C::kBBytes), dst_s = smem_u32(smem_sb + s * C::kSbBytes);
+                const uint32_t bytes = weights ? kTileBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 2 : 1);
+                if constexpr (CTAS == 1) {
+                    mbar_expect_tx_elected(elected, fb, bytes);
+                    if (weights) {
+                        bulk_load_elected(elected, smem_u32(smem_a + s * kTileBytes), a.W + (w_tile + kb) * kTileBytes, kTileBytes, fb);
                     } else {
-                        for (int i = 0; i < boxes; ++i)
-                            tma_load_2d_elected(elected, dst + i * kBoxRows * kStageRowBytes, &map_x32, kb * kStageRowBytes, tile.row + i * kBoxRows, fb);
+                        const uint8_t *x = a.X + (x_tile + kb) * kTileBytes, *xs = a.X + (s_tile + kb) * kTileBytes + kCodeBytes;
+                        const int64_t next_block = (int64_t)plan.num_kb * kTileBytes;
+                        bulk_load_elected(elected, dst_b, x + sub * 128, (uint32_t)in_first * 128, fb);
+                        if (in_first < mine) bulk_load_elected(elected, dst_b + in_first * 128, x + next_block, (uint32_t)(mine - in_first) * 128, fb);
+                        bulk_load_elected(elected, dst_s, xs, kScaleBytes, fb);
+                        if (two_scales) bulk_load_elected(elected, dst_s + kScaleBytes, xs + next_block, kScaleBytes, fb);
                     }
-                    bulk_load_elected(elected, dst_s, sb + kb * 2 * kAtomBytes, scale_bytes, fb);
-                    if (two_blocks) bulk_load_elected(elected, dst_s + 2 * kAtomBytes, sb + atom_row + kb * 2 * kAtomBytes, scale_bytes, fb);
+                } else {
+                    if (leader) mbar_expect_tx_elected(elected, fb, 2 * bytes);
+                    const uint32_t fb_leader = map_to_cta(fb, 0);
+                    constexpr int kRowsPerTile = kTileBytes / 128;
+                    if (weights) {
+                        tma_load_2d_pair_elected(elected, smem_u32(smem_a + s * kTileBytes), &map_w, 0, (int32_t)((w_tile + kb) * kRowsPerTile), fb_leader);
+                    } else {
+                        const int box = mine % 32 == 0 ? 32 : 16;
+                        for (int r = 0; r < mine; r += box) {
+                            const bool second = r >= in_first;
+                            const int64_t at = (x_tile + kb + (second ? plan.num_kb : 0)) * kRowsPerTile + (second ? r - in_first : sub + r);
+                            tma_load_2d_pair_elected(elected, dst_b + r * 128, box == 32 ? &map_x32 : &map_x16, 0, (int32_t)at, fb_leader);
+                        }
+                        for (int i = 0; i < (two_scales ? 2 : 1); ++i)
+                            tma_load_2d_pair_elected(elected, dst_s + i * kScaleBytes, &map_s, 0,
+                                                     (int32_t)((s_tile + kb + i * plan.num_kb) * kRowsPerTile + kTileRows), fb_leader);
+                    }
                 }
                 ++issued;
                 if (++s == C::kStages) { s = 0; phase ^= 1u; }
@@ -238,64 +280,75 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             // Aborting: this warp's copies land before the CTA gives up its shared memory (bounded: the other producer may have stopped
             // a stage earlier, and its barrier then never completes).
             const uint64_t t0 = global_timer_ns();
-            for (int64_t i = 1; i <= (issued < C::kStages ? issued : C::kStages); ++i) {
-                const int64_t k = issued - i;
-                while (!mbar_try_wait(smem_u32(full_bar + k % C::kStages), (uint32_t)(k / C::kStages) & 1u) && global_timer_ns() - t0 < 50000000ull) {}
+            if (leader) {
+                for (int64_t i = 1; i <= (issued < C::kStages ? issued : C::kStages); ++i) {
+                    const int64_t k = issued - i;
+                    while (!mbar_try_wait(smem_u32(full_bar + k % C::kStages), (uint32_t)(k / C::kStages) & 1u) && global_timer_ns() - t0 < 50000000ull) {}
+                }
+            } else {
+                while (global_timer_ns() - t0 < 1000000ull) {}  // the peer cannot poll the leader's barrier
             }
         }
     } else if (warp == 1) {
-        // ---------------- MMA issuer ----------------
-        const uint32_t elected = elect_one();
-        auto uniform = [&](bool mine) { return (bool)__all_sync(0xffffffffu, mine); };
-        int s = 0, as = 0;
-        uint32_t phase = 0, aphase = 0;
-        uint32_t scale_buffer = 0;
-        bool ok = true;
-        for (int32_t t = first_tile; ok && walk.find(t, table, a.E, plan, tile); t += tile_step) {
-            ok = uniform(mbar_wait(smem_u32(tmem_empty_bar + as), aphase ^ 1u, abort_flag, a.status));
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t tmem_d = tmem_base + (uint32_t)(as * BN);
-            const uint32_t idesc = kInstrDesc | ((uint32_t)(tile.width() >> 3) << 17);
-            const int sub = tile.first % kAtomRows;  // a multiple of 32
-            const bool two_blocks = sub + tile.width() > kAtomRows;
-            for (int kb = 0; kb < plan.num_kb; ++kb) {
-                ok = uniform(mbar_wait(smem_u32(full_bar + s), phase, abort_flag, a.status));
+        // ---------------- MMA issuer (the leader's drives the pair) ----------------
+        if (leader) {
+            const uint32_t elected = elect_one();
+            auto uniform = [&](bool mine) { return (bool)__all_sync(0xffffffffu, mine); };
+            auto commit = [&](uint64_t *bar) {
+                if (CTAS == 2) umma_commit_pair_elected(elected, smem_u32(bar));
+                else umma_commit_elected(elected, smem_u32(bar));
+            };
+            int s = 0, as = 0;
+            uint32_t phase = 0, aphase = 0;
+            uint32_t scale_buffer = 0;
+            bool ok = true;
+            for (int32_t t = first_tile; ok && walk.find(t, table, a.E, plan, tile); t += tile_step) {
+                ok = uniform(mbar_wait(smem_u32(tmem_empty_bar + as), aphase ^ 1u, abort_flag, a.status));
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t da = smem_desc_sw128(smem_u32(smem_a + s * C::kABytes));
-                const uint64_t db = smem_desc_sw128(smem_u32(smem_b + s * C::kBBytes));
-                const uint64_t dsa = scale_desc(smem_u32(smem_sa + s * C::kSaBytes)), dsb = scale_desc(smem_u32(smem_sb + s * C::kSbBytes));
-                // scales of this stage: per atom 4 columns for the weights, 8 for the tokens; the two buffers take turns
-                const uint32_t sa_col = tmem_base + (uint32_t)(C::kScaleCol0) + scale_buffer, sb_col = sa_col + 8;
-                scale_buffer = scale_buffer == 0 ? kScaleCols : 0;
-                const int blocks = min(kStageK / kBlock, plan.k_blocks - kb * (kStageK / kBlock));
+                const int width = width_of(tile);
+                const uint32_t tmem_d = tmem_base + (uint32_t)(as * BN);
+                const uint32_t idesc = C::kInstrDesc | ((uint32_t)(width >> 3) << 17);
+                const int sub = tile.first % kTileRows;  // a multiple of 32
+                const bool two_blocks = sub + width > kTileRows;
+                for (int kb = 0; kb < plan.num_kb; ++kb) {
+                    ok = uniform(mbar_wait(smem_u32(full_bar + s), phase, abort_flag, a.status));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t a_addr = smem_u32(smem_a + s * kTileBytes);
+                    const uint64_t da = smem_desc_sw128(a_addr), db = smem_desc_sw128(smem_u32(smem_b + s * C::kBBytes));
+                    const uint64_t dsa = scale_desc(a_addr + kCodeBytes), dsb = scale_desc(smem_u32(smem_sb + s * C::kSbBytes));
+                    // scales of this stage: per atom 4 columns for the weights, 8 for the tokens; the two buffers take turns
+                    const uint32_t sa_col = tmem_base + (uint32_t)(C::kScaleCol0) + scale_buffer, sb_col = sa_col + 8;
+                    scale_buffer = scale_buffer == 0 ? kScaleCols : 0;
+                    const int blocks = min(kTileK / kBlock, plan.k_blocks - kb * (kTileK / kBlock));
 #pragma unroll
-                for (int atom = 0; atom < 2; ++atom) {
-                    if (4 * atom >= blocks) break;
-                    copy_scales_elected(elected, sa_col + 4 * atom, dsa + (uint64_t)(atom * (kAtomBytes >> 4)));
-                    copy_scales_elected(elected, sb_col + 8 * atom, dsb + (uint64_t)(atom * (kAtomBytes >> 4)));
-                    if (two_blocks) copy_scales_elected(elected, sb_col + 8 * atom + 4, dsb + (uint64_t)((2 + atom) * (kAtomBytes >> 4)));
-                }
+                    for (int atom = 0; atom < 2; ++atom) {
+                        if (4 * atom >= blocks) break;
+                        copy_scales_elected<CTAS>(elected, sa_col + 4 * atom, dsa + (uint64_t)(atom * (kAtomBytes >> 4)));
+                        copy_scales_elected<CTAS>(elected, sb_col + 8 * atom, dsb + (uint64_t)(atom * (kAtomBytes >> 4)));
+                        if (two_blocks) copy_scales_elected<CTAS>(elected, sb_col + 8 * atom + 4, dsb + (uint64_t)((2 + atom) * (kAtomBytes >> 4)));
+                    }
 #pragma unroll
-                for (int k = 0; k < kStageK / kMmaK; ++k) {
-                    if (2 * k >= blocks) break;
-                    const uint32_t half = (uint32_t)(k & 1) * 2;  // blocks 0 and 1 or 2 and 3 of the atom
-                    mma_mxf4_elected(elected, tmem_d, da + (uint64_t)(2 * k), db + (uint64_t)(2 * k), idesc | (half << 4) | (half << 29),
-                                     sa_col + 4 * (k >> 1), sb_col + 8 * (k >> 1) + (uint32_t)(sub >> 5), (uint32_t)((kb | k) != 0));
+                    for (int k = 0; k < kTileK / kMmaK; ++k) {
+                        if (2 * k >= blocks) break;
+                        const uint32_t half = (uint32_t)(k & 1) * 2;  // blocks 0 and 1 or 2 and 3 of the atom
+                        mma_mxf4_elected<CTAS>(elected, tmem_d, da + (uint64_t)(2 * k), db + (uint64_t)(2 * k), idesc | (half << 4) | (half << 29),
+                                               sa_col + 4 * (k >> 1), sb_col + 8 * (k >> 1) + (uint32_t)(sub >> 5), (uint32_t)((kb | k) != 0));
+                    }
+                    commit(empty_bar + s);
+                    if (++s == C::kStages) { s = 0; phase ^= 1u; }
                 }
-                umma_commit_elected(elected, smem_u32(empty_bar + s));
-                if (++s == C::kStages) { s = 0; phase ^= 1u; }
+                if (!ok) break;
+                commit(tmem_full_bar + as);
+                if (++as == kAccStages) { as = 0; aphase ^= 1u; }
             }
-            if (!ok) break;
-            umma_commit_elected(elected, smem_u32(tmem_full_bar + as));
-            if (++as == kAccStages) { as = 0; aphase ^= 1u; }
-        }
-        if (!ok) {
-            // Aborting: wait (bounded) for the tensor core to finish what was issued.
-            umma_commit_elected(elected, smem_u32(drain_bar));
-            const uint64_t t0 = global_timer_ns();
-            while (!mbar_try_wait(smem_u32(drain_bar), 0) && global_timer_ns() - t0 < 50000000ull) {}
+            if (!ok) {
+                // Aborting: wait (bounded) for the tensor core to finish what was issued.
+                commit(drain_bar);
+                const uint64_t t0 = global_timer_ns();
+                while (!mbar_try_wait(smem_u32(drain_bar), 0) && global_timer_ns() - t0 < 50000000ull) {}
+            }
         }
     } else {
         // ---------------- epilogue ----------------
@@ -303,64 +356,118 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         const int quarter = warp & 3;  // TMEM lanes 32 * quarter .. + 31
         constexpr int kGroups = EW / 4;  // warps that share a quarter take every kGroups-th run of 32 columns
         const int group = ew >> 2;
+        T *stage = reinterpret_cast<T *>(smem_stage) + ew * (kStoreRows * 32);
         int as = 0;
         uint32_t aphase = 0;
         grid_dependency_wait();  // before anything is written: an earlier kernel may still read Y
         for (int32_t t = first_tile; walk.find(t, table, a.E, plan, tile); t += tile_step) {
-            const int feature = tile.feature + quarter * 32 + lane;
+            const int feature0 = tile.feature + (int)rank * kTileRows + quarter * 32, feature = feature0 + lane;
             const bool mine = feature < a.N;
             const float bias = mine && a.bias != nullptr ? __ldg(a.bias + (int64_t)tile.expert * a.N + feature) : 0.0f;
             const bool ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(tmem_full_bar + as), aphase, abort_flag, a.status));
             if (!ok) break;
             tc_fence_after();
-            T *y = reinterpret_cast<T *>(a.Y) + (int64_t)tile.row * a.ldy + feature;
             const uint32_t acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(as * BN);
+            auto release = [&]() {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (CTAS == 2) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(tmem_empty_bar + as), 0));
+                    else mbar_arrive(smem_u32(tmem_empty_bar + as));
+                }
+            };
+            bool released = false;
             for (int col = group * 32; col < tile.count; col += 32 * kGroups) {
                 uint32_t v[32];
                 tmem_ld_32x32(acc + (uint32_t)col, v);
                 tmem_ld_wait();
+                if (col + 32 * kGroups >= tile.count) {  // the last block of this warp: the accumulator is handed back
+                    release();
+                    released = true;
+                }
+                if (feature0 >= a.N) continue;
 #pragma unroll
-                for (int j = 0; j < 32; j += 2) {
-                    float y0 = __uint_as_float(v[j]) + bias, y1 = __uint_as_float(v[j + 1]) + bias;
-                    if (a.act == Q8_ACT_GELU) gelu_fast_x2(pack_f32x2(y0, y1), y0, y1);
-                    if (mine && col + j < tile.count) y[(int64_t)(col + j) * a.ldy] = from_float<T>(y0);
-                    if (mine && col + j + 1 < tile.count) y[(int64_t)(col + j + 1) * a.ldy] = from_float<T>(y1);
+                for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + bias);
+                if (a.act == Q8_ACT_GELU) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        float y0, y1;
+                        gelu_fast_x2(pack_f32x2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), y0, y1);
+                        v[j] = __float_as_uint(y0);
+                        v[j + 1] = __float_as_uint(y1);
+                    }
+                }
+                // (rows behind the last expert's, or of the next one, are not to be touched: only a plain product's end is cut off by the store)
+                if (STAGED && (col + 32 <= tile.count || a.offsets == nullptr)) {
+                    if (lane == 0) tma_store_wait_read();  // the block before has left the staging buffer
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) stage[j * 32 + lane] = from_float<T>(__uint_as_float(v[j]));
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) tma_store_2d(&map_y, feature0, tile.row + col, smem_u32(stage));
+                } else if (mine) {
+                    T *y = reinterpret_cast<T *>(a.Y) + (int64_t)(tile.row + col) * a.ldy + feature;
+                    if (col + 32 <= tile.count) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j, y += a.ldy) *y = from_float<T>(__uint_as_float(v[j]));
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j, y += a.ldy)
+                            if (col + j < tile.count) *y = from_float<T>(__uint_as_float(v[j]));
+                    }
                 }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(tmem_empty_bar + as));
+            if (!released) release();
             if (++as == kAccStages) { as = 0; aphase ^= 1u; }
         }
+        if (STAGED && lane == 0) tma_store_wait_all();
     }
 
     // ---------------- teardown (reached by every thread, also when aborting) ----------------
     tc_fence_before();
     __syncthreads();
+    if (CTAS == 2) {
+        __syncwarp();
+        cluster_sync_all();  // the peer has finished with this CTA's barriers and with the shared accumulators
+    }
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();
-        tmem_dealloc(tmem_base, C::kTmemCols);
+        if (CTAS == 2) tmem_dealloc_pair(tmem_base, C::kTmemCols);
+        else tmem_dealloc(tmem_base, C::kTmemCols);
     }
 }
 
 // ------------------------------------------------------------------ host side
-// Codes [rows, pitch bytes] in boxes of 128 bytes x box_rows, 128-byte swizzle; what lies outside reads as zero.
-bool codes_map(CUtensorMap *map, const uint8_t *base, int64_t rows, int64_t pitch, int box_rows)
+// Tiles as rows of 128 bytes, boxes of box_rows of them; what lies behind the last reads as zero.
+bool tiles_map(CUtensorMap *map, const uint8_t *base, int64_t tiles, int box_rows)
 {
     const auto fn = encode_tiled_fn();
     if (!fn) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
-    const cuuint32_t box[2] = {kStageRowBytes, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    const cuuint64_t dims[2] = {128, (cuuint64_t)(tiles * (kTileBytes / 128))}, strides[1] = {128};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, estr[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+// The output in blocks of 32 tokens x 32 features; stores are cut off at its edges.
+bool output_map(CUtensorMap *map, const Mx4GemmArgs &a)
+{
+    const auto fn = encode_tiled_fn();
+    if (!fn) return false;
+    const int size = a.y_dtype == Q8_F32 ? 4 : 2;
+    const cuuint64_t dims[2] = {(cuuint64_t)a.N, (cuuint64_t)a.M}, strides[1] = {(cuuint64_t)(a.ldy * size)};
+    const cuuint32_t box[2] = {32, kStoreRows}, estr[2] = {1, 1};
+    return fn(map, size == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, a.Y, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool output_aligned(const Mx4GemmArgs &a) { return reinterpret_cast<uintptr_t>(a.Y) % 16 == 0 && a.ldy * (a.y_dtype == Q8_F32 ? 4 : 2) % 16 == 0; }
 
-template <int BN, int EW, typename T>
+template <int CTAS, int BN, int EW, bool STAGED, typename T>
 cudaError_t launch_typed(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, cudaStream_t s)
 {
-    using C = Cfg<BN, EW>;
-    auto kernel = mx4_gemm_kernel<BN, EW, T>;
+    using C = Cfg<CTAS, BN, EW, STAGED, sizeof(T)>;
+    auto kernel = mx4_gemm_kernel<CTAS, BN, EW, STAGED, T>;
     static bool attr_set[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -371,28 +478,49 @@ cudaError_t launch_typed(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, 
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
-    const int64_t pitch = code_pitch(a.K);
-    CUtensorMap mw, mx, mx32;
-    if (!codes_map(&mw, a.Wq, (int64_t)a.E * a.N, pitch, kTileM) || !codes_map(&mx, a.Xq, a.M, pitch, BN) || !codes_map(&mx32, a.Xq, a.M, pitch, kBoxRows))
-        return cudaErrorInvalidValue;
-    const int sms = sm_count();
-    const int grid = (int)(tiles < sms ? tiles : sms);
+    CUtensorMap mw = {}, mx32 = {}, mx16 = {}, ms = {}, my = {};
+    if (CTAS == 2) {
+        const int64_t w_tiles = (int64_t)a.E * plan.w_blocks * plan.num_kb;
+        const int64_t x_tiles = (a.offsets != nullptr ? most_row_blocks(a.M, a.E) : ceil_div(a.M, kTileRows)) * plan.num_kb;
+        if (!tiles_map(&mw, a.W, w_tiles, kTileBytes / 128) || !tiles_map(&mx32, a.X, x_tiles, 32) || !tiles_map(&mx16, a.X, x_tiles, 16) ||
+            !tiles_map(&ms, a.X, x_tiles, kScaleBytes / 128))
+            return cudaErrorInvalidValue;
+    }
+    if (STAGED && !output_map(&my, a)) return cudaErrorInvalidValue;
+    const int64_t units = sm_count() / CTAS;
+    const int grid = (int)(tiles < units ? tiles : units) * CTAS;
     LaunchInfo &li = last_launch_info();
     li.gemm_kernel = 1;
     li.block_n = plan.tile_n;
-    li.ctas = 1;
+    li.ctas = CTAS;
+    li.epilogue_warps = EW;
+    li.store_mode = STAGED;
     li.grid = grid;
     li.launches += 1;
-    return launch_overlapping_tail(kernel, dim3(grid), dim3(C::kThreads), C::kSmemBytes, s, mw, mx, mx32, a, plan);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(C::kThreads);
+    cfg.dynamicSmemBytes = C::kSmemBytes;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CTAS;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CTAS == 2 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, mw, mx32, mx16, ms, my, a, plan);
 }
 
-template <int BN, int EW>
+template <int CTAS, int BN, int EW, bool STAGED>
 cudaError_t launch_shape(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, cudaStream_t s)
 {
     switch (a.y_dtype) {
-        case Q8_F32: return launch_typed<BN, EW, float>(a, plan, tiles, s);
-        case Q8_F16: return launch_typed<BN, EW, __half>(a, plan, tiles, s);
-        default: return launch_typed<BN, EW, __nv_bfloat16>(a, plan, tiles, s);
+        case Q8_F32: return launch_typed<CTAS, BN, EW, STAGED, float>(a, plan, tiles, s);
+        case Q8_F16: return launch_typed<CTAS, BN, EW, STAGED, __half>(a, plan, tiles, s);
+        default: return launch_typed<CTAS, BN, EW, STAGED, __nv_bfloat16>(a, plan, tiles, s);
     }
 }
 
@@ -401,21 +529,30 @@ cudaError_t launch_shape(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, 
 cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s)
 {
     Plan p;
-    p.tiles_m = (int32_t)ceil_div(a.N, kTileM);
-    p.num_kb = (int32_t)ceil_div(a.K, kStageK);
+    p.num_kb = (int32_t)tiles_along(a.K);
     p.k_blocks = (int32_t)ceil_div(a.K, kBlock);
-    p.atoms = (int32_t)scale_atoms(a.K);
-    p.w_row_blocks = (int32_t)ceil_div(a.N, kAtomRows);
+    p.w_blocks = (int32_t)ceil_div(a.N, kTileRows);
+    p.tiles_m = p.w_blocks;
     const int64_t hit = a.E < a.M ? a.E : a.M;        // experts with tokens, at most
     const int64_t mean = ceil_div(a.M, a.E);
     const int sms = sm_count();
+    const int64_t extra = a.E > 1 ? hit : 0;  // tiles that are not full, at most
+    // pairs once each has work
+    const int64_t pairs = ceil_div(a.N, 2 * kTileRows);
+    if (mean > 128 && (ceil_div(a.M, 192)) * pairs >= sms / 2) {
+        p.tile_n = 192;
+        p.tiles_m = (int32_t)pairs;
+        const int64_t tiles = (ceil_div(a.M, 192) + extra) * pairs;
+        return output_aligned(a) ? launch_shape<2, 192, 16, true>(a, p, tiles, s) : launch_shape<2, 192, 16, false>(a, p, tiles, s);
+    }
     // widest tile that still gives every SM one
     p.tile_n = 192;
     for (int n : {128, 64})
         if (mean <= n || (a.E == 1 && ceil_div(a.M, p.tile_n) * p.tiles_m < sms)) p.tile_n = n;
-    const int64_t tiles = (ceil_div(a.M, p.tile_n) + (a.E > 1 ? hit : 0)) * p.tiles_m;  // at most
+    const int64_t tiles = (ceil_div(a.M, p.tile_n) + extra) * p.tiles_m;  // at most
     if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
-    return p.tile_n == 64 ? launch_shape<64, 8>(a, p, tiles, s) : p.tile_n == 128 ? launch_shape<128, 8>(a, p, tiles, s) : launch_shape<192, 8>(a, p, tiles, s);
+    return p.tile_n == 64 ? launch_shape<1, 64, 8, false>(a, p, tiles, s)
+                          : p.tile_n == 128 ? launch_shape<1, 128, 8, false>(a, p, tiles, s) : launch_shape<1, 192, 8, false>(a, p, tiles, s);
 }
 
 }  // namespace q8

@@ -15,7 +15,6 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <limits>
-#include <vector>
 
 #include "q8.h"
 
@@ -27,7 +26,7 @@ namespace {
     X(q8_linear_workspace_bytes) X(q8_linear_q) X(q8_linear_requant) X(q8_linear_q_requant) X(q8_linear_dyn)            \
     X(q8_embedding) X(q8_add_layernorm) X(q8_add_layernorm_quant) X(q8_add_layernorm_absmax) X(q8_attention)            \
     X(q8_attention_quant) X(q8_attention_absmax) X(q8_embed_layernorm)                                                  \
-    X(q8_mx4_quantize) X(q8_mx4_dequantize) X(q8_mx4_fake_quantize) X(q8_mx4_scales_bytes) X(q8_mx4_linear)             \
+    X(q8_mx4_quantize) X(q8_mx4_dequantize) X(q8_mx4_fake_quantize) X(q8_mx4_bytes) X(q8_mx4_linear)             \
     X(q8_mx4_linear_workspace_bytes) X(q8_mx4_linear_q) X(q8_mx4_linear_grouped) X(q8_mx4_linear_grouped_workspace_bytes)
 #define Q8_DECLARE(name) decltype(&::name) p_##name = nullptr;
 Q8_CALLS(Q8_DECLARE)
@@ -518,33 +517,29 @@ T *mx4_ptr(Call &c, PyObject *o, at::ScalarType type, int64_t values = -1)
     }
     return p;
 }
-// The parts of a quantised tensor (codes, scales, K)
+// A quantised tensor (tiles, shape)
 struct Quantized {
-    const uint8_t *codes = nullptr, *scales = nullptr;
+    const uint8_t *tiles = nullptr;
     const at::Tensor *t = nullptr;
-    int64_t groups = 1, rows = 0, K = 0;
-    Quantized(Call &c, PyObject *o, int64_t dims)
+    int64_t dims = 0, groups = 1, rows = 0, K = 0;
+    Quantized(Call &c, PyObject *o, int64_t want)
     {
-        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3) {
+        c.plain = c.plain && PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 2 && PyTuple_Check(PyTuple_GET_ITEM(o, 1));
+        if (!c.plain) return;
+        PyObject *data = PyTuple_GET_ITEM(o, 0), *shape = PyTuple_GET_ITEM(o, 1);
+        dims = PyTuple_GET_SIZE(shape);
+        c.plain = data != Py_None && (dims == 2 || dims == 3) && (want == 0 || dims == want);
+        if (!c.plain) return;
+        tiles = mx4_ptr<const uint8_t>(c, data, at::kByte);
+        groups = dims == 3 ? c.integer(PyTuple_GET_ITEM(shape, 0)) : 1;
+        rows = c.integer(PyTuple_GET_ITEM(shape, dims - 2));
+        K = c.integer(PyTuple_GET_ITEM(shape, dims - 1));
+        if (!c.plain || K < 1) {
             c.plain = false;
             return;
         }
-        codes = mx4_ptr<const uint8_t>(c, PyTuple_GET_ITEM(o, 0), at::kByte);
-        scales = mx4_ptr<const uint8_t>(c, PyTuple_GET_ITEM(o, 1), at::kByte);
-        K = c.integer(PyTuple_GET_ITEM(o, 2));
-        if (!c.plain || PyTuple_GET_ITEM(o, 0) == Py_None || PyTuple_GET_ITEM(o, 1) == Py_None || K < 1) {
-            c.plain = false;
-            return;
-        }
-        t = &THPVariable_Unpack(PyTuple_GET_ITEM(o, 0));
-        const int64_t d = t->dim();
-        if ((d != 2 && d != 3) || (dims != 0 && d != dims) || t->size(d - 1) != 16 * ((K - 1) / 32 + 1)) {
-            c.plain = false;
-            return;
-        }
-        groups = d == 3 ? t->size(0) : 1;
-        rows = t->size(d - 2);
-        if ((size_t)THPVariable_Unpack(PyTuple_GET_ITEM(o, 1)).numel() < p_q8_mx4_scales_bytes(groups, rows, K)) c.plain = false;
+        t = &THPVariable_Unpack(data);
+        c.plain = groups >= 0 && rows >= 0 && (size_t)t->numel() >= p_q8_mx4_bytes(groups, rows, K);
     }
 };
 // None or a torch.dtype
@@ -594,7 +589,7 @@ struct Mx4Workspace {
     }
 };
 
-// (X, dev_status) -> (codes, scales, K)
+// (X, dev_status) -> tiles
 PyObject *mx4_quantize(Args a)
 {
     Call c;
@@ -602,18 +597,10 @@ PyObject *mx4_quantize(Args a)
     if (!rows_of(c, a[0], 0, &x)) return other_form();
     auto status = mx4_ptr<int32_t>(c, a[1], kI32);
     if (!c.plain || x.K < 1) return other_form();
-    std::vector<int64_t> shape = x.t->sizes().vec();
-    shape.back() = 16 * ((x.K - 1) / 32 + 1);
-    const auto bytes = at::TensorOptions().dtype(at::kByte).device(x.t->device());
-    at::Tensor codes = at::empty(shape, bytes), scales = at::empty({(int64_t)p_q8_mx4_scales_bytes(x.groups, x.rows, x.K)}, bytes);
-    auto q = static_cast<uint8_t *>(codes.data_ptr()), w = static_cast<uint8_t *>(scales.data_ptr());
-    if (!run("q8_mx4_quantize", [&](void *s) { return p_q8_mx4_quantize(x.ptr, x.dtype, x.groups, x.rows, x.K, x.ld, q, w, status, s); })) return nullptr;
-    PyObject *r = PyTuple_New(3);
-    if (r == nullptr) return nullptr;
-    PyTuple_SET_ITEM(r, 0, THPVariable_Wrap(codes));
-    PyTuple_SET_ITEM(r, 1, THPVariable_Wrap(scales));
-    PyTuple_SET_ITEM(r, 2, PyLong_FromLongLong(x.K));
-    return r;
+    at::Tensor tiles = at::empty({(int64_t)p_q8_mx4_bytes(x.groups, x.rows, x.K)}, at::TensorOptions().dtype(at::kByte).device(x.t->device()));
+    auto t = static_cast<uint8_t *>(tiles.data_ptr());
+    if (!run("q8_mx4_quantize", [&](void *s) { return p_q8_mx4_quantize(x.ptr, x.dtype, x.groups, x.rows, x.K, x.ld, t, status, s); })) return nullptr;
+    return THPVariable_Wrap(tiles);
 }
 
 // (T, dtype)
@@ -623,12 +610,10 @@ PyObject *mx4_dequantize(Args a)
     Quantized t(c, a[0], 0);
     at::ScalarType type;
     if (!c.plain || !dtype_or(a[1], at::kFloat, &type)) return other_form();
-    std::vector<int64_t> shape = t.t->sizes().vec();
-    shape.back() = t.K;
-    at::Tensor y = at::empty(shape, at::TensorOptions().dtype(type).device(t.t->device()));
+    const auto options = at::TensorOptions().dtype(type).device(t.t->device());
+    at::Tensor y = t.dims == 3 ? at::empty({t.groups, t.rows, t.K}, options) : at::empty({t.rows, t.K}, options);
     void *p = y.data_ptr();
-    if (!run("q8_mx4_dequantize", [&](void *s) { return p_q8_mx4_dequantize(t.codes, t.scales, t.groups, t.rows, t.K, p, mx4_dtype(type), t.K, s); }))
-        return nullptr;
+    if (!run("q8_mx4_dequantize", [&](void *s) { return p_q8_mx4_dequantize(t.tiles, t.groups, t.rows, t.K, p, mx4_dtype(type), t.K, s); })) return nullptr;
     return THPVariable_Wrap(y);
 }
 
@@ -661,7 +646,7 @@ PyObject *mx4_linear(Args a)
     Mx4Workspace ws(c, a[6], p_q8_mx4_linear_workspace_bytes(x.rows, x.K), *x.t);
     if (!c.plain) return other_form();
     if (!run("q8_mx4_linear", [&](void *s) {
-            return p_q8_mx4_linear(x.ptr, x.dtype, x.ld, w.codes, w.scales, bias, act, y.r.ptr, y.r.dtype, y.r.ld, x.rows, w.rows, x.K, ws.ptr, ws.bytes,
+            return p_q8_mx4_linear(x.ptr, x.dtype, x.ld, w.tiles, bias, act, y.r.ptr, y.r.dtype, y.r.ld, x.rows, w.rows, x.K, ws.ptr, ws.bytes,
                                    status, s);
         }))
         return nullptr;
@@ -680,7 +665,7 @@ PyObject *mx4_linear_q(Args a)
     Mx4Output y(c, a[4], a[5], kF32, x.rows, w.rows, *x.t);
     if (!c.plain) return other_form();
     if (!run("q8_mx4_linear_q", [&](void *s) {
-            return p_q8_mx4_linear_q(x.codes, x.scales, w.codes, w.scales, bias, act, y.r.ptr, y.r.dtype, y.r.ld, x.rows, w.rows, x.K, status, s);
+            return p_q8_mx4_linear_q(x.tiles, w.tiles, bias, act, y.r.ptr, y.r.dtype, y.r.ld, x.rows, w.rows, x.K, status, s);
         }))
         return nullptr;
     return y.result();
@@ -705,7 +690,7 @@ PyObject *mx4_linear_grouped(Args a)
     Mx4Workspace ws(c, a[8], p_q8_mx4_linear_grouped_workspace_bytes(T, w.groups, x.K), *x.t);
     if (!c.plain) return other_form();
     if (!run("q8_mx4_linear_grouped", [&](void *s) {
-            return p_q8_mx4_linear_grouped(x.ptr, x.dtype, x.ld, x.rows, rows, offsets, w.groups, w.codes, w.scales, bias, act, y.r.ptr, y.r.dtype, y.r.ld, T,
+            return p_q8_mx4_linear_grouped(x.ptr, x.dtype, x.ld, x.rows, rows, offsets, w.groups, w.tiles, bias, act, y.r.ptr, y.r.dtype, y.r.ld, T,
                                            w.rows, x.K, ws.ptr, ws.bytes, status, s);
         }))
         return nullptr;

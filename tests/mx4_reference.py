@@ -45,15 +45,18 @@ def rounded(x):
 
 
 def unpack(t, group=0):
-    """Codes and exponents of a matrix (or one group) from the layout that include/q8.h describes."""
-    codes = t.codes if t.codes.dim() == 2 else t.codes[group]
-    rows, blocks = codes.shape[0], codes.shape[1] // 16
-    b = codes.cpu().numpy()
-    code = np.stack([b & 15, b >> 4], -1).reshape(rows, blocks * 32)
-    row_blocks, atoms = -(-rows // 128), -(-t.K // 128)
-    s = t.scales.cpu().numpy()[group * row_blocks * atoms * 512:][:row_blocks * atoms * 512]
-    s = s.reshape(row_blocks, atoms, 32, 4, 4).transpose(0, 3, 2, 1, 4).reshape(row_blocks * 128, atoms * 4)
-    return code.astype(np.int64), s[:rows].astype(np.int64), blocks
+    """Codes and exponents of a matrix (or one group) from the layout that include/q8.h describes, all columns of its tiles."""
+    rows, K = t.shape[-2:]
+    row_tiles, k_tiles = -(-rows // 128), -(-K // 256)
+    tiles = t.tiles.cpu().numpy()[group * row_tiles * k_tiles * 17408:][:row_tiles * k_tiles * 17408].reshape(row_tiles, k_tiles, 17408)
+    b = tiles[:, :, :16384].reshape(row_tiles, k_tiles, 128, 8, 16)
+    code = np.empty_like(b)
+    for r in range(8):
+        for place in range(8):
+            code[:, :, r::8, place ^ r] = b[:, :, r::8, place]
+    code = np.stack([code & 15, code >> 4], -1).transpose(0, 2, 1, 3, 4, 5).reshape(row_tiles * 128, k_tiles * 256)
+    s = tiles[:, :, 16384:].reshape(row_tiles, k_tiles, 2, 32, 4, 4).transpose(0, 4, 3, 1, 2, 5).reshape(row_tiles * 128, k_tiles * 8)
+    return code[:rows].astype(np.int64), s[:rows].astype(np.int64), -(-K // 32)
 
 
 def gelu(y):

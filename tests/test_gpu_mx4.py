@@ -34,7 +34,7 @@ def check_codes(t, x, group=0):
     want_code, want_E = ref.quantize(ref.as_numpy(x))
     assert np.array_equal(E[:, :blocks], want_E)
     assert not E[:, blocks:].any(), "scales behind the last block"
-    assert np.array_equal(code, want_code)
+    assert np.array_equal(code[:, :32 * blocks], want_code) and not code[:, 32 * blocks:].any()
 
 
 # ---------------------------------------------------------------- quantisation
@@ -44,7 +44,7 @@ def test_quantize(rows, K, dtype):
     x = values((rows, K), rows + K, dtype)
     word = status_word()
     t = q8.q8_mx4_quantize(x, dev_status=word)
-    assert t.codes.shape == (rows, 16 * -(-K // 32)) and t.K == K
+    assert t.tiles.numel() == q8.q8_mx4_bytes(1, rows, K) and t.shape == (rows, K)
     check_codes(t, x)
     assert word.item() == 0
     for out in TYPES:
@@ -284,7 +284,7 @@ def test_grouped_many_experts():
 def test_grouped_is_the_plain_layer_for_one_expert():
     x, w = values((300, 512), 1, torch.bfloat16), weights((1, 384, 512), 2)
     W = q8.q8_mx4_quantize(w)
-    one = q8.Mx4(W.codes[0], W.scales, W.K)
+    one = q8.Mx4(W.tiles, W.shape[1:])
     offsets = torch.tensor([0, 300], dtype=torch.int32).cuda()
     assert torch.equal(q8.q8_mx4_linear_grouped(x, offsets, W), q8.q8_mx4_linear(x, one))
 
@@ -414,8 +414,7 @@ def test_weights_made_right_before_the_layer():
     got = []
     for w in ws:
         fresh = q8.q8_mx4_quantize(w)
-        W.codes.copy_(fresh.codes)
-        W.scales.copy_(fresh.scales)
+        W.tiles.copy_(fresh.tiles)
         got.append(q8.q8_mx4_linear(x, W))
         fresh = q8.q8_mx4_quantize(w)
         got.append(q8.q8_mx4_linear(x, fresh))
@@ -439,10 +438,10 @@ def test_refusals_on_the_device():
         q8.q8_mx4_linear(values((64, 4), 1).t(), W)
     with pytest.raises(TypeError, match="overlap"):
         q8.q8_mx4_linear(values((1, 64), 1).expand(4, 64), W)
-    with pytest.raises(ValueError, match="bytes of scales"):
-        q8.q8_mx4_linear(x, q8.Mx4(W.codes, W.scales[:100], W.K))
-    with pytest.raises(ValueError, match="do not hold"):
-        q8.q8_mx4_linear(x, q8.Mx4(W.codes, W.scales, 65))
+    with pytest.raises(ValueError, match="bytes of tiles"):
+        q8.q8_mx4_linear(x, q8.Mx4(W.tiles[:17407], W.shape))
+    with pytest.raises(ValueError, match="bytes of tiles"):
+        q8.q8_mx4_linear(values((4, 257), 1), q8.Mx4(W.tiles, (8, 257)))
     with pytest.raises(q8.Q8Error) as e:
         q8.q8_mx4_linear(x, W, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert e.value.status == q8.Q8_ERR_WORKSPACE

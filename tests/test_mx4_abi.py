@@ -18,35 +18,34 @@ def lib():
 
 
 def test_sizes(lib):
-    assert [q8.q8_mx4_codes_bytes(5, K) for K in (1, 32, 33, 1000)] == [80, 80, 160, 2560]
-    assert [q8.q8_mx4_scales_bytes(1, r, K) for r, K in ((1, 1), (128, 128), (129, 128), (128, 129), (0, 5))] == [512, 512, 1024, 1024, 0]
-    assert q8.q8_mx4_scales_bytes(3, 130, 300) == 3 * 2 * 3 * 512
-    assert q8.q8_mx4_codes_bytes(-1, 4) == q8.q8_mx4_codes_bytes(4, 0) == q8.q8_mx4_scales_bytes(1 << 30, 4, 4) == 0
-    assert q8.q8_mx4_linear_workspace_bytes(3, 64) == 256 + 512
-    assert q8.q8_mx4_linear_grouped_workspace_bytes(300, 7, 64) == 9728 + (2 + 7) * 512
-    assert q8.q8_mx4_linear_grouped_workspace_bytes(4, 1000, 64) == 256 + 4 * 512
+    assert [q8.q8_mx4_bytes(1, r, K) // 17408 for r, K in ((1, 1), (128, 256), (129, 256), (128, 257), (0, 5))] == [1, 1, 2, 2, 0]
+    assert q8.q8_mx4_bytes(3, 130, 600) == 3 * 2 * 3 * 17408
+    assert q8.q8_mx4_bytes(1, -1, 4) == q8.q8_mx4_bytes(1, 4, 0) == q8.q8_mx4_bytes(1 << 30, 4, 4) == 0
+    assert q8.q8_mx4_linear_workspace_bytes(3, 64) == 17408
+    assert q8.q8_mx4_linear_grouped_workspace_bytes(300, 7, 64) == (2 + 7) * 17408
+    assert q8.q8_mx4_linear_grouped_workspace_bytes(4, 1000, 64) == 4 * 17408
     assert q8.q8_mx4_linear_grouped_workspace_bytes(4, 1025, 64) == 0
 
 
-def linear(lib, X=FAKE, xt=0, ldx=64, Wq=FAKE, Ws=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, M=4, N=8, K=64, ws=FAKE, size=MANY, word=None):
-    return lib.q8_mx4_linear(X, xt, ldx, Wq, Ws, bias, act, Y, yt, ldy, M, N, K, ws, size, word, None)
+def linear(lib, X=FAKE, xt=0, ldx=64, Wq=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, M=4, N=8, K=64, ws=FAKE, size=MANY, word=None):
+    return lib.q8_mx4_linear(X, xt, ldx, Wq, bias, act, Y, yt, ldy, M, N, K, ws, size, word, None)
 
 
-def linear_q(lib, Xq=FAKE, Xs=FAKE, Wq=FAKE, Ws=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, M=4, N=8, K=64, word=None):
-    return lib.q8_mx4_linear_q(Xq, Xs, Wq, Ws, bias, act, Y, yt, ldy, M, N, K, word, None)
+def linear_q(lib, Xq=FAKE, Wq=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, M=4, N=8, K=64, word=None):
+    return lib.q8_mx4_linear_q(Xq, Wq, bias, act, Y, yt, ldy, M, N, K, word, None)
 
 
-def grouped(lib, X=FAKE, xt=0, ldx=64, x_rows=4, rows=None, offsets=FAKE, E=3, Wq=FAKE, Ws=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, T=4, N=8, K=64,
+def grouped(lib, X=FAKE, xt=0, ldx=64, x_rows=4, rows=None, offsets=FAKE, E=3, Wq=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, T=4, N=8, K=64,
             ws=FAKE, size=MANY, word=None):
-    return lib.q8_mx4_linear_grouped(X, xt, ldx, x_rows, rows, offsets, E, Wq, Ws, bias, act, Y, yt, ldy, T, N, K, ws, size, word, None)
+    return lib.q8_mx4_linear_grouped(X, xt, ldx, x_rows, rows, offsets, E, Wq, bias, act, Y, yt, ldy, T, N, K, ws, size, word, None)
 
 
-def quantize(lib, X=FAKE, t=0, G=1, R=4, K=64, ld=64, codes=FAKE, scales=FAKE, word=None):
-    return lib.q8_mx4_quantize(X, t, G, R, K, ld, codes, scales, word, None)
+def quantize(lib, X=FAKE, t=0, G=1, R=4, K=64, ld=64, out=FAKE, word=None):
+    return lib.q8_mx4_quantize(X, t, G, R, K, ld, out, word, None)
 
 
-def dequantize(lib, codes=FAKE, scales=FAKE, G=1, R=4, K=64, Y=FAKE, t=0, ld=64):
-    return lib.q8_mx4_dequantize(codes, scales, G, R, K, Y, t, ld, None)
+def dequantize(lib, T=FAKE, G=1, R=4, K=64, Y=FAKE, t=0, ld=64):
+    return lib.q8_mx4_dequantize(T, G, R, K, Y, t, ld, None)
 
 
 def fake(lib, X=FAKE, t=0, R=4, K=64, ld=64, out=FAKE, ldo=64, word=None):
@@ -54,11 +53,11 @@ def fake(lib, X=FAKE, t=0, R=4, K=64, ld=64, out=FAKE, ldo=64, word=None):
 
 
 @pytest.mark.parametrize("call,arguments,status", [
-    *[(linear, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "Wq", "Ws", "Y", "ws")],
-    *[(linear_q, {k: None}, q8.Q8_ERR_NULL) for k in ("Xq", "Xs", "Wq", "Ws", "Y")],
-    *[(grouped, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "offsets", "Wq", "Ws", "Y", "ws")],
-    *[(quantize, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "codes", "scales")],
-    *[(dequantize, {k: None}, q8.Q8_ERR_NULL) for k in ("Y", "codes", "scales")],
+    *[(linear, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "Wq", "Y", "ws")],
+    *[(linear_q, {k: None}, q8.Q8_ERR_NULL) for k in ("Xq", "Wq", "Y")],
+    *[(grouped, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "offsets", "Wq", "Y", "ws")],
+    *[(quantize, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "out")],
+    *[(dequantize, {k: None}, q8.Q8_ERR_NULL) for k in ("Y", "T")],
     *[(fake, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "out")],
     *[(call, {k: 3}, q8.Q8_ERR_ARG) for call in (linear, grouped) for k in ("xt", "yt", "act")],
     *[(call, {"t": 7}, q8.Q8_ERR_ARG) for call in (quantize, dequantize, fake)],
@@ -72,12 +71,12 @@ def fake(lib, X=FAKE, t=0, R=4, K=64, ld=64, out=FAKE, ldo=64, word=None):
         {"T": -1}, {"T": 5}, {"E": -1}, {"E": 1025}, {"x_rows": -1}, {"x_rows": 3}, {"K": 0}, {"ldx": 1}, {"ldy": 7}, {"N": 1 << 30, "ldy": 1 << 30})],
     *[(quantize, bad, q8.Q8_ERR_SHAPE) for bad in ({"G": -1}, {"R": -1}, {"K": 0}, {"ld": 63}, {"G": 1 << 20, "R": 1 << 20})],
     (dequantize, {"ld": 1}, q8.Q8_ERR_SHAPE), (fake, {"ld": 1}, q8.Q8_ERR_SHAPE), (fake, {"ldo": 1}, q8.Q8_ERR_SHAPE),
-    *[(linear, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("X", 2), ("Wq", 8), ("Ws", 8), ("bias", 2), ("Y", 2), ("ws", 128), ("word", 2))],
-    *[(linear_q, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("Xq", 8), ("Xs", 8), ("Wq", 8), ("Ws", 8), ("bias", 2), ("Y", 2), ("word", 2))],
-    *[(grouped, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("X", 2), ("rows", 2), ("offsets", 2), ("Wq", 8), ("Ws", 8), ("bias", 2), ("Y", 2), ("ws", 128))],
-    (linear, {"xt": 1, "X": FAKE + 1}, q8.Q8_ERR_ALIGN), (quantize, {"X": FAKE + 2}, q8.Q8_ERR_ALIGN), (quantize, {"codes": FAKE + 4}, q8.Q8_ERR_ALIGN),
-    (dequantize, {"scales": FAKE + 4}, q8.Q8_ERR_ALIGN), (fake, {"out": FAKE + 1}, q8.Q8_ERR_ALIGN),
-    (linear, {"size": 256 + 511}, q8.Q8_ERR_WORKSPACE), (grouped, {"size": 256 + 3 * 512 - 1}, q8.Q8_ERR_WORKSPACE),
+    *[(linear, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("X", 2), ("Wq", 8), ("bias", 2), ("Y", 2), ("ws", 128), ("word", 2))],
+    *[(linear_q, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("Xq", 8), ("Wq", 8), ("bias", 2), ("Y", 2), ("word", 2))],
+    *[(grouped, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("X", 2), ("rows", 2), ("offsets", 2), ("Wq", 8), ("bias", 2), ("Y", 2), ("ws", 128))],
+    (linear, {"xt": 1, "X": FAKE + 1}, q8.Q8_ERR_ALIGN), (quantize, {"X": FAKE + 2}, q8.Q8_ERR_ALIGN), (quantize, {"out": FAKE + 4}, q8.Q8_ERR_ALIGN),
+    (dequantize, {"T": FAKE + 4}, q8.Q8_ERR_ALIGN), (fake, {"out": FAKE + 1}, q8.Q8_ERR_ALIGN),
+    (linear, {"size": 17407}, q8.Q8_ERR_WORKSPACE), (grouped, {"size": 3 * 17408 - 1}, q8.Q8_ERR_WORKSPACE),
     # nothing to do: never reaches the device
     *[(call, {k: 0}, q8.Q8_OK) for call in (linear, linear_q) for k in ("M", "N")], *[(grouped, {k: 0}, q8.Q8_OK) for k in ("T", "N", "E")],
     *[(quantize, {k: 0, "X": None}, q8.Q8_OK) for k in ("G", "R")], (dequantize, {"R": 0}, q8.Q8_OK), (fake, {"R": 0, "X": None}, q8.Q8_OK)])
@@ -86,7 +85,7 @@ def test_refusals(lib, call, arguments, status):
 
 
 def test_tensors_of_the_host_are_refused(lib):
-    W = q8.Mx4(torch.zeros(8, 32, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8), 64)
+    W = q8.Mx4(torch.zeros(17408, dtype=torch.uint8), (8, 64))
     with pytest.raises(TypeError, match="X must be a CUDA tensor"):
         q8.q8_mx4_quantize(torch.zeros(4, 64))
     with pytest.raises(TypeError, match="CUDA tensor"):
