@@ -47,68 +47,54 @@ struct Cfg {
     static constexpr int kTableBytes = 3 * (kMaxExperts + 1) * 4 + 4;
     static constexpr int kBudget = 227 * 1024 - 1024 - kTableBytes - kStagingBytes - 512;
     static constexpr int kStages = kBudget / kStageBytes > 8 ? 8 : kBudget / kStageBytes;
-    static constexpr int kScaleCol0 = kAccStages * BN;
+    // Two accumulators of 256 columns leave no room for the scales: they share 48 columns, which the epilogue empties first.
+    static constexpr int kAccStride = BN == 256 ? 512 - 2 * kScaleCols - 256 : BN;
+    static constexpr int kScaleCol0 = kAccStride + BN;
     static constexpr int kTmemCols = kScaleCol0 + 2 * kScaleCols <= 128 ? 128 : kScaleCol0 + 2 * kScaleCols <= 256 ? 256 : 512;
     static constexpr int kBarrierBytes = (2 * kStages + 2 * kAccStages + 1) * 8 + 16;
     static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStagingBytes + kTableBytes + kBarrierBytes;
     static_assert(kScaleCol0 + 2 * kScaleCols <= 512, "TMEM columns");
     static_assert(kSmemBytes <= 232448 && kStages >= 3, "shared memory budget");
-    static_assert(BN % (32 * CTAS) == 0 && BN <= 192 && kBBytes % 1024 == 0, "tile width");
+    static_assert(BN % (32 * CTAS) == 0 && (BN <= 192 || (BN == 256 && CTAS == 2 && EW == 16)) && kBBytes % 1024 == 0, "tile width");
     // Instruction descriptor of kind::mxf4: E2M1 operands, both K-major, UE8M0 scales, M = 128 or 256 for the pair; N / 8 in bits
     // 17..22, which half of a scale word serves in bits 4..5 (B) and 29..30 (A).
     static constexpr uint32_t kInstrDesc = (1u << 7) | (1u << 10) | (1u << 23) | ((uint32_t)CTAS << 27);
 };
 
+// The instructions below are issued by one elected lane.
 template <int CTAS>
-__device__ __forceinline__ void mma_mxf4_elected(uint32_t elected, uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc,
-                                                 uint32_t tmem_sa, uint32_t tmem_sb, uint32_t accumulate)
+__device__ __forceinline__ void mma_mxf4(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t tmem_sa, uint32_t tmem_sb,
+                                         uint32_t accumulate)
 {
     if constexpr (CTAS == 2)
         asm volatile(
-            "{\n\t.reg .pred p, e;\n\t"
+            "{\n\t.reg .pred p;\n\t"
             "setp.ne.b32 p, %6, 0;\n\t"
-            "setp.ne.b32 e, %7, 0;\n\t"
-            "@e tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate), "r"(elected)
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate)
             : "memory");
     else
         asm volatile(
-            "{\n\t.reg .pred p, e;\n\t"
+            "{\n\t.reg .pred p;\n\t"
             "setp.ne.b32 p, %6, 0;\n\t"
-            "setp.ne.b32 e, %7, 0;\n\t"
-            "@e tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate), "r"(elected)
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate)
             : "memory");
 }
 // 512 bytes of shared memory (32 lanes x 16 bytes) to four columns of each of the four lane quarters; with CTAS = 2 in both CTAs, each from
 // its own shared memory
 template <int CTAS>
-__device__ __forceinline__ void copy_scales_elected(uint32_t elected, uint32_t tmem, uint64_t desc)
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc)
 {
-    if constexpr (CTAS == 2)
-        asm volatile(
-            "{\n\t.reg .pred e;\n\t"
-            "setp.ne.b32 e, %2, 0;\n\t"
-            "@e tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}"
-            ::"r"(tmem), "l"(desc), "r"(elected)
-            : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred e;\n\t"
-            "setp.ne.b32 e, %2, 0;\n\t"
-            "@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}"
-            ::"r"(tmem), "l"(desc), "r"(elected)
-            : "memory");
+    if constexpr (CTAS == 2) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 // Untiled copy global -> shared; both 16-byte aligned, bytes a multiple of 16.
-__device__ __forceinline__ void bulk_load_elected(uint32_t elected, uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {
-    asm volatile(
-        "{\n\t.reg .pred e;\n\t"
-        "setp.ne.b32 e, %4, 0;\n\t"
-        "@e cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
-        ::"r"(dst), "l"(src), "r"(bytes), "r"(bar), "r"(elected)
-        : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
 }
 // An atom of scales in shared memory: no swizzle, 8 rows of 16 bytes contiguous, 128 bytes from one group of 8 to the next.
 __device__ __forceinline__ uint64_t scale_desc(uint32_t saddr)
@@ -155,7 +141,7 @@ struct TileWalk {
 
 template <int CTAS, int BN, int EW, bool STAGED, typename T>
 __global__ void __launch_bounds__(96 + 32 * EW, 1)
-mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x32, const __grid_constant__ CUtensorMap map_x16,
+mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_x32, const __grid_constant__ CUtensorMap map_x16,
                 const __grid_constant__ CUtensorMap map_s, const __grid_constant__ CUtensorMap map_y, Mx4GemmArgs a, Plan plan)
 {
     using C = Cfg<CTAS, BN, EW, STAGED, sizeof(T)>;
@@ -222,7 +208,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         // A pair's loads all report to the leader's barrier, which its MMA warp waits on.  The tensor maps of the pair see tiles as rows of 128
         // bytes: 136 of them to a tile, the last 8 its scales.
         const bool weights = warp == 0;
-        if (!weights) grid_dependency_wait();
+        if (!weights || CTAS == 2) grid_dependency_wait();  // (a pair's weight producer loads token scales too)
         const uint32_t elected = elect_one();
         int s = 0;
         uint32_t phase = 0;
@@ -236,42 +222,50 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             const int64_t s_tile = ((int64_t)table.block[tile.expert] + tile.first / kTileRows) * plan.num_kb;
             const bool two_scales = tile.first % kTileRows + width > kTileRows;  // the tile's tokens lie in two row blocks
             const int in_first = min(mine, kTileRows - sub);                     // of this CTA's tokens, those in the first row block
+            const uint32_t bytes = CTAS == 1 ? (weights ? kTileBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 2 : 1))
+                                             : 2 * (weights ? kTileBytes + kScaleBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 1 : 0));
             for (int kb = 0; kb < plan.num_kb; ++kb) {
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(empty_bar + s), phase ^ 1u, abort_flag, a.status));
                 if (!ok) break;
-                const uint32_t fb = smem_u32(full_bar + s);
-                const uint32_t dst_b = smem_u32(smem_b + s * C::kBBytes), dst_s = smem_u32(smem_sb + s * C::kSbBytes);
-                const uint32_t bytes = weights ? kTileBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 2 : 1);
-                if constexpr (CTAS == 1) {
-                    mbar_expect_tx_elected(elected, fb, bytes);
-                    if (weights) {
-                        bulk_load_elected(elected, smem_u32(smem_a + s * kTileBytes), a.W + (w_tile + kb) * kTileBytes, kTileBytes, fb);
-                    } else {
-                        const uint8_t *x = a.X + (x_tile + kb) * kTileBytes, *xs = a.X + (s_tile + kb) * kTileBytes + kCodeBytes;
-                        const int64_t next_block = (int64_t)plan.num_kb * kTileBytes;
-                        bulk_load_elected(elected, dst_b, x + sub * 128, (uint32_t)in_first * 128, fb);
-                        if (in_first < mine) bulk_load_elected(elected, dst_b + in_first * 128, x + next_block, (uint32_t)(mine - in_first) * 128, fb);
-                        bulk_load_elected(elected, dst_s, xs, kScaleBytes, fb);
-                        if (two_scales) bulk_load_elected(elected, dst_s + kScaleBytes, xs + next_block, kScaleBytes, fb);
-                    }
-                } else {
-                    if (leader) mbar_expect_tx_elected(elected, fb, 2 * bytes);
-                    const uint32_t fb_leader = map_to_cta(fb, 0);
-                    constexpr int kRowsPerTile = kTileBytes / 128;
-                    if (weights) {
-                        tma_load_2d_pair_elected(elected, smem_u32(smem_a + s * kTileBytes), &map_w, 0, (int32_t)((w_tile + kb) * kRowsPerTile), fb_leader);
-                    } else {
-                        const int box = mine % 32 == 0 ? 32 : 16;
-                        for (int r = 0; r < mine; r += box) {
-                            const bool second = r >= in_first;
-                            const int64_t at = (x_tile + kb + (second ? plan.num_kb : 0)) * kRowsPerTile + (second ? r - in_first : sub + r);
-                            tma_load_2d_pair_elected(elected, dst_b + r * 128, box == 32 ? &map_x32 : &map_x16, 0, (int32_t)at, fb_leader);
+                if (elected) {
+                    const uint32_t fb = smem_u32(full_bar + s);
+                    const uint32_t dst_b = smem_u32(smem_b + s * C::kBBytes), dst_s = smem_u32(smem_sb + s * C::kSbBytes);
+                    if constexpr (CTAS == 1) {
+                        mbar_expect_tx(fb, bytes);
+                        if (weights) {
+                            bulk_load(smem_u32(smem_a + s * kTileBytes), a.W + (w_tile + kb) * kTileBytes, kTileBytes, fb);
+                        } else {
+                            const uint8_t *x = a.X + (x_tile + kb) * kTileBytes, *xs = a.X + (s_tile + kb) * kTileBytes + kCodeBytes;
+                            const int64_t next_block = (int64_t)plan.num_kb * kTileBytes;
+                            bulk_load(dst_b, x + sub * 128, (uint32_t)in_first * 128, fb);
+                            if (in_first < mine) bulk_load(dst_b + in_first * 128, x + next_block, (uint32_t)(mine - in_first) * 128, fb);
+                            bulk_load(dst_s, xs, kScaleBytes, fb);
+                            if (two_scales) bulk_load(dst_s + kScaleBytes, xs + next_block, kScaleBytes, fb);
                         }
-                        for (int i = 0; i < (two_scales ? 2 : 1); ++i)
-                            tma_load_2d_pair_elected(elected, dst_s + i * kScaleBytes, &map_s, 0,
-                                                     (int32_t)((s_tile + kb + i * plan.num_kb) * kRowsPerTile + kTileRows), fb_leader);
+                    } else {
+                        if (leader) mbar_expect_tx(fb, bytes);
+                        const uint32_t fb_leader = map_to_cta(fb, 0);
+                        constexpr int kRowsPerTile = kTileBytes / 128;
+                        if (weights) {
+                            tma_load_2d_pair(smem_u32(smem_a + s * kTileBytes), &map_w, 0, (int32_t)(w_tile + kb) * kRowsPerTile, fb_leader);
+                            tma_load_2d_pair(dst_s, &map_s, 0, (int32_t)(s_tile + kb) * kRowsPerTile + kTileRows, fb_leader);
+                        } else {
+                            if (mine == kTileRows) {
+                                tma_load_2d_pair(dst_b, &map_x, 0, (int32_t)(x_tile + kb) * kRowsPerTile, fb_leader);
+                            } else {
+                                const int box = mine % 32 == 0 ? 32 : 16;
+                                for (int r = 0; r < mine; r += box) {
+                                    const bool second = r >= in_first;
+                                    const int32_t at = (int32_t)(x_tile + kb + (second ? plan.num_kb : 0)) * kRowsPerTile + (second ? r - in_first : sub + r);
+                                    tma_load_2d_pair(dst_b + r * 128, box == 32 ? &map_x32 : &map_x16, 0, at, fb_leader);
+                                }
+                            }
+                            if (two_scales)
+                                tma_load_2d_pair(dst_s + kScaleBytes, &map_s, 0, (int32_t)(s_tile + kb + plan.num_kb) * kRowsPerTile + kTileRows, fb_leader);
+                        }
                     }
                 }
+                __syncwarp();
                 ++issued;
                 if (++s == C::kStages) { s = 0; phase ^= 1u; }
             }
@@ -295,19 +289,21 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             const uint32_t elected = elect_one();
             auto uniform = [&](bool mine) { return (bool)__all_sync(0xffffffffu, mine); };
             auto commit = [&](uint64_t *bar) {
-                if (CTAS == 2) umma_commit_pair_elected(elected, smem_u32(bar));
-                else umma_commit_elected(elected, smem_u32(bar));
+                if (CTAS == 2) umma_commit_pair(smem_u32(bar));
+                else umma_commit(smem_u32(bar));
             };
             int s = 0, as = 0;
             uint32_t phase = 0, aphase = 0;
             uint32_t scale_buffer = 0;
             bool ok = true;
             for (int32_t t = first_tile; ok && walk.find(t, table, a.E, plan, tile); t += tile_step) {
-                ok = uniform(mbar_wait(smem_u32(tmem_empty_bar + as), aphase ^ 1u, abort_flag, a.status));
+                // the tile before last has left this accumulator, or the last one the columns that it shares with it
+                constexpr bool kShared = C::kAccStride < BN;
+                ok = uniform(mbar_wait(smem_u32(tmem_empty_bar + (kShared ? as ^ 1 : as)), kShared && as == 1 ? aphase : aphase ^ 1u, abort_flag, a.status));
                 if (!ok) break;
                 tc_fence_after();
                 const int width = width_of(tile);
-                const uint32_t tmem_d = tmem_base + (uint32_t)(as * BN);
+                const uint32_t tmem_d = tmem_base + (uint32_t)(as * C::kAccStride);
                 const uint32_t idesc = C::kInstrDesc | ((uint32_t)(width >> 3) << 17);
                 const int sub = tile.first % kTileRows;  // a multiple of 32
                 const bool two_blocks = sub + width > kTileRows;
@@ -322,30 +318,34 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                     const uint32_t sa_col = tmem_base + (uint32_t)(C::kScaleCol0) + scale_buffer, sb_col = sa_col + 8;
                     scale_buffer = scale_buffer == 0 ? kScaleCols : 0;
                     const int blocks = min(kTileK / kBlock, plan.k_blocks - kb * (kTileK / kBlock));
+                    if (elected) {
 #pragma unroll
-                    for (int atom = 0; atom < 2; ++atom) {
-                        if (4 * atom >= blocks) break;
-                        copy_scales_elected<CTAS>(elected, sa_col + 4 * atom, dsa + (uint64_t)(atom * (kAtomBytes >> 4)));
-                        copy_scales_elected<CTAS>(elected, sb_col + 8 * atom, dsb + (uint64_t)(atom * (kAtomBytes >> 4)));
-                        if (two_blocks) copy_scales_elected<CTAS>(elected, sb_col + 8 * atom + 4, dsb + (uint64_t)((2 + atom) * (kAtomBytes >> 4)));
-                    }
+                        for (int atom = 0; atom < 2; ++atom) {
+                            if (4 * atom >= blocks) break;
+                            copy_scales<CTAS>(sa_col + 4 * atom, dsa + (uint64_t)(atom * (kAtomBytes >> 4)));
+                            copy_scales<CTAS>(sb_col + 8 * atom, dsb + (uint64_t)(atom * (kAtomBytes >> 4)));
+                            if (two_blocks) copy_scales<CTAS>(sb_col + 8 * atom + 4, dsb + (uint64_t)((2 + atom) * (kAtomBytes >> 4)));
+                        }
 #pragma unroll
-                    for (int k = 0; k < kTileK / kMmaK; ++k) {
-                        if (2 * k >= blocks) break;
-                        const uint32_t half = (uint32_t)(k & 1) * 2;  // blocks 0 and 1 or 2 and 3 of the atom
-                        mma_mxf4_elected<CTAS>(elected, tmem_d, da + (uint64_t)(2 * k), db + (uint64_t)(2 * k), idesc | (half << 4) | (half << 29),
-                                               sa_col + 4 * (k >> 1), sb_col + 8 * (k >> 1) + (uint32_t)(sub >> 5), (uint32_t)((kb | k) != 0));
+                        for (int k = 0; k < kTileK / kMmaK; ++k) {
+                            if (2 * k >= blocks) break;
+                            const uint32_t half = (uint32_t)(k & 1) * 2;  // blocks 0 and 1 or 2 and 3 of the atom
+                            mma_mxf4<CTAS>(tmem_d, da + (uint64_t)(2 * k), db + (uint64_t)(2 * k), idesc | (half << 4) | (half << 29), sa_col + 4 * (k >> 1),
+                                           sb_col + 8 * (k >> 1) + (uint32_t)(sub >> 5), (uint32_t)((kb | k) != 0));
+                        }
+                        commit(empty_bar + s);
+                        if (kb + 1 == plan.num_kb) commit(tmem_full_bar + as);
                     }
-                    commit(empty_bar + s);
+                    __syncwarp();
                     if (++s == C::kStages) { s = 0; phase ^= 1u; }
                 }
                 if (!ok) break;
-                commit(tmem_full_bar + as);
                 if (++as == kAccStages) { as = 0; aphase ^= 1u; }
             }
             if (!ok) {
                 // Aborting: wait (bounded) for the tensor core to finish what was issued.
-                commit(drain_bar);
+                if (elected) commit(drain_bar);
+                __syncwarp();
                 const uint64_t t0 = global_timer_ns();
                 while (!mbar_try_wait(smem_u32(drain_bar), 0) && global_timer_ns() - t0 < 50000000ull) {}
             }
@@ -367,7 +367,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             const bool ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(tmem_full_bar + as), aphase, abort_flag, a.status));
             if (!ok) break;
             tc_fence_after();
-            const uint32_t acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(as * BN);
+            const uint32_t acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(as * C::kAccStride);
             auto release = [&]() {
                 tc_fence_before();
                 __syncwarp();
@@ -376,12 +376,18 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                     else mbar_arrive(smem_u32(tmem_empty_bar + as));
                 }
             };
+            // With shared columns the first accumulator is emptied from its end, the second from its beginning, and both are handed on once no
+            // warp has shared columns left to read; a warp gets to the next tile only after all of this one, so the rest is empty in time.
+            constexpr int kRounds = (BN / 32 + kGroups - 1) / kGroups;
             bool released = false;
-            for (int col = group * 32; col < tile.count; col += 32 * kGroups) {
+#pragma unroll 1
+            for (int i = 0; i < kRounds; ++i) {
+                const int block = C::kAccStride < BN && as == 0 ? BN / 32 - 1 - (i * kGroups + group) : i * kGroups + group, col = block * 32;
+                if (col >= tile.count || col >= BN) continue;
                 uint32_t v[32];
                 tmem_ld_32x32(acc + (uint32_t)col, v);
                 tmem_ld_wait();
-                if (col + 32 * kGroups >= tile.count) {  // the last block of this warp: the accumulator is handed back
+                if (C::kAccStride < BN ? !released : col + 32 * kGroups >= tile.count) {
                     release();
                     released = true;
                 }
@@ -478,11 +484,11 @@ cudaError_t launch_typed(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, 
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
-    CUtensorMap mw = {}, mx32 = {}, mx16 = {}, ms = {}, my = {};
+    CUtensorMap mw = {}, mx = {}, mx32 = {}, mx16 = {}, ms = {}, my = {};
     if (CTAS == 2) {
         const int64_t w_tiles = (int64_t)a.E * plan.w_blocks * plan.num_kb;
         const int64_t x_tiles = (a.offsets != nullptr ? most_row_blocks(a.M, a.E) : ceil_div(a.M, kTileRows)) * plan.num_kb;
-        if (!tiles_map(&mw, a.W, w_tiles, kTileBytes / 128) || !tiles_map(&mx32, a.X, x_tiles, 32) || !tiles_map(&mx16, a.X, x_tiles, 16) ||
+        if (!tiles_map(&mw, a.W, w_tiles, kTileBytes / 128) || !tiles_map(&mx, a.X, x_tiles, kTileRows) || !tiles_map(&mx32, a.X, x_tiles, 32) || !tiles_map(&mx16, a.X, x_tiles, 16) ||
             !tiles_map(&ms, a.X, x_tiles, kScaleBytes / 128))
             return cudaErrorInvalidValue;
     }
@@ -511,7 +517,7 @@ cudaError_t launch_typed(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, 
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = CTAS == 2 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, mw, mx32, mx16, ms, my, a, plan);
+    return cudaLaunchKernelEx(&cfg, kernel, mw, mx, mx32, mx16, ms, my, a, plan);
 }
 
 template <int CTAS, int BN, int EW, bool STAGED>
@@ -536,14 +542,14 @@ cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s)
     const int64_t hit = a.E < a.M ? a.E : a.M;        // experts with tokens, at most
     const int64_t mean = ceil_div(a.M, a.E);
     const int sms = sm_count();
-    const int64_t extra = a.E > 1 ? hit : 0;  // tiles that are not full, at most
+    const int64_t extra = a.E > 1 ? hit : 0;  // tiles of tokens that are not full, at most
     // pairs once each has work
     const int64_t pairs = ceil_div(a.N, 2 * kTileRows);
-    if (mean > 128 && (ceil_div(a.M, 192)) * pairs >= sms / 2) {
-        p.tile_n = 192;
+    if (mean > 128 && ceil_div(a.M, 256) * pairs >= sms / 2) {
+        p.tile_n = 256;
         p.tiles_m = (int32_t)pairs;
-        const int64_t tiles = (ceil_div(a.M, 192) + extra) * pairs;
-        return output_aligned(a) ? launch_shape<2, 192, 16, true>(a, p, tiles, s) : launch_shape<2, 192, 16, false>(a, p, tiles, s);
+        const int64_t tiles = (ceil_div(a.M, 256) + extra) * pairs;
+        return output_aligned(a) ? launch_shape<2, 256, 16, true>(a, p, tiles, s) : launch_shape<2, 256, 16, false>(a, p, tiles, s);
     }
     // widest tile that still gives every SM one
     p.tile_n = 192;
