@@ -6,6 +6,7 @@
 // r + 64 and r + 96 that lie side by side in an atom of scales: the four bytes of each leave as one 16-byte store.
 
 #include "q8_mx4.cuh"
+#include "q8_sm100_ptx.cuh"
 
 namespace q8 {
 
@@ -21,29 +22,66 @@ enum Kind { kMatrix, kFake, kSlots1, kSlots4 };
 template <int KIND>
 constexpr int kRows = KIND == kSlots1 ? 1 : 4;
 
+// Eight values as they lie in memory: four words of two, or eight words of one.
+template <typename T>
+constexpr int kWords = sizeof(T) == 4 ? 8 : 4;
+
 // Eight values from column k0 on; those at or behind `valid` are 0.
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, int valid, bool vec, float (&v)[8])
+__device__ __forceinline__ void load8(const T *p, int valid, bool vec, uint32_t (&w)[kWords<T>])
 {
     if (vec && valid >= 8) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 a = __ldcs(reinterpret_cast<const float4 *>(p)), b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-            const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(p));
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                T h[2];
-                memcpy(h, &w[i], 4);
-                v[2 * i] = to_float(h[0]);
-                v[2 * i + 1] = to_float(h[1]);
-            }
+        for (int i = 0; i < kWords<T> / 4; ++i) {
+            const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
+            w[4 * i] = a.x; w[4 * i + 1] = a.y; w[4 * i + 2] = a.z; w[4 * i + 3] = a.w;
+        }
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = i < valid ? reinterpret_cast<const uint32_t *>(p)[i] : 0u;
+    } else {
+        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (2 * i < valid ? (uint32_t)h[2 * i] : 0u) | (2 * i + 1 < valid ? (uint32_t)h[2 * i + 1] << 16 : 0u);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(const uint32_t (&w)[kWords<T>], float (&v)[8])
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+    } else if constexpr (std::is_same<T, __half>::value) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < valid ? to_float(p[i]) : 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+}
+// The fp32 bits of max|v|; at least those of an infinity where one of the values is NaN or infinite.
+template <typename T>
+__device__ __forceinline__ uint32_t max_bits(const uint32_t (&w)[kWords<T>])
+{
+    if constexpr (sizeof(T) == 4) {
+        float m = __uint_as_float(w[0]);
+#pragma unroll
+        for (int i = 1; i < 8; ++i) asm("max.NaN.xorsign.abs.f32 %0, %0, %1;" : "+f"(m) : "f"(__uint_as_float(w[i])));
+        return __float_as_uint(m) & 0x7fffffffu;
+    } else {  // magnitudes order like their bits, two to a word
+        uint32_t m = w[0] & 0x7fff7fffu;
+#pragma unroll
+        for (int i = 1; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+        m = max(m & 0xffffu, m >> 16);
+        if constexpr (std::is_same<T, __half>::value) return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));  // (NaN stays NaN)
+        else return m << 16;
     }
 }
 
@@ -72,17 +110,20 @@ __device__ __forceinline__ void store8(T *p, int valid, bool vec, const float (&
 
 // E of the block that this lane and its three neighbours hold, and the lane's codes.  NaN becomes 0; neither NaN nor an infinity is
 // in the maximum (`odd` says that there was one).
-__device__ __forceinline__ uint32_t quantize8(float (&v)[8], uint32_t &E, bool &odd)
+template <typename T>
+__device__ __forceinline__ uint32_t quantize8(const uint32_t (&w)[kWords<T>], uint32_t &E, bool &odd)
 {
-    uint32_t top = 0;
+    float v[8];
+    unpack8<T>(w, v);
+    uint32_t top = max_bits<T>(w);
+    if (__any_sync(0xffffffffu, top >= 0x7f800000u)) {  // once more, without what is not a number
+        odd = true;
+        top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t bits = __float_as_uint(v[i]) & 0x7fffffffu;
-        if (bits >= 0x7f800000u) {
-            odd = true;
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t bits = __float_as_uint(v[i]) & 0x7fffffffu;
             if (bits > 0x7f800000u) v[i] = 0.0f;
-        } else {
-            top = max(top, bits);
+            if (bits < 0x7f800000u) top = max(top, bits);
         }
     }
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -90,8 +131,9 @@ __device__ __forceinline__ uint32_t quantize8(float (&v)[8], uint32_t &E, bool &
     const uint32_t field = top >> 23;
     E = field > 2 ? field - 2 : 0;
     const float inv = inverse_scale(E);
+    const uint64_t inv2 = ptx::pack_f32x2(inv, inv);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], inv);
+    for (int i = 0; i < 8; i += 2) ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(v[i], v[i + 1]), inv2), v[i], v[i + 1]);
     return pack_e2m1(v);
 }
 
@@ -115,12 +157,15 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     if (task >= tasks) return;
     int64_t first, row_step, end;
     int64_t chunk, block = 0;
+    int r0 = 0;
     if (KIND == kMatrix) {  // row_lanes of the 32 rows r, with r + 32, ... each, of a block of 128
         const int64_t blocks = ceil_div(a.rows, kTileRows);
-        block = task / row_lanes / chunks;
+        const int64_t line = task / chunks;
+        chunk = task - line * chunks;
+        block = line / row_lanes;
         const int64_t group = block / blocks;
-        chunk = task / row_lanes % chunks;
-        first = group * a.rows + (block - group * blocks) * kTileRows + task % row_lanes;
+        r0 = (int)(line - block * row_lanes);
+        first = group * a.rows + (block - group * blocks) * kTileRows + r0;
         end = (group + 1) * a.rows;
         row_step = 32;
     } else {
@@ -132,7 +177,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     const int64_t k0 = chunk * kChunk + lane * 8;
     const int valid = (int)max((int64_t)0, min((int64_t)8, a.K - k0));
     bool odd = false;
-    float v[R][8];
+    uint32_t v[R][kWords<T>];
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         const int64_t row = first + j * row_step;
@@ -146,14 +191,14 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
                 there = false;
             }
         }
-        load8(reinterpret_cast<const T *>(a.X) + from * a.ld + k0, there ? valid : 0, vec != 0, v[j]);
+        load8<T>(reinterpret_cast<const T *>(a.X) + from * a.ld + k0, there ? valid : 0, vec != 0, v[j]);
     }
     uint32_t words[R];
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         const int64_t row = first + j * row_step;
         uint32_t E;
-        const uint32_t codes = quantize8(v[j], E, odd);
+        const uint32_t codes = quantize8<T>(v[j], E, odd);
         if (KIND == kFake) {
             if (row < end) {
                 float back[8];
@@ -171,7 +216,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
         w |= __shfl_xor_sync(0xffffffffu, w, 8);
         words[j] = w;
         if (KIND == kMatrix) {
-            const int r = (int)(task % row_lanes) + 32 * j;
+            const int r = r0 + 32 * j;
             if (row < end) *reinterpret_cast<uint32_t *>(a.out + (block * chunks + chunk) * kTileBytes + code_place(r, lane)) = codes;
         } else if (row < end) {
             // the expert that owns the slot: the last one that starts at or before it
@@ -192,7 +237,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     }
     if constexpr (KIND == kMatrix) {
         if ((lane & 15) == 0)
-            *reinterpret_cast<uint4 *>(a.out + (block * chunks + chunk) * kTileBytes + scale_place((int)(task % row_lanes), lane >> 2)) =
+            *reinterpret_cast<uint4 *>(a.out + (block * chunks + chunk) * kTileBytes + scale_place(r0, lane >> 2)) =
                 make_uint4(words[0], words[1], words[2], words[3]);
     }
     if (a.status != nullptr) {
