@@ -137,17 +137,18 @@ __device__ __forceinline__ uint32_t quantize8(const uint32_t (&w)[kWords<T>], ui
     return pack_e2m1(v);
 }
 
+// (Rows and tasks are counted in 32 bits: with 64-bit divisions the indices took as many instructions as the arithmetic.)
 template <typename T, int KIND>
-__global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs a, int64_t tasks, int row_lanes, int vec, int vec_out)
+__global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs a, uint32_t tasks, uint32_t chunks, uint32_t row_lanes, int vec, int vec_out)
 {
     constexpr int R = kRows<KIND>;
     constexpr bool kSlots = KIND == kSlots1 || KIND == kSlots4;
+    constexpr int kRowStep = KIND == kMatrix ? 32 : 1;
     __shared__ int32_t table_words[kSlots ? 2 * (kMaxExperts + 1) : 1];
     grid_dependency_wait();
     grid_dependency_release_next(true);
     const int lane = threadIdx.x & 31;
-    const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int64_t chunks = ceil_div(a.K, kChunk);
+    const uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5);
     ExpertTable table{table_words, table_words + kMaxExperts + 1, nullptr};
     bool bad_index = false;
     if (kSlots) {
@@ -155,48 +156,58 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
         __syncthreads();
     }
     if (task >= tasks) return;
-    int64_t first, row_step, end;
-    int64_t chunk, block = 0;
-    int r0 = 0;
-    if (KIND == kMatrix) {  // row_lanes of the 32 rows r, with r + 32, ... each, of a block of 128
-        const int64_t blocks = ceil_div(a.rows, kTileRows);
-        const int64_t line = task / chunks;
-        chunk = task - line * chunks;
-        block = line / row_lanes;
-        const int64_t group = block / blocks;
-        r0 = (int)(line - block * row_lanes);
-        first = group * a.rows + (block - group * blocks) * kTileRows + r0;
-        end = (group + 1) * a.rows;
-        row_step = 32;
+    const uint32_t line = task / chunks, chunk = task - line * chunks;
+    const int32_t rows = (int32_t)a.rows;
+    int32_t first, end = rows;
+    uint8_t *tile = nullptr;
+    uint32_t r0 = 0;
+    if (KIND == kMatrix) {  // the row r0 of a block of 128, r0 < row_lanes, and those 32, 64 and 96 further
+        const uint32_t block = line / row_lanes;
+        r0 = line - block * row_lanes;
+        uint32_t in_group = block;
+        first = 0;
+        if (a.groups > 1) {
+            const uint32_t blocks = (uint32_t)(rows + kTileRows - 1) / kTileRows, group = block / blocks;
+            in_group = block - group * blocks;
+            first = (int32_t)group * rows;
+            end = first + rows;
+        }
+        first += (int32_t)(in_group * kTileRows + r0);
+        tile = a.out + ((int64_t)block * chunks + chunk) * kTileBytes;
     } else {
-        chunk = task % chunks;
-        first = task / chunks * R;
-        end = a.rows;
-        row_step = 1;
+        first = (int32_t)line * R;
     }
-    const int64_t k0 = chunk * kChunk + lane * 8;
-    const int valid = (int)max((int64_t)0, min((int64_t)8, a.K - k0));
+    const int32_t k0 = (int32_t)chunk * kChunk + lane * 8, valid = max(0, min(8, (int32_t)a.K - k0));
     bool odd = false;
     uint32_t v[R][kWords<T>];
+    if (kSlots && a.index != nullptr) {
+        int32_t from[R];
 #pragma unroll
-    for (int j = 0; j < R; ++j) {
-        const int64_t row = first + j * row_step;
-        int64_t from = row;
-        bool there = row < end;
-        if (kSlots && there && a.index != nullptr) {
-            from = __ldg(a.index + row);
-            if (from < 0 || from >= a.x_rows) {  // counts as a row of zeros
-                const bool owned = row >= table.start[0] && row < table.start[a.E];
-                bad_index |= owned;
-                there = false;
-            }
+        for (int j = 0; j < R; ++j) from[j] = first + j < end ? __ldg(a.index + first + j) : 0;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const bool there = from[j] >= 0 && from[j] < a.x_rows;  // else it counts as a row of zeros
+            if (!there && first + j >= table.start[0] && first + j < table.start[a.E]) bad_index = true;
+            load8<T>(reinterpret_cast<const T *>(a.X) + from[j] * a.ld + k0, there && first + j < end ? valid : 0, vec != 0, v[j]);
         }
-        load8<T>(reinterpret_cast<const T *>(a.X) + from * a.ld + k0, there ? valid : 0, vec != 0, v[j]);
+    } else {
+        const T *x = reinterpret_cast<const T *>(a.X) + first * a.ld + k0;
+#pragma unroll
+        for (int j = 0; j < R; ++j, x += kRowStep * a.ld) load8<T>(x, first + j * kRowStep < end ? valid : 0, vec != 0, v[j]);
     }
     uint32_t words[R];
+    int expert = 0;
+    if (kSlots) {  // the expert that owns the first slot: the last one that starts at or before it
+        int hi = a.E;
+        while (expert < hi) {
+            const int mid = (expert + hi) >> 1;
+            if (table.start[mid + 1] <= first) expert = mid + 1;
+            else hi = mid;
+        }
+    }
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-        const int64_t row = first + j * row_step;
+        const int32_t row = first + j * kRowStep;
         uint32_t E;
         const uint32_t codes = quantize8<T>(v[j], E, odd);
         if (KIND == kFake) {
@@ -216,29 +227,19 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
         w |= __shfl_xor_sync(0xffffffffu, w, 8);
         words[j] = w;
         if (KIND == kMatrix) {
-            const int r = r0 + 32 * j;
-            if (row < end) *reinterpret_cast<uint32_t *>(a.out + (block * chunks + chunk) * kTileBytes + code_place(r, lane)) = codes;
+            if (row < end) *reinterpret_cast<uint32_t *>(tile + code_place((int)r0, lane) + 32 * 128 * j) = codes;
         } else if (row < end) {
-            // the expert that owns the slot: the last one that starts at or before it
-            int lo = 0, hi = a.E;
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (table.start[mid + 1] <= row) lo = mid + 1;
-                else hi = mid;
-            }
-            if (lo < a.E && row >= table.start[lo]) {
-                const int64_t in_expert = row - table.start[lo];
-                const int r = (int)(in_expert % kTileRows);
-                uint8_t *tile = a.out + ((table.block[lo] + in_expert / kTileRows) * chunks + chunk) * kTileBytes;
-                *reinterpret_cast<uint32_t *>(tile + code_place(r, lane)) = codes;
-                if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(tile + scale_place(r, lane >> 2)) = w;
+            while (expert < a.E && table.start[expert + 1] <= row) ++expert;
+            if (expert < a.E && row >= table.start[expert]) {
+                const uint32_t in_expert = (uint32_t)(row - table.start[expert]), r = in_expert % kTileRows;
+                uint8_t *t = a.out + ((int64_t)(table.block[expert] + in_expert / kTileRows) * chunks + chunk) * kTileBytes;
+                *reinterpret_cast<uint32_t *>(t + code_place((int)r, lane)) = codes;
+                if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(t + scale_place((int)r, lane >> 2)) = w;
             }
         }
     }
     if constexpr (KIND == kMatrix) {
-        if ((lane & 15) == 0)
-            *reinterpret_cast<uint4 *>(a.out + (block * chunks + chunk) * kTileBytes + scale_place(r0, lane >> 2)) =
-                make_uint4(words[0], words[1], words[2], words[3]);
+        if ((lane & 15) == 0) *reinterpret_cast<uint4 *>(tile + scale_place((int)r0, lane >> 2)) = make_uint4(words[0], words[1], words[2], words[3]);
     }
     if (a.status != nullptr) {
         const uint32_t flags = (odd ? 1u << Q8_ERR_SCALE : 0u) | (bad_index ? 1u << Q8_ERR_INDEX : 0u);
@@ -248,37 +249,35 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-mx4_dequantize_kernel(const uint8_t *tiles, int64_t groups, int64_t rows, int64_t K, T *Y, int64_t ldy, int64_t tasks, int vec)
+mx4_dequantize_kernel(const uint8_t *tiles, uint32_t groups, uint32_t rows, int32_t K, T *Y, int64_t ldy, uint32_t tasks, uint32_t chunks, int vec)
 {
     grid_dependency_wait();
     const int lane = threadIdx.x & 31;
-    const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5);
     if (task >= tasks) return;
-    const int64_t chunks = ceil_div(K, kChunk), chunk = task % chunks, first = task / chunks * 4;
-    const int64_t k0 = chunk * kChunk + lane * 8;
+    const uint32_t line = task / chunks, chunk = task - line * chunks, first = line * 4, all = groups * rows;
+    const int32_t k0 = (int32_t)chunk * kChunk + lane * 8;
     if (k0 >= K) return;
-    const int valid = (int)min((int64_t)8, K - k0);
-    const int64_t blocks = ceil_div(rows, kTileRows);
+    const int valid = min(8, K - k0);
+    const uint32_t blocks = (rows + kTileRows - 1) / kTileRows;
     uint32_t c[4], E[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t row = first + j;
-        c[j] = E[j] = 0;
-        if (row >= groups * rows) continue;
-        const int64_t group = row / rows, r = row - group * rows;
-        const uint8_t *tile = tiles + ((group * blocks + r / kTileRows) * chunks + chunk) * kTileBytes;
+    for (uint32_t j = 0; j < 4; ++j) {
+        const uint32_t row = min(first + j, all - 1), group = groups > 1 ? row / rows : 0, r = row - group * rows;
+        const uint8_t *tile = tiles + ((int64_t)(group * blocks + r / kTileRows) * chunks + chunk) * kTileBytes;
         c[j] = __ldg(reinterpret_cast<const uint32_t *>(tile + code_place((int)(r % kTileRows), lane)));
         E[j] = __ldg(tile + scale_place((int)(r % kTileRows), lane >> 2));
     }
+    T *y = Y + first * ldy + k0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (first + j >= groups * rows) continue;
+    for (uint32_t j = 0; j < 4; ++j, y += ldy) {
+        if (first + j >= all) break;
         float v[8];
         unpack_e2m1(c[j], v);
         const float s = E[j] == 255 ? __uint_as_float(0x7fc00000u) : scale_value(E[j]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], s);
-        store8(Y + (first + j) * ldy + k0, valid, vec != 0, v);
+        store8(y, valid, vec != 0, v);
     }
 }
 
@@ -286,23 +285,21 @@ bool rows_aligned(const void *p, int64_t ld, int size) { return reinterpret_cast
 
 cudaError_t grid_of(int64_t tasks, dim3 *grid)
 {
-    const int64_t ctas = ceil_div(tasks, kWarps);
-    if (ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    *grid = dim3((unsigned)ctas);
+    if (tasks > 0x7fffffff) return cudaErrorInvalidConfiguration;  // more than 2^41 values
+    *grid = dim3((unsigned)ceil_div(tasks, kWarps));
     return cudaSuccess;
 }
 
 template <typename T, int KIND>
 cudaError_t launch_kind(const Mx4QuantizeArgs &a, cudaStream_t s)
 {
-    const int64_t chunks = ceil_div(a.K, kChunk);
-    const int row_lanes = (int)(a.rows < 32 ? a.rows : 32);
-    const int64_t tasks = KIND == kMatrix ? a.groups * ceil_div(a.rows, kTileRows) * chunks * row_lanes : ceil_div(a.rows, kRows<KIND>) * chunks;
+    const int64_t chunks = ceil_div(a.K, kChunk), row_lanes = a.rows < 32 ? a.rows : 32;
+    const int64_t tasks = (KIND == kMatrix ? a.groups * ceil_div(a.rows, kTileRows) * row_lanes : ceil_div(a.rows, kRows<KIND>)) * chunks;
     dim3 grid;
     cudaError_t e = grid_of(tasks, &grid);
     if (e != cudaSuccess) return e;
-    return launch_overlapping_tail(mx4_quantize_kernel<T, KIND>, grid, dim3(kThreads), 0, s, a, tasks, row_lanes,
-                                   (int)rows_aligned(a.X, a.ld, sizeof(T)), (int)rows_aligned(a.Xhat, a.ldo, sizeof(T)));
+    return launch_overlapping_tail(mx4_quantize_kernel<T, KIND>, grid, dim3(kThreads), 0, s, a, tasks, chunks, row_lanes,
+                                   rows_aligned(a.X, a.ld, sizeof(T)), rows_aligned(a.Xhat, a.ldo, sizeof(T)));
 }
 
 template <typename T>
@@ -329,15 +326,15 @@ cudaError_t launch_mx4_quantize(const Mx4QuantizeArgs &a, int dtype, cudaStream_
 cudaError_t launch_mx4_dequantize(const uint8_t *tiles, int64_t groups, int64_t rows, int64_t K, void *Y, int dtype, int64_t ldy, cudaStream_t s)
 {
     last_launch_info().launches += 1;
-    const int64_t tasks = ceil_div(groups * rows, 4) * ceil_div(K, kChunk);
+    const int64_t chunks = ceil_div(K, kChunk), tasks = ceil_div(groups * rows, 4) * chunks;
     dim3 grid;
     cudaError_t e = grid_of(tasks, &grid);
     if (e != cudaSuccess) return e;
-    const int vec = rows_aligned(Y, ldy, dtype == Q8_F32 ? 4 : 2);
+    const bool vec = rows_aligned(Y, ldy, dtype == Q8_F32 ? 4 : 2);
     switch (dtype) {
-        case Q8_F32: return launch_overlapping_tail(mx4_dequantize_kernel<float>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<float *>(Y), ldy, tasks, vec);
-        case Q8_F16: return launch_overlapping_tail(mx4_dequantize_kernel<__half>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<__half *>(Y), ldy, tasks, vec);
-        default: return launch_overlapping_tail(mx4_dequantize_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<__nv_bfloat16 *>(Y), ldy, tasks, vec);
+        case Q8_F32: return launch_overlapping_tail(mx4_dequantize_kernel<float>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<float *>(Y), ldy, tasks, chunks, vec);
+        case Q8_F16: return launch_overlapping_tail(mx4_dequantize_kernel<__half>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<__half *>(Y), ldy, tasks, chunks, vec);
+        default: return launch_overlapping_tail(mx4_dequantize_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<__nv_bfloat16 *>(Y), ldy, tasks, chunks, vec);
     }
 }
 
