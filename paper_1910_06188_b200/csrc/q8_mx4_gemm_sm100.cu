@@ -114,30 +114,35 @@ struct Plan {
 struct Tile {
     int32_t expert, first, row, count, feature;
 };
-// Tiles in rising order, those of an expert features first.  A warp looks at 32 experts at a time.
+// Tile t, those of an expert ordered features first; false behind the last one.
 template <int TILE_M>
-struct TileWalk {
-    int32_t base = 0;  // the batch of experts that the last tile was found in
-    __device__ __forceinline__ bool find(int32_t t, const ExpertTable &table, int E, const Plan &p, Tile &out)
-    {
-        const int lane = threadIdx.x & 31;
-        if (t >= table.tile[E]) return false;
-        while (true) {
-            const uint32_t past = __ballot_sync(0xffffffffu, base + lane < E && table.tile[min(base + lane + 1, E)] > t);
-            if (past != 0) {
-                const int e = base + __ffs(past) - 1;
-                const int32_t local = t - table.tile[e], n = local / p.tiles_m;
-                out.expert = e;
-                out.first = n * p.tile_n;
-                out.row = table.start[e] + out.first;
-                out.count = min(p.tile_n, table.start[e + 1] - out.row);
-                out.feature = (local - n * p.tiles_m) * TILE_M;
-                return true;
-            }
-            base += 32;
-        }
+__device__ __forceinline__ bool find_tile(int32_t t, const ExpertTable &table, int E, const Plan &p, Tile &out)
+{
+    if (t >= table.tile[E]) return false;
+    int e = 0, hi = E - 1;  // the last expert whose tiles begin at or before t: those without tokens have none
+    while (e < hi) {
+        const int mid = (e + hi + 1) >> 1;
+        if (table.tile[mid] <= t) e = mid;
+        else hi = mid - 1;
     }
-};
+    const uint32_t local = (uint32_t)(t - table.tile[e]), n = local / (uint32_t)p.tiles_m;
+    out.expert = e;
+    out.first = (int32_t)n * p.tile_n;
+    out.row = table.start[e] + out.first;
+    out.count = min(p.tile_n, table.start[e + 1] - out.row);
+    out.feature = (int32_t)(local - n * p.tiles_m) * TILE_M;
+    return true;
+}
+
+// Bounded wait whose first try is in line.
+__device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status)
+{
+    return mbar_wait(bar, parity, abort_flag, status);
+}
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status)
+{
+    return mbar_try_wait(bar, parity) || wait_on(bar, parity, abort_flag, status);
+}
 
 template <int CTAS, int BN, int EW, bool STAGED, typename T>
 __global__ void __launch_bounds__(96 + 32 * EW, 1)
@@ -200,7 +205,6 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     grid_dependency_release_next(true);
 
     const int32_t first_tile = blockIdx.x / CTAS, tile_step = gridDim.x / CTAS;
-    TileWalk<TILE_M> walk;
     Tile tile;
     auto width_of = [&](const Tile &t) { return (t.count + kStep - 1) / kStep * kStep; };
     if (warp == 0 || warp == 2) {
@@ -209,25 +213,25 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         // bytes: 136 of them to a tile, the last 8 its scales.
         const bool weights = warp == 0;
         if (!weights || CTAS == 2) grid_dependency_wait();  // (a pair's weight producer loads token scales too)
-        const uint32_t elected = elect_one();
-        int s = 0;
-        uint32_t phase = 0;
-        int64_t issued = 0;
-        bool ok = true;
-        for (int32_t t = first_tile; ok && walk.find(t, table, a.E, plan, tile); t += tile_step) {
-            const int width = width_of(tile), mine = width / CTAS;
-            const int64_t w_tile = ((int64_t)tile.expert * plan.w_blocks + tile.feature / kTileRows + rank) * plan.num_kb;
-            const int first = tile.first + (int)rank * mine, sub = first % kTileRows;
-            const int64_t x_tile = ((int64_t)table.block[tile.expert] + first / kTileRows) * plan.num_kb;
-            const int64_t s_tile = ((int64_t)table.block[tile.expert] + tile.first / kTileRows) * plan.num_kb;
-            const bool two_scales = tile.first % kTileRows + width > kTileRows;  // the tile's tokens lie in two row blocks
-            const int in_first = min(mine, kTileRows - sub);                     // of this CTA's tokens, those in the first row block
-            const uint32_t bytes = CTAS == 1 ? (weights ? kTileBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 2 : 1))
-                                             : 2 * (weights ? kTileBytes + kScaleBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 1 : 0));
-            for (int kb = 0; kb < plan.num_kb; ++kb) {
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(empty_bar + s), phase ^ 1u, abort_flag, a.status));
-                if (!ok) break;
-                if (elected) {
+        // One lane does all of it: a warp that waits together and then lets one lane issue takes 500 cycles a stage, more than the products.
+        if (elect_one()) {
+            int s = 0;
+            uint32_t phase = 0;
+            int64_t issued = 0;
+            bool ok = true;
+            for (int32_t t = first_tile; ok && find_tile<TILE_M>(t, table, a.E, plan, tile); t += tile_step) {
+                const int width = width_of(tile), mine = width / CTAS;
+                const int64_t w_tile = ((int64_t)tile.expert * plan.w_blocks + tile.feature / kTileRows + rank) * plan.num_kb;
+                const int first = tile.first + (int)rank * mine, sub = first % kTileRows;
+                const int64_t x_tile = ((int64_t)table.block[tile.expert] + first / kTileRows) * plan.num_kb;
+                const int64_t s_tile = ((int64_t)table.block[tile.expert] + tile.first / kTileRows) * plan.num_kb;
+                const bool two_scales = tile.first % kTileRows + width > kTileRows;  // the tile's tokens lie in two row blocks
+                const int in_first = min(mine, kTileRows - sub);                     // of this CTA's tokens, those in the first row block
+                const uint32_t bytes = CTAS == 1 ? (weights ? kTileBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 2 : 1))
+                                                 : 2 * (weights ? kTileBytes + kScaleBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 1 : 0));
+                for (int kb = 0; kb < plan.num_kb; ++kb) {
+                    ok = wait_for(smem_u32(empty_bar + s), phase ^ 1u, abort_flag, a.status);
+                    if (!ok) break;
                     const uint32_t fb = smem_u32(full_bar + s);
                     const uint32_t dst_b = smem_u32(smem_b + s * C::kBBytes), dst_s = smem_u32(smem_sb + s * C::kSbBytes);
                     if constexpr (CTAS == 1) {
@@ -264,30 +268,27 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                                 tma_load_2d_pair(dst_s + kScaleBytes, &map_s, 0, (int32_t)(s_tile + kb + plan.num_kb) * kRowsPerTile + kTileRows, fb_leader);
                         }
                     }
+                    ++issued;
+                    if (++s == C::kStages) { s = 0; phase ^= 1u; }
                 }
-                __syncwarp();
-                ++issued;
-                if (++s == C::kStages) { s = 0; phase ^= 1u; }
             }
-        }
-        if (!ok) {
-            // Aborting: this warp's copies land before the CTA gives up its shared memory (bounded: the other producer may have stopped
-            // a stage earlier, and its barrier then never completes).
-            const uint64_t t0 = global_timer_ns();
-            if (leader) {
-                for (int64_t i = 1; i <= (issued < C::kStages ? issued : C::kStages); ++i) {
-                    const int64_t k = issued - i;
-                    while (!mbar_try_wait(smem_u32(full_bar + k % C::kStages), (uint32_t)(k / C::kStages) & 1u) && global_timer_ns() - t0 < 50000000ull) {}
+            if (!ok) {
+                // Aborting: this warp's copies land before the CTA gives up its shared memory (bounded: the other producer may have stopped
+                // a stage earlier, and its barrier then never completes).
+                const uint64_t t0 = global_timer_ns();
+                if (leader) {
+                    for (int64_t i = 1; i <= (issued < C::kStages ? issued : C::kStages); ++i) {
+                        const int64_t k = issued - i;
+                        while (!mbar_try_wait(smem_u32(full_bar + k % C::kStages), (uint32_t)(k / C::kStages) & 1u) && global_timer_ns() - t0 < 50000000ull) {}
+                    }
+                } else {
+                    while (global_timer_ns() - t0 < 1000000ull) {}  // the peer cannot poll the leader's barrier
                 }
-            } else {
-                while (global_timer_ns() - t0 < 1000000ull) {}  // the peer cannot poll the leader's barrier
             }
         }
     } else if (warp == 1) {
         // ---------------- MMA issuer (the leader's drives the pair) ----------------
-        if (leader) {
-            const uint32_t elected = elect_one();
-            auto uniform = [&](bool mine) { return (bool)__all_sync(0xffffffffu, mine); };
+        if (leader && elect_one()) {
             auto commit = [&](uint64_t *bar) {
                 if (CTAS == 2) umma_commit_pair(smem_u32(bar));
                 else umma_commit(smem_u32(bar));
@@ -296,10 +297,10 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             uint32_t phase = 0, aphase = 0;
             uint32_t scale_buffer = 0;
             bool ok = true;
-            for (int32_t t = first_tile; ok && walk.find(t, table, a.E, plan, tile); t += tile_step) {
+            for (int32_t t = first_tile; ok && find_tile<TILE_M>(t, table, a.E, plan, tile); t += tile_step) {
                 // the tile before last has left this accumulator, or the last one the columns that it shares with it
                 constexpr bool kShared = C::kAccStride < BN;
-                ok = uniform(mbar_wait(smem_u32(tmem_empty_bar + (kShared ? as ^ 1 : as)), kShared && as == 1 ? aphase : aphase ^ 1u, abort_flag, a.status));
+                ok = wait_for(smem_u32(tmem_empty_bar + (kShared ? as ^ 1 : as)), kShared && as == 1 ? aphase : aphase ^ 1u, abort_flag, a.status);
                 if (!ok) break;
                 tc_fence_after();
                 const int width = width_of(tile);
@@ -308,7 +309,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 const int sub = tile.first % kTileRows;  // a multiple of 32
                 const bool two_blocks = sub + width > kTileRows;
                 for (int kb = 0; kb < plan.num_kb; ++kb) {
-                    ok = uniform(mbar_wait(smem_u32(full_bar + s), phase, abort_flag, a.status));
+                    ok = wait_for(smem_u32(full_bar + s), phase, abort_flag, a.status);
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t a_addr = smem_u32(smem_a + s * kTileBytes);
@@ -318,25 +319,22 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                     const uint32_t sa_col = tmem_base + (uint32_t)(C::kScaleCol0) + scale_buffer, sb_col = sa_col + 8;
                     scale_buffer = scale_buffer == 0 ? kScaleCols : 0;
                     const int blocks = min(kTileK / kBlock, plan.k_blocks - kb * (kTileK / kBlock));
-                    if (elected) {
 #pragma unroll
-                        for (int atom = 0; atom < 2; ++atom) {
-                            if (4 * atom >= blocks) break;
-                            copy_scales<CTAS>(sa_col + 4 * atom, dsa + (uint64_t)(atom * (kAtomBytes >> 4)));
-                            copy_scales<CTAS>(sb_col + 8 * atom, dsb + (uint64_t)(atom * (kAtomBytes >> 4)));
-                            if (two_blocks) copy_scales<CTAS>(sb_col + 8 * atom + 4, dsb + (uint64_t)((2 + atom) * (kAtomBytes >> 4)));
-                        }
-#pragma unroll
-                        for (int k = 0; k < kTileK / kMmaK; ++k) {
-                            if (2 * k >= blocks) break;
-                            const uint32_t half = (uint32_t)(k & 1) * 2;  // blocks 0 and 1 or 2 and 3 of the atom
-                            mma_mxf4<CTAS>(tmem_d, da + (uint64_t)(2 * k), db + (uint64_t)(2 * k), idesc | (half << 4) | (half << 29), sa_col + 4 * (k >> 1),
-                                           sb_col + 8 * (k >> 1) + (uint32_t)(sub >> 5), (uint32_t)((kb | k) != 0));
-                        }
-                        commit(empty_bar + s);
-                        if (kb + 1 == plan.num_kb) commit(tmem_full_bar + as);
+                    for (int atom = 0; atom < 2; ++atom) {
+                        if (4 * atom >= blocks) break;
+                        copy_scales<CTAS>(sa_col + 4 * atom, dsa + (uint64_t)(atom * (kAtomBytes >> 4)));
+                        copy_scales<CTAS>(sb_col + 8 * atom, dsb + (uint64_t)(atom * (kAtomBytes >> 4)));
+                        if (two_blocks) copy_scales<CTAS>(sb_col + 8 * atom + 4, dsb + (uint64_t)((2 + atom) * (kAtomBytes >> 4)));
                     }
-                    __syncwarp();
+#pragma unroll
+                    for (int k = 0; k < kTileK / kMmaK; ++k) {
+                        if (2 * k >= blocks) break;
+                        const uint32_t half = (uint32_t)(k & 1) * 2;  // blocks 0 and 1 or 2 and 3 of the atom
+                        mma_mxf4<CTAS>(tmem_d, da + (uint64_t)(2 * k), db + (uint64_t)(2 * k), idesc | (half << 4) | (half << 29), sa_col + 4 * (k >> 1),
+                                       sb_col + 8 * (k >> 1) + (uint32_t)(sub >> 5), (uint32_t)((kb | k) != 0));
+                    }
+                    commit(empty_bar + s);
+                    if (kb + 1 == plan.num_kb) commit(tmem_full_bar + as);
                     if (++s == C::kStages) { s = 0; phase ^= 1u; }
                 }
                 if (!ok) break;
@@ -344,8 +342,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             }
             if (!ok) {
                 // Aborting: wait (bounded) for the tensor core to finish what was issued.
-                if (elected) commit(drain_bar);
-                __syncwarp();
+                commit(drain_bar);
                 const uint64_t t0 = global_timer_ns();
                 while (!mbar_try_wait(smem_u32(drain_bar), 0) && global_timer_ns() - t0 < 50000000ull) {}
             }
@@ -360,11 +357,11 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         int as = 0;
         uint32_t aphase = 0;
         grid_dependency_wait();  // before anything is written: an earlier kernel may still read Y
-        for (int32_t t = first_tile; walk.find(t, table, a.E, plan, tile); t += tile_step) {
+        for (int32_t t = first_tile; find_tile<TILE_M>(t, table, a.E, plan, tile); t += tile_step) {
             const int feature0 = tile.feature + (int)rank * kTileRows + quarter * 32, feature = feature0 + lane;
             const bool mine = feature < a.N;
             const float bias = mine && a.bias != nullptr ? __ldg(a.bias + (int64_t)tile.expert * a.N + feature) : 0.0f;
-            const bool ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(tmem_full_bar + as), aphase, abort_flag, a.status));
+            const bool ok = __all_sync(0xffffffffu, wait_for(smem_u32(tmem_full_bar + as), aphase, abort_flag, a.status));
             if (!ok) break;
             tc_fence_after();
             const uint32_t acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(as * C::kAccStride);
@@ -431,6 +428,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     }
 
     // ---------------- teardown (reached by every thread, also when aborting) ----------------
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (CTAS == 2) {
