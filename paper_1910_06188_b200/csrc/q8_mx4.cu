@@ -154,6 +154,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     constexpr bool kSlots = KIND == kSlots1 || KIND == kSlots4;
     constexpr int kRowStep = KIND == kMatrix ? 32 : 1;
     __shared__ int32_t table_words[kSlots ? 2 * (kMaxExperts + 1) : 1];
+    // The product behind this pass reads weights and offsets at once, so it starts when everything before this kernel has ended.
     grid_dependency_wait();
     grid_dependency_release_next(true);
     const int lane = threadIdx.x & 31;

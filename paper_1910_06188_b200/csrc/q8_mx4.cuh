@@ -184,7 +184,7 @@ struct Mx4GemmArgs {
     const int32_t *offsets = nullptr;  // [E + 1], or nullptr with E == 1
     int E = 1;
     int32_t *status;
-    bool weights_early = false;  // the kernel before this one in the stream waited for all before it and writes neither weights nor offsets
+    bool behind_quantise = false;  // the kernel before this one in the stream is the quantise pass of the same call
 };
 cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s);
 

@@ -175,7 +175,7 @@ q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *
     g.act = act;
     g.E = 1;
     g.status = dev_status;
-    g.weights_early = true;
+    g.behind_quantise = true;
     return cuda_status(launch_mx4_gemm(g, s));
 }
 
@@ -224,7 +224,7 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
     g.offsets = offsets;
     g.E = (int)experts;
     g.status = dev_status;
-    g.weights_early = true;
+    g.behind_quantise = true;
     return cuda_status(launch_mx4_gemm(g, s));
 }
 

@@ -31,7 +31,6 @@ using namespace mx4;
 using gemm_detail::encode_tiled_fn;
 using gemm_detail::gelu_fast_x2;
 
-constexpr int kMmaK = 64;
 constexpr int kAccStages = 2;
 constexpr int kScaleBytes = 2 * kAtomBytes;  // of a tile
 constexpr int kScaleCols = 4 * 2 + 8 * 2;    // TMEM columns of a stage's scales: 128 weight rows, 256 token rows, two atoms each
@@ -61,33 +60,43 @@ struct Cfg {
     static constexpr uint32_t kInstrDesc = (1u << 7) | (1u << 10) | (1u << 23) | ((uint32_t)CTAS << 27);
 };
 
-// The instructions below are issued by one elected lane.
+// The instructions below are issued by one elected lane.  Descriptors of shared memory are given by their lower words, in which the
+// address (in units of 16 bytes) is the only part that changes; what is constant is put together in line.
+constexpr uint32_t kOperandHigh = (1024 >> 4) | (1u << 14) | (2u << 29);  // K-major, 128-byte swizzle, 8-row groups 1024 bytes apart
+constexpr uint32_t kScalesHigh = (128 >> 4) | (1u << 14);                 // no swizzle, groups of 8 rows of 16 bytes 128 bytes apart
+__device__ __forceinline__ uint32_t operand_low(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t scales_low(uint32_t saddr) { return (saddr & 0x3FFFFu) >> 4; }
+
 template <int CTAS>
-__device__ __forceinline__ void mma_mxf4(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t tmem_sa, uint32_t tmem_sb,
+__device__ __forceinline__ void mma_mxf4(uint32_t tmem_d, uint32_t a_low, uint32_t b_low, uint32_t idesc, uint32_t tmem_sa, uint32_t tmem_sb,
                                          uint32_t accumulate)
 {
     if constexpr (CTAS == 2)
         asm volatile(
-            "{\n\t.reg .pred p;\n\t"
+            "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
             "setp.ne.b32 p, %6, 0;\n\t"
-            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate)
+            "mov.b64 da, {%1, %7};\n\tmov.b64 db, {%2, %7};\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %3, [%4], [%5], p;\n\t}"
+            ::"r"(tmem_d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate), "n"(kOperandHigh)
             : "memory");
     else
         asm volatile(
-            "{\n\t.reg .pred p;\n\t"
+            "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
             "setp.ne.b32 p, %6, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate)
+            "mov.b64 da, {%1, %7};\n\tmov.b64 db, {%2, %7};\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], da, db, %3, [%4], [%5], p;\n\t}"
+            ::"r"(tmem_d), "r"(a_low), "r"(b_low), "r"(idesc), "r"(tmem_sa), "r"(tmem_sb), "r"(accumulate), "n"(kOperandHigh)
             : "memory");
 }
 // 512 bytes of shared memory (32 lanes x 16 bytes) to four columns of each of the four lane quarters; with CTAS = 2 in both CTAs, each from
 // its own shared memory
 template <int CTAS>
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc)
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t low)
 {
-    if constexpr (CTAS == 2) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
-    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    if constexpr (CTAS == 2)
+        asm volatile("{\n\t.reg .b64 d;\n\tmov.b64 d, {%1, %2};\n\ttcgen05.cp.cta_group::2.32x128b.warpx4 [%0], d;\n\t}" ::"r"(tmem), "r"(low), "n"(kScalesHigh) : "memory");
+    else
+        asm volatile("{\n\t.reg .b64 d;\n\tmov.b64 d, {%1, %2};\n\ttcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n\t}" ::"r"(tmem), "r"(low), "n"(kScalesHigh) : "memory");
 }
 // Untiled copy global -> shared; both 16-byte aligned, bytes a multiple of 16.
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
@@ -96,12 +105,6 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
                  : "memory");
 }
-// An atom of scales in shared memory: no swizzle, 8 rows of 16 bytes contiguous, 128 bytes from one group of 8 to the next.
-__device__ __forceinline__ uint64_t scale_desc(uint32_t saddr)
-{
-    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
-}
-
 struct Plan {
     int32_t tile_n;    // tokens of a full tile
     int32_t tiles_m;   // tiles of features
@@ -190,9 +193,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         if (CTAS == 2) tmem_alloc_pair(smem_u32(tmem_slot), C::kTmemCols);
         else tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
     }
-    // Offsets and weights are there already when the kernel before this one is the quantise pass of the same call; else that
-    // kernel may have written them.
-    if (!a.weights_early) grid_dependency_wait();
+    // (The offsets may be read at once, see below.)
     if (warp == 2) {
         const bool bad = build_expert_table(table, a.offsets, a.E, (int32_t)a.M, plan.tile_n, plan.tiles_m);
         if (bad && lane == 0 && blockIdx.x == 0 && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_INDEX);
@@ -212,13 +213,16 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         // A pair's loads all report to the leader's barrier, which its MMA warp waits on.  The tensor maps of the pair see tiles as rows of 128
         // bytes: 136 of them to a tile, the last 8 its scales.
         const bool weights = warp == 0;
-        if (!weights || CTAS == 2) grid_dependency_wait();  // (a pair's weight producer loads token scales too)
+        // A quantise pass of the same call has waited for all kernels before it when this one starts, and writes neither weights nor
+        // offsets, so these may be read before it ends: as much as the ring holds.  (Asking for the rest into L2 as well holds up the loads behind it:
+        // 24 x 4096 -> 16384 9.9 -> 10.6 us, 32 slots on 64 experts 9.5 -> 12.)
+        const bool early = CTAS == 1 && a.behind_quantise;
         // One lane does all of it: a warp that waits together and then lets one lane issue takes 500 cycles a stage, more than the products.
         if (elect_one()) {
             int s = 0;
             uint32_t phase = 0;
             int64_t issued = 0;
-            bool ok = true;
+            bool ok = true, waited = false;
             for (int32_t t = first_tile; ok && find_tile<TILE_M>(t, table, a.E, plan, tile); t += tile_step) {
                 const int width = width_of(tile), mine = width / CTAS;
                 const int64_t w_tile = ((int64_t)tile.expert * plan.w_blocks + tile.feature / kTileRows + rank) * plan.num_kb;
@@ -229,22 +233,30 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 const int in_first = min(mine, kTileRows - sub);                     // of this CTA's tokens, those in the first row block
                 const uint32_t bytes = CTAS == 1 ? (weights ? kTileBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 2 : 1))
                                                  : 2 * (weights ? kTileBytes + kScaleBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 1 : 0));
+                if (!waited && !(weights && early)) grid_dependency_wait();
+                waited = true;
+                const uint8_t *w = a.W + w_tile * kTileBytes, *x = a.X + x_tile * kTileBytes, *xs = a.X + s_tile * kTileBytes + kCodeBytes;
+                const int64_t next_block = (int64_t)plan.num_kb * kTileBytes;
+                bool ready = mbar_try_wait(smem_u32(empty_bar + s), phase ^ 1u);
                 for (int kb = 0; kb < plan.num_kb; ++kb) {
-                    ok = wait_for(smem_u32(empty_bar + s), phase ^ 1u, abort_flag, a.status);
+                    ok = ready || wait_on(smem_u32(empty_bar + s), phase ^ 1u, abort_flag, a.status);
                     if (!ok) break;
+                    const int s_next = s + 1 == C::kStages ? 0 : s + 1;
+                    ready = mbar_try_wait(smem_u32(empty_bar + s_next), phase ^ (s_next == 0 ? 0u : 1u));  // (its answer is there by the time it is needed)
                     const uint32_t fb = smem_u32(full_bar + s);
                     const uint32_t dst_b = smem_u32(smem_b + s * C::kBBytes), dst_s = smem_u32(smem_sb + s * C::kSbBytes);
                     if constexpr (CTAS == 1) {
                         mbar_expect_tx(fb, bytes);
                         if (weights) {
-                            bulk_load(smem_u32(smem_a + s * kTileBytes), a.W + (w_tile + kb) * kTileBytes, kTileBytes, fb);
+                            bulk_load(smem_u32(smem_a + s * kTileBytes), w, kTileBytes, fb);
+                            w += kTileBytes;
                         } else {
-                            const uint8_t *x = a.X + (x_tile + kb) * kTileBytes, *xs = a.X + (s_tile + kb) * kTileBytes + kCodeBytes;
-                            const int64_t next_block = (int64_t)plan.num_kb * kTileBytes;
                             bulk_load(dst_b, x + sub * 128, (uint32_t)in_first * 128, fb);
                             if (in_first < mine) bulk_load(dst_b + in_first * 128, x + next_block, (uint32_t)(mine - in_first) * 128, fb);
                             bulk_load(dst_s, xs, kScaleBytes, fb);
                             if (two_scales) bulk_load(dst_s + kScaleBytes, xs + next_block, kScaleBytes, fb);
+                            x += kTileBytes;
+                            xs += kTileBytes;
                         }
                     } else {
                         if (leader) mbar_expect_tx(fb, bytes);
@@ -269,7 +281,8 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                         }
                     }
                     ++issued;
-                    if (++s == C::kStages) { s = 0; phase ^= 1u; }
+                    s = s_next;
+                    if (s == 0) phase ^= 1u;
                 }
             }
             if (!ok) {
@@ -295,7 +308,11 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             };
             int s = 0, as = 0;
             uint32_t phase = 0, aphase = 0;
-            uint32_t scale_buffer = 0;
+            const uint32_t a0 = operand_low(smem_u32(smem_a)), b0 = operand_low(smem_u32(smem_b));
+            const uint32_t sa0 = scales_low(smem_u32(smem_a + kCodeBytes)), sb0 = scales_low(smem_u32(smem_sb));
+            uint32_t scale_col = tmem_base + C::kScaleCol0;
+            const uint32_t scale_sum = 2 * scale_col + kScaleCols;
+            const int last_blocks = plan.k_blocks - (plan.num_kb - 1) * (kTileK / kBlock);  // of the last stage
             bool ok = true;
             for (int32_t t = first_tile; ok && find_tile<TILE_M>(t, table, a.E, plan, tile); t += tile_step) {
                 // the tile before last has left this accumulator, or the last one the columns that it shares with it
@@ -307,35 +324,49 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 const uint32_t tmem_d = tmem_base + (uint32_t)(as * C::kAccStride);
                 const uint32_t idesc = C::kInstrDesc | ((uint32_t)(width >> 3) << 17);
                 const int sub = tile.first % kTileRows;  // a multiple of 32
+                const uint32_t sub_col = (uint32_t)sub >> 5;
                 const bool two_blocks = sub + width > kTileRows;
+                bool ready = mbar_try_wait(smem_u32(full_bar + s), phase);
                 for (int kb = 0; kb < plan.num_kb; ++kb) {
-                    ok = wait_for(smem_u32(full_bar + s), phase, abort_flag, a.status);
+                    ok = ready || wait_on(smem_u32(full_bar + s), phase, abort_flag, a.status);
                     if (!ok) break;
+                    const int s_next = s + 1 == C::kStages ? 0 : s + 1;
+                    ready = mbar_try_wait(smem_u32(full_bar + s_next), phase ^ (s_next == 0 ? 1u : 0u));
                     tc_fence_after();
-                    const uint32_t a_addr = smem_u32(smem_a + s * kTileBytes);
-                    const uint64_t da = smem_desc_sw128(a_addr), db = smem_desc_sw128(smem_u32(smem_b + s * C::kBBytes));
-                    const uint64_t dsa = scale_desc(a_addr + kCodeBytes), dsb = scale_desc(smem_u32(smem_sb + s * C::kSbBytes));
+                    const uint32_t da = a0 + (uint32_t)s * (kTileBytes >> 4), db = b0 + (uint32_t)s * (C::kBBytes >> 4);
+                    const uint32_t dsa = sa0 + (uint32_t)s * (kTileBytes >> 4), dsb = sb0 + (uint32_t)s * (C::kSbBytes >> 4);
                     // scales of this stage: per atom 4 columns for the weights, 8 for the tokens; the two buffers take turns
-                    const uint32_t sa_col = tmem_base + (uint32_t)(C::kScaleCol0) + scale_buffer, sb_col = sa_col + 8;
-                    scale_buffer = scale_buffer == 0 ? kScaleCols : 0;
-                    const int blocks = min(kTileK / kBlock, plan.k_blocks - kb * (kTileK / kBlock));
-#pragma unroll
-                    for (int atom = 0; atom < 2; ++atom) {
-                        if (4 * atom >= blocks) break;
-                        copy_scales<CTAS>(sa_col + 4 * atom, dsa + (uint64_t)(atom * (kAtomBytes >> 4)));
-                        copy_scales<CTAS>(sb_col + 8 * atom, dsb + (uint64_t)(atom * (kAtomBytes >> 4)));
-                        if (two_blocks) copy_scales<CTAS>(sb_col + 8 * atom + 4, dsb + (uint64_t)((2 + atom) * (kAtomBytes >> 4)));
-                    }
-#pragma unroll
-                    for (int k = 0; k < kTileK / kMmaK; ++k) {
-                        if (2 * k >= blocks) break;
-                        const uint32_t half = (uint32_t)(k & 1) * 2;  // blocks 0 and 1 or 2 and 3 of the atom
-                        mma_mxf4<CTAS>(tmem_d, da + (uint64_t)(2 * k), db + (uint64_t)(2 * k), idesc | (half << 4) | (half << 29), sa_col + 4 * (k >> 1),
-                                       sb_col + 8 * (k >> 1) + (uint32_t)(sub >> 5), (uint32_t)((kb | k) != 0));
+                    const uint32_t sa_col = scale_col, sb_col = sa_col + 8;
+                    scale_col = scale_sum - scale_col;
+                    // Blocks 0 and 1 or 2 and 3 of an atom serve a product: half 0 or 2 of its words.
+                    auto product = [&](int k, uint32_t accumulate) {
+                        const uint32_t half = (uint32_t)(k & 1) * 2;
+                        mma_mxf4<CTAS>(tmem_d, da + (uint32_t)(2 * k), db + (uint32_t)(2 * k), idesc | (half << 4) | (half << 29), sa_col + 4 * (k >> 1),
+                                       sb_col + 8 * (k >> 1) + sub_col, accumulate);
+                    };
+                    auto scales = [&](int atom) {
+                        copy_scales<CTAS>(sa_col + 4 * atom, dsa + (uint32_t)(atom * (kAtomBytes >> 4)));
+                        copy_scales<CTAS>(sb_col + 8 * atom, dsb + (uint32_t)(atom * (kAtomBytes >> 4)));
+                        if (BN > 128 && two_blocks) copy_scales<CTAS>(sb_col + 8 * atom + 4, dsb + (uint32_t)((2 + atom) * (kAtomBytes >> 4)));
+                    };
+                    if (kb + 1 < plan.num_kb || last_blocks == kTileK / kBlock) {  // (a whole tile: without a test at every instruction)
+                        scales(0);
+                        scales(1);
+                        product(0, kb != 0);
+                        product(1, 1);
+                        product(2, 1);
+                        product(3, 1);
+                    } else {
+                        scales(0);
+                        if (last_blocks > 4) scales(1);
+                        product(0, kb != 0);
+#pragma unroll 1
+                        for (int k = 1; 2 * k < last_blocks; ++k) product(k, 1);
                     }
                     commit(empty_bar + s);
                     if (kb + 1 == plan.num_kb) commit(tmem_full_bar + as);
-                    if (++s == C::kStages) { s = 0; phase ^= 1u; }
+                    s = s_next;
+                    if (s == 0) phase ^= 1u;
                 }
                 if (!ok) break;
                 if (++as == kAccStages) { as = 0; aphase ^= 1u; }
@@ -356,10 +387,12 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         T *stage = reinterpret_cast<T *>(smem_stage) + ew * (kStoreRows * 32);
         int as = 0;
         uint32_t aphase = 0;
-        grid_dependency_wait();  // before anything is written: an earlier kernel may still read Y
+        bool waited = false;
         for (int32_t t = first_tile; find_tile<TILE_M>(t, table, a.E, plan, tile); t += tile_step) {
             const int feature0 = tile.feature + (int)rank * kTileRows + quarter * 32, feature = feature0 + lane;
             const bool mine = feature < a.N;
+            if (!waited) grid_dependency_wait();  // (an earlier kernel may have written the bias, or still read Y)
+            waited = true;
             const float bias = mine && a.bias != nullptr ? __ldg(a.bias + (int64_t)tile.expert * a.N + feature) : 0.0f;
             const bool ok = __all_sync(0xffffffffu, wait_for(smem_u32(tmem_full_bar + as), aphase, abort_flag, a.status));
             if (!ok) break;
@@ -427,6 +460,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         if (STAGED && lane == 0) tma_store_wait_all();
     }
 
+    grid_dependency_wait();  // also where a CTA had no tile: this kernel ends after the one before it
     // ---------------- teardown (reached by every thread, also when aborting) ----------------
     __syncwarp();
     tc_fence_before();
