@@ -6,7 +6,6 @@
 // r + 64 and r + 96 that lie side by side in an atom of scales: the four bytes of each leave as one 16-byte store.
 
 #include "q8_mx4.cuh"
-#include "q8_sm100_ptx.cuh"
 
 namespace q8 {
 
@@ -21,73 +20,6 @@ constexpr int kChunk = kTileK;  // columns of a warp
 enum Kind { kMatrix, kFake, kSlots1, kSlots4 };
 template <int KIND>
 constexpr int kRows = KIND == kSlots1 ? 1 : 4;
-
-// Eight values as they lie in memory: four words of two, or eight words of one.
-template <typename T>
-constexpr int kWords = sizeof(T) == 4 ? 8 : 4;
-
-// Eight values from column k0 on; those at or behind `valid` are 0.
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, int valid, int vec, uint32_t (&w)[kWords<T>])
-{
-    if (sizeof(T) == 4 && vec >= 32 && valid >= 8) {
-        asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[kWords<T> - 4]), "=r"(w[kWords<T> - 3]), "=r"(w[kWords<T> - 2]), "=r"(w[kWords<T> - 1])
-                     : "l"(p));
-    } else if (vec >= 16 && valid >= 8) {
-#pragma unroll
-        for (int i = 0; i < kWords<T> / 4; ++i) {
-            const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
-            w[4 * i] = a.x; w[4 * i + 1] = a.y; w[4 * i + 2] = a.z; w[4 * i + 3] = a.w;
-        }
-    } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = i < valid ? reinterpret_cast<const uint32_t *>(p)[i] : 0u;
-    } else {
-        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (2 * i < valid ? (uint32_t)h[2 * i] : 0u) | (2 * i + 1 < valid ? (uint32_t)h[2 * i + 1] << 16 : 0u);
-    }
-}
-template <typename T>
-__device__ __forceinline__ void unpack8(const uint32_t (&w)[kWords<T>], float (&v)[8])
-{
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-    } else if constexpr (std::is_same<T, __half>::value) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-            v[2 * i] = f.x;
-            v[2 * i + 1] = f.y;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    }
-}
-// The fp32 bits of max|v|; at least those of an infinity where one of the values is NaN or infinite.
-template <typename T>
-__device__ __forceinline__ uint32_t max_bits(const uint32_t (&w)[kWords<T>])
-{
-    if constexpr (sizeof(T) == 4) {
-        float m = __uint_as_float(w[0]);
-#pragma unroll
-        for (int i = 1; i < 8; ++i) asm("max.NaN.xorsign.abs.f32 %0, %0, %1;" : "+f"(m) : "f"(__uint_as_float(w[i])));
-        return __float_as_uint(m) & 0x7fffffffu;
-    } else {  // magnitudes order like their bits, two to a word
-        uint32_t m = w[0] & 0x7fff7fffu;
-#pragma unroll
-        for (int i = 1; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
-        m = max(m & 0xffffu, m >> 16);
-        if constexpr (std::is_same<T, __half>::value) return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));  // (NaN stays NaN)
-        else return m << 16;
-    }
-}
 
 template <typename T>
 __device__ __forceinline__ void store8(T *p, int valid, int vec, const float (&v)[8])
@@ -115,35 +47,6 @@ __device__ __forceinline__ void store8(T *p, int valid, int vec, const float (&v
         for (int i = 0; i < 8; ++i)
             if (i < valid) p[i] = from_float<T>(v[i]);
     }
-}
-
-// E of the block that this lane and its three neighbours hold, and the lane's codes.  NaN becomes 0; neither NaN nor an infinity is
-// in the maximum (`odd` says that there was one).
-template <typename T>
-__device__ __forceinline__ uint32_t quantize8(const uint32_t (&w)[kWords<T>], uint32_t &E, bool &odd)
-{
-    float v[8];
-    unpack8<T>(w, v);
-    uint32_t top = max_bits<T>(w);
-    if (__any_sync(0xffffffffu, top >= 0x7f800000u)) {  // once more, without what is not a number
-        odd = true;
-        top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t bits = __float_as_uint(v[i]) & 0x7fffffffu;
-            if (bits > 0x7f800000u) v[i] = 0.0f;
-            if (bits < 0x7f800000u) top = max(top, bits);
-        }
-    }
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const uint32_t field = top >> 23;
-    E = field > 2 ? field - 2 : 0;
-    const float inv = inverse_scale(E);
-    const uint64_t inv2 = ptx::pack_f32x2(inv, inv);
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(v[i], v[i + 1]), inv2), v[i], v[i + 1]);
-    return pack_e2m1(v);
 }
 
 // (Rows and tasks are counted in 32 bits: with 64-bit divisions the indices took as many instructions as the arithmetic.)
@@ -291,14 +194,6 @@ mx4_dequantize_kernel(const uint8_t *tiles, uint32_t groups, uint32_t rows, int3
     }
 }
 
-// The largest access of up to 32 bytes that the rows are aligned for.  (fp32 in two halves of 16 bytes writes half sectors: dequantising
-// 24576 x 1024 30 us, in one piece 17.)
-int rows_aligned(const void *p, int64_t ld, int size)
-{
-    const uint64_t all = reinterpret_cast<uintptr_t>(p) | (uint64_t)(ld * size);
-    return all % 32 == 0 ? 32 : all % 16 == 0 ? 16 : 0;
-}
-
 cudaError_t grid_of(int64_t tasks, dim3 *grid)
 {
     if (tasks > 0x7fffffff) return cudaErrorInvalidConfiguration;  // more than 2^41 values
@@ -315,7 +210,7 @@ cudaError_t launch_kind(const Mx4QuantizeArgs &a, cudaStream_t s)
     cudaError_t e = grid_of(tasks, &grid);
     if (e != cudaSuccess) return e;
     return launch_overlapping_tail(mx4_quantize_kernel<T, KIND>, grid, dim3(kThreads), 0, s, a, tasks, chunks, row_lanes,
-                                   rows_aligned(a.X, a.ld, sizeof(T)), rows_aligned(a.Xhat, a.ldo, sizeof(T)));
+                                   value_alignment(a.X, a.ld, sizeof(T)), value_alignment(a.Xhat, a.ldo, sizeof(T)));
 }
 
 template <typename T>
@@ -346,7 +241,7 @@ cudaError_t launch_mx4_dequantize(const uint8_t *tiles, int64_t groups, int64_t 
     dim3 grid;
     cudaError_t e = grid_of(tasks, &grid);
     if (e != cudaSuccess) return e;
-    const int vec = rows_aligned(Y, ldy, dtype == Q8_F32 ? 4 : 2);
+    const int vec = value_alignment(Y, ldy, dtype == Q8_F32 ? 4 : 2);
     switch (dtype) {
         case Q8_F32: return launch_overlapping_tail(mx4_dequantize_kernel<float>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<float *>(Y), ldy, tasks, chunks, vec);
         case Q8_F16: return launch_overlapping_tail(mx4_dequantize_kernel<__half>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<__half *>(Y), ldy, tasks, chunks, vec);

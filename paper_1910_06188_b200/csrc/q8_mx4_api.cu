@@ -34,6 +34,37 @@ q8_status check_layer(int64_t M, int64_t N, int64_t K, int64_t E, int64_t ldy)
     return Q8_OK;
 }
 
+// The activation into the workspace and the product from there, or both in one kernel where the tokens are few.
+q8_status quantize_and_multiply(Mx4GemmArgs g, const void *X, int x_dtype, int64_t ldx, int64_t x_rows, const int32_t *index, void *workspace,
+                                cudaStream_t s)
+{
+    if (mx4_fused_preferred(g.M, g.E, g.offsets != nullptr)) {
+        g.values = X;
+        g.x_dtype = x_dtype;
+        g.ldx = ldx;
+        g.x_rows = x_rows;
+        g.index = index;
+        return cuda_status(launch_mx4_gemm(g, s));
+    }
+    Mx4QuantizeArgs a = {};
+    a.X = X;
+    a.ld = ldx;
+    a.groups = 1;
+    a.rows = g.M;
+    a.K = g.K;
+    a.out = static_cast<uint8_t *>(workspace);
+    a.status = g.status;
+    a.offsets = g.offsets;
+    a.E = g.E;
+    a.index = index;
+    a.x_rows = x_rows;
+    const cudaError_t e = launch_mx4_quantize(a, x_dtype, s);
+    if (e != cudaSuccess) return Q8_ERR_CUDA;
+    g.X = a.out;
+    g.behind_quantise = true;
+    return cuda_status(launch_mx4_gemm(g, s));
+}
+
 }  // namespace
 
 extern "C" {
@@ -151,19 +182,7 @@ q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *
         !aligned_to(Y, dtype_bytes(y_dtype)) || !aligned_to(dev_status, 4) || !aligned_to(workspace, 256))
         return Q8_ERR_ALIGN;
     if (workspace_bytes < q8_mx4_linear_workspace_bytes(M, K)) return Q8_ERR_WORKSPACE;
-    Mx4QuantizeArgs a = {};
-    a.X = X;
-    a.ld = ldx;
-    a.groups = 1;
-    a.rows = M;
-    a.K = K;
-    a.out = static_cast<uint8_t *>(workspace);
-    a.status = dev_status;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = launch_mx4_quantize(a, x_dtype, s);
-    if (e != cudaSuccess) return Q8_ERR_CUDA;
     Mx4GemmArgs g = {};
-    g.X = a.out;
     g.W = Wq;
     g.bias = bias;
     g.Y = Y;
@@ -175,8 +194,7 @@ q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *
     g.act = act;
     g.E = 1;
     g.status = dev_status;
-    g.behind_quantise = true;
-    return cuda_status(launch_mx4_gemm(g, s));
+    return quantize_and_multiply(g, X, x_dtype, ldx, M, nullptr, workspace, static_cast<cudaStream_t>(stream));
 }
 
 q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t x_rows, const int32_t *rows, const int32_t *offsets, int64_t experts,
@@ -195,23 +213,7 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
         !aligned_to(bias, 4) || !aligned_to(Y, dtype_bytes(y_dtype)) || !aligned_to(dev_status, 4) || !aligned_to(workspace, 256))
         return Q8_ERR_ALIGN;
     if (workspace_bytes < q8_mx4_linear_grouped_workspace_bytes(T, experts, K)) return Q8_ERR_WORKSPACE;
-    Mx4QuantizeArgs a = {};
-    a.X = X;
-    a.ld = ldx;
-    a.groups = 1;
-    a.rows = T;
-    a.K = K;
-    a.out = static_cast<uint8_t *>(workspace);
-    a.status = dev_status;
-    a.offsets = offsets;
-    a.E = (int)experts;
-    a.index = rows;
-    a.x_rows = x_rows;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = launch_mx4_quantize(a, x_dtype, s);
-    if (e != cudaSuccess) return Q8_ERR_CUDA;
     Mx4GemmArgs g = {};
-    g.X = a.out;
     g.W = Wq;
     g.bias = bias;
     g.Y = Y;
@@ -224,8 +226,7 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
     g.offsets = offsets;
     g.E = (int)experts;
     g.status = dev_status;
-    g.behind_quantise = true;
-    return cuda_status(launch_mx4_gemm(g, s));
+    return quantize_and_multiply(g, X, x_dtype, ldx, x_rows, rows, workspace, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

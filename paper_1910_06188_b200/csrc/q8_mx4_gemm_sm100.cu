@@ -12,6 +12,9 @@
 //               32), fp32 accumulators in TMEM, double buffered
 //   warps 3..   epilogue: tcgen05.ld, bias, GELU, conversion, store
 //
+// Few tokens (X not void): no quantise pass; the epilogue warps first quantise the tokens of the tile into the operand stages themselves,
+// while the weights, which are what such a product waits for, are on their way.
+//
 // CTAS = 2 (cta_group::2): a pair of SMs shares a tile of 256 features; each loads its own 128 rows of weights, half of the tokens and the
 // scales of all of them.  A plain product is the grouped one with a single expert.  Every wait on an mbarrier is bounded: after
 // ~2 s the CTA raises Q8_ERR_TIMEOUT in the status word, all roles leave their loops, copies and products in flight are waited for
@@ -34,18 +37,20 @@ using gemm_detail::gelu_fast_x2;
 constexpr int kAccStages = 2;
 constexpr int kScaleBytes = 2 * kAtomBytes;  // of a tile
 constexpr int kScaleCols = 4 * 2 + 8 * 2;    // TMEM columns of a stage's scales: 128 weight rows, 256 token rows, two atoms each
+constexpr int kFusedStages = 9;
+constexpr int kFusedTokens = 32;                // of a tile
 constexpr int kStoreRows = 32;               // tokens of a staged block of 32 features
 
-template <int CTAS, int BN, int EW, bool STAGED, int SIZE>
+template <int CTAS, int BN, int EW, bool STAGED, int SIZE, bool FUSED>
 struct Cfg {
     static constexpr int kThreads = 96 + 32 * EW;
     static constexpr int kBBytes = BN / CTAS * 128;
-    static constexpr int kSbBytes = 2 * kScaleBytes;  // two row blocks: a tile of 192 may start in the middle of one
+    static constexpr int kSbBytes = (FUSED ? 1 : 2) * kScaleBytes;  // two row blocks: a tile of 192 may start in the middle of one
     static constexpr int kStageBytes = kTileBytes + kBBytes + kSbBytes;
     static constexpr int kStagingBytes = STAGED ? EW * kStoreRows * 32 * SIZE : 0;
     static constexpr int kTableBytes = 3 * (kMaxExperts + 1) * 4 + 4;
     static constexpr int kBudget = 227 * 1024 - 1024 - kTableBytes - kStagingBytes - 512;
-    static constexpr int kStages = kBudget / kStageBytes > 8 ? 8 : kBudget / kStageBytes;
+    static constexpr int kStages = FUSED ? kFusedStages : kBudget / kStageBytes > 8 ? 8 : kBudget / kStageBytes;
     // Two accumulators of 256 columns leave no room for the scales: they share 48 columns, which the epilogue empties first.
     static constexpr int kAccStride = BN == 256 ? 512 - 2 * kScaleCols - 256 : BN;
     static constexpr int kScaleCol0 = kAccStride + BN;
@@ -54,7 +59,7 @@ struct Cfg {
     static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStagingBytes + kTableBytes + kBarrierBytes;
     static_assert(kScaleCol0 + 2 * kScaleCols <= 512, "TMEM columns");
     static_assert(kSmemBytes <= 232448 && kStages >= 3, "shared memory budget");
-    static_assert(BN % (32 * CTAS) == 0 && (BN <= 192 || (BN == 256 && CTAS == 2 && EW == 16)) && kBBytes % 1024 == 0, "tile width");
+    static_assert(BN % (FUSED ? 32 : 64) == 0 && (!FUSED || (CTAS == 1 && BN == kFusedTokens && EW == 8)) && (BN <= 192 || (BN == 256 && CTAS == 2 && EW == 16)) && kBBytes % 1024 == 0, "tile width");
     // Instruction descriptor of kind::mxf4: E2M1 operands, both K-major, UE8M0 scales, M = 128 or 256 for the pair; N / 8 in bits
     // 17..22, which half of a scale word serves in bits 4..5 (B) and 29..30 (A).
     static constexpr uint32_t kInstrDesc = (1u << 7) | (1u << 10) | (1u << 23) | ((uint32_t)CTAS << 27);
@@ -111,6 +116,7 @@ struct Plan {
     int32_t num_kb;    // stages of a tile
     int32_t k_blocks;  // blocks of 32 along K
     int32_t w_blocks;  // row blocks of one expert's weights
+    int32_t x_vec;     // bytes that loads of the tokens' values may take at once
 };
 
 // A tile: expert, its first token (in the expert and as a row of Y), how many tokens it has, its first feature.
@@ -137,6 +143,10 @@ __device__ __forceinline__ bool find_tile(int32_t t, const ExpertTable &table, i
     return true;
 }
 
+__device__ __forceinline__ void mbar_arrive_many(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
 // Bounded wait whose first try is in line.
 __device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status)
 {
@@ -147,12 +157,79 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile
     return mbar_try_wait(bar, parity) || wait_on(bar, parity, abort_flag, status);
 }
 
-template <int CTAS, int BN, int EW, bool STAGED, typename T>
+// The tokens of a tile into the stages of the operand ring.  The EW warps share the stages of a tile, and where it has more than four
+// tokens the rows of a stage: a warp takes four rows of every (EW / warps a stage)-th one, the values of the next on their way
+// while it rounds these.
+template <int EW, int STAGES, int B_BYTES, int SB_BYTES, typename X>
+__device__ __forceinline__ bool quantize_tokens(const Mx4GemmArgs &a, const Plan &plan, const Tile &tile, int ew, int32_t stage0, uint8_t *smem_b, uint8_t *smem_sb,
+                                                uint64_t *full_bar, uint64_t *empty_bar, volatile int *abort_flag)
+{
+    const int lane = threadIdx.x & 31;
+    const int share = tile.count <= 4 ? 1 : tile.count <= 8 ? 2 : tile.count <= 16 ? 4 : 8;  // warps of a stage
+    const int every = EW / share, r0 = ew % share;
+    const X *from[4];
+    bool there[4], odd = false, bad = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = r0 + share * j;
+        int32_t row = tile.row + r;
+        there[j] = r < tile.count;
+        if (there[j] && a.index != nullptr) {
+            row = __ldg(a.index + row);
+            if (row < 0 || row >= a.x_rows) {  // counts as a row of zeros
+                there[j] = false;
+                bad = true;
+            }
+        }
+        from[j] = reinterpret_cast<const X *>(a.values) + (int64_t)row * a.ldx + lane * 8;
+    }
+    uint32_t v[4][kWords<X>];
+    auto load = [&](int kb) {
+        const int valid = max(0, min(8, (int)a.K - kb * kTileK - lane * 8));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load8<X>(from[j] + kb * kTileK, there[j] ? valid : 0, plan.x_vec, v[j]);
+    };
+    int kb = ew / share;
+    if (kb < plan.num_kb) load(kb);
+    for (; kb < plan.num_kb; kb += every) {
+        const uint32_t step = (uint32_t)(stage0 + kb), s = step % STAGES, parity = (step / STAGES) & 1u;
+        uint32_t now[4][kWords<X>];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < kWords<X>; ++i) now[j][i] = v[j][i];
+        if (kb + every < plan.num_kb) load(kb + every);
+        if (!__all_sync(0xffffffffu, wait_for(smem_u32(empty_bar + s), parity ^ 1u, abort_flag, a.status))) return false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = r0 + share * j;
+            if (r >= tile.count) break;
+            uint32_t E;
+            const uint32_t codes = quantize8<X>(now[j], E, odd);
+            uint32_t w = E << (8 * ((lane >> 2) & 3));
+            w |= __shfl_xor_sync(0xffffffffu, w, 4);
+            w |= __shfl_xor_sync(0xffffffffu, w, 8);
+            *reinterpret_cast<uint32_t *>(smem_b + s * B_BYTES + code_place(r, lane)) = codes;
+            if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(smem_sb + s * SB_BYTES + scale_place(r, lane >> 2) - kCodeBytes) = w;
+        }
+        fence_proxy_async_smem();  // what the tensor cores read they read through the asynchronous proxy
+        __syncwarp();
+        if (lane == 0) mbar_arrive_many(smem_u32(full_bar + s), (uint32_t)every);
+    }
+    if (a.status != nullptr) {
+        const uint32_t flags = (odd ? 1u << Q8_ERR_SCALE : 0u) | (bad ? 1u << Q8_ERR_INDEX : 0u);
+        if (flags != 0) atomicOr(a.status, (int32_t)flags);
+    }
+    return true;
+}
+
+template <int CTAS, int BN, int EW, bool STAGED, typename T, typename X>
 __global__ void __launch_bounds__(96 + 32 * EW, 1)
 mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_x32, const __grid_constant__ CUtensorMap map_x16,
                 const __grid_constant__ CUtensorMap map_s, const __grid_constant__ CUtensorMap map_y, Mx4GemmArgs a, Plan plan)
 {
-    using C = Cfg<CTAS, BN, EW, STAGED, sizeof(T)>;
+    constexpr bool FUSED = !std::is_void<X>::value;
+    using C = Cfg<CTAS, BN, EW, STAGED, sizeof(T), FUSED>;
     constexpr int TILE_M = kTileRows * CTAS;
     constexpr int kStep = 16 * CTAS;  // widths of tiles are multiples of this
     extern __shared__ uint8_t smem_raw[];
@@ -178,7 +255,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     const bool leader = rank == 0;
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::kStages; ++s) {
-            mbar_init(smem_u32(full_bar + s), 2);  // both producers (the leader's), with the byte counts
+            mbar_init(smem_u32(full_bar + s), FUSED ? 1 + EW : 2);  // both producers (the leader's), with the byte counts
             mbar_init(smem_u32(empty_bar + s), 1);
         }
         for (int s = 0; s < kAccStages; ++s) {
@@ -193,8 +270,8 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         if (CTAS == 2) tmem_alloc_pair(smem_u32(tmem_slot), C::kTmemCols);
         else tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
     }
-    // (The offsets may be read at once, see below.)
     if (warp == 2) {
+        if (a.offsets != nullptr && !a.behind_quantise) grid_dependency_wait();
         const bool bad = build_expert_table(table, a.offsets, a.E, (int32_t)a.M, plan.tile_n, plan.tiles_m);
         if (bad && lane == 0 && blockIdx.x == 0 && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_INDEX);
     }
@@ -208,7 +285,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     const int32_t first_tile = blockIdx.x / CTAS, tile_step = gridDim.x / CTAS;
     Tile tile;
     auto width_of = [&](const Tile &t) { return (t.count + kStep - 1) / kStep * kStep; };
-    if (warp == 0 || warp == 2) {
+    if (warp == 0 || (warp == 2 && !FUSED)) {
         // ---------------- producers ----------------
         // A pair's loads all report to the leader's barrier, which its MMA warp waits on.  The tensor maps of the pair see tiles as rows of 128
         // bytes: 136 of them to a tile, the last 8 its scales.
@@ -323,7 +400,9 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 const int width = width_of(tile);
                 const uint32_t tmem_d = tmem_base + (uint32_t)(as * C::kAccStride);
                 const uint32_t idesc = C::kInstrDesc | ((uint32_t)(width >> 3) << 17);
-                const int sub = tile.first % kTileRows;  // a multiple of 32
+                // Where the tile's first token is in its row block: a multiple of 64, so that the scales start at an even column, as they have to.
+                // (Tokens that were quantised here are at the start of the stage, wherever the tile begins.)
+                const int sub = FUSED ? 0 : tile.first % kTileRows;
                 const uint32_t sub_col = (uint32_t)sub >> 5;
                 const bool two_blocks = sub + width > kTileRows;
                 bool ready = mbar_try_wait(smem_u32(full_bar + s), phase);
@@ -378,7 +457,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 while (!mbar_try_wait(smem_u32(drain_bar), 0) && global_timer_ns() - t0 < 50000000ull) {}
             }
         }
-    } else {
+    } else if (warp >= 3) {
         // ---------------- epilogue ----------------
         const int ew = warp - 3;
         const int quarter = warp & 3;  // TMEM lanes 32 * quarter .. + 31
@@ -388,7 +467,14 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         int as = 0;
         uint32_t aphase = 0;
         bool waited = false;
+        int32_t stage0 = 0;  // stages of the tiles before
         for (int32_t t = first_tile; find_tile<TILE_M>(t, table, a.E, plan, tile); t += tile_step) {
+            if constexpr (FUSED) {
+                if (!waited) grid_dependency_wait();
+                waited = true;
+                if (!quantize_tokens<EW, C::kStages, C::kBBytes, C::kSbBytes, X>(a, plan, tile, ew, stage0, smem_b, smem_sb, full_bar, empty_bar, abort_flag)) break;
+                stage0 += plan.num_kb;
+            }
             const int feature0 = tile.feature + (int)rank * kTileRows + quarter * 32, feature = feature0 + lane;
             const bool mine = feature < a.N;
             if (!waited) grid_dependency_wait();  // (an earlier kernel may have written the bias, or still read Y)
@@ -501,11 +587,11 @@ bool output_map(CUtensorMap *map, const Mx4GemmArgs &a)
 }
 bool output_aligned(const Mx4GemmArgs &a) { return reinterpret_cast<uintptr_t>(a.Y) % 16 == 0 && a.ldy * (a.y_dtype == Q8_F32 ? 4 : 2) % 16 == 0; }
 
-template <int CTAS, int BN, int EW, bool STAGED, typename T>
+template <int CTAS, int BN, int EW, bool STAGED, typename T, typename X>
 cudaError_t launch_typed(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, cudaStream_t s)
 {
-    using C = Cfg<CTAS, BN, EW, STAGED, sizeof(T)>;
-    auto kernel = mx4_gemm_kernel<CTAS, BN, EW, STAGED, T>;
+    using C = Cfg<CTAS, BN, EW, STAGED, sizeof(T), !std::is_void<X>::value>;
+    auto kernel = mx4_gemm_kernel<CTAS, BN, EW, STAGED, T, X>;
     static bool attr_set[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -552,21 +638,23 @@ cudaError_t launch_typed(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, 
     return cudaLaunchKernelEx(&cfg, kernel, mw, mx, mx32, mx16, ms, my, a, plan);
 }
 
-template <int CTAS, int BN, int EW, bool STAGED>
+template <int CTAS, int BN, int EW, bool STAGED, typename X = void>
 cudaError_t launch_shape(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, cudaStream_t s)
 {
     switch (a.y_dtype) {
-        case Q8_F32: return launch_typed<CTAS, BN, EW, STAGED, float>(a, plan, tiles, s);
-        case Q8_F16: return launch_typed<CTAS, BN, EW, STAGED, __half>(a, plan, tiles, s);
-        default: return launch_typed<CTAS, BN, EW, STAGED, __nv_bfloat16>(a, plan, tiles, s);
+        case Q8_F32: return launch_typed<CTAS, BN, EW, STAGED, float, X>(a, plan, tiles, s);
+        case Q8_F16: return launch_typed<CTAS, BN, EW, STAGED, __half, X>(a, plan, tiles, s);
+        default: return launch_typed<CTAS, BN, EW, STAGED, __nv_bfloat16, X>(a, plan, tiles, s);
     }
 }
 
 }  // namespace
 
+bool mx4_fused_preferred(int64_t M, int64_t E, bool grouped) { return grouped ? M <= 16 * E : M <= kFusedTokens; }
+
 cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s)
 {
-    Plan p;
+    Plan p = {};
     p.num_kb = (int32_t)tiles_along(a.K);
     p.k_blocks = (int32_t)ceil_div(a.K, kBlock);
     p.w_blocks = (int32_t)ceil_div(a.N, kTileRows);
@@ -575,6 +663,16 @@ cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s)
     const int64_t mean = ceil_div(a.M, a.E);
     const int sms = sm_count();
     const int64_t extra = a.E > 1 ? hit : 0;  // tiles of tokens that are not full, at most
+    if (a.values != nullptr) {
+        p.tile_n = kFusedTokens;
+        p.x_vec = value_alignment(a.values, a.ldx, a.x_dtype == Q8_F32 ? 4 : 2);
+        const int64_t tiles = (ceil_div(a.M, p.tile_n) + extra) * p.tiles_m;
+        switch (a.x_dtype) {
+            case Q8_F32: return launch_shape<1, kFusedTokens, 8, false, float>(a, p, tiles, s);
+            case Q8_F16: return launch_shape<1, kFusedTokens, 8, false, __half>(a, p, tiles, s);
+            default: return launch_shape<1, kFusedTokens, 8, false, __nv_bfloat16>(a, p, tiles, s);
+        }
+    }
     // pairs once each has work
     const int64_t pairs = ceil_div(a.N, 2 * kTileRows);
     if (mean > 128 && ceil_div(a.M, 256) * pairs >= sms / 2) {

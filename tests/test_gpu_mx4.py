@@ -269,6 +269,23 @@ def test_grouped(offsets, T, N, K):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("counts", [[8, 8, 14, 34], [0, 70, 0, 0, 1, 0], [33, 0, 0, 5], [2, 0, 96, 1, 0, 0, 0, 3], [31, 32, 33, 0, 0, 0, 0, 0, 0]])
+def test_grouped_few_slots_unevenly(counts, dtype):
+    """Experts with more slots than the others have on average."""
+    offsets = [0, *np.cumsum(counts).tolist()]
+    run_grouped(offsets, offsets[-1], 200, 600, dtype, q8.Q8_ACT_GELU)
+    run_grouped([v + 3 for v in offsets], offsets[-1] + 10, 128, 256, dtype, tokens=9)
+
+
+@pytest.mark.parametrize("counts", [[700, 0, 1300], [256, 257, 255, 1, 0, 900], [1023, 1025]])
+def test_grouped_many_slots(counts):
+    """Enough for pairs of CTAs: full and cut tiles of experts, features that end in the first half of a pair's tile."""
+    offsets = [0, *np.cumsum(counts).tolist()]
+    for dtype, N in ((torch.float32, 2400), (torch.bfloat16, 2500), (torch.float16, 2305)):
+        run_grouped(offsets, offsets[-1] + 5, N, 520, dtype, q8.Q8_ACT_GELU, tokens=offsets[-1] // 2)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
 @pytest.mark.parametrize("E,T", [(7, 20), (64, 40), (64, 3000), (5, 4000), (1, 100)])
 def test_grouped_routed(E, T, dtype):
     cuts = np.sort(np.random.RandomState(E).randint(0, T + 1, E - 1)).tolist()
