@@ -787,7 +787,7 @@ def q8_mx4_linear(X, W: Mx4, bias=None, act: int = Q8_ACT_NONE, Y=None, dtype: O
         workspace = _mx4_empty(q8_mx4_linear_workspace_bytes(M, K), torch.uint8, X.device, stream)
     _mx4_same_device(X, W.tiles, bias, Y, workspace, dev_status)
     st = load().q8_mx4_linear(x, x_dtype, ldx, wq, _mx4_bias(bias, N), int(act), y, y_dtype, ldy, M, N, K,
-                              _any_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(),
+                              _any_ptr(workspace, "workspace") or None, workspace.numel() * workspace.element_size(),
                               _ptr(dev_status, torch.int32, "dev_status"), _stream(stream))
     _check(st, "q8_mx4_linear")
     return Y

@@ -46,15 +46,6 @@ struct ExpertTable {
     int32_t *block;  // E + 1
     int32_t *tile;   // E + 1, or nullptr
 };
-__device__ __forceinline__ int32_t scan_max(int32_t v, int lane)
-{
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int32_t o = __shfl_up_sync(0xffffffffu, v, d);
-        if (lane >= d) v = max(v, o);
-    }
-    return v;
-}
 __device__ __forceinline__ int32_t scan_sum(int32_t v, int lane)
 {
 #pragma unroll
@@ -64,45 +55,49 @@ __device__ __forceinline__ int32_t scan_sum(int32_t v, int lane)
     }
     return v;
 }
-// Written by one warp, 32 experts at a time.  Offsets outside [0, T] or below an earlier one (a caller's mistake) are moved to the
-// nearest allowed value, so that every slot belongs to one expert at most and no access leaves the tensors; returns whether there
-// were any.  An expert has ceil(slots / tile_n) tiles_m tiles.  offsets == nullptr: one expert with all T slots.
+// Written by one warp, a lane a run of neighbouring experts.  Offsets outside [0, T] or below an earlier one (a caller's mistake)
+// are moved to the nearest allowed value, so that every slot belongs to one expert at most and no access leaves the tensors; returns
+// whether there were any.  An expert has ceil(slots / tile_n) tiles_m tiles.
 __device__ __forceinline__ bool build_expert_table(const ExpertTable &t, const int32_t *offsets, int E, int32_t T, int32_t tile_n, int32_t tiles_m)
 {
     const int lane = threadIdx.x & 31;
-    if (offsets == nullptr) {
-        if (lane < 2) {
-            t.start[lane] = lane * T;
-            t.block[lane] = lane * ((T + kTileRows - 1) / kTileRows);
-            if (t.tile != nullptr) t.tile[lane] = lane * ((T + tile_n - 1) / tile_n * tiles_m);
-        }
-        __syncwarp();
-        return false;
-    }
+    const int run = (E + 32) / 32, lo = min(lane * run, E + 1), hi = min(lo + run, E + 1);  // of E + 1 offsets
+    for (int i = lane; i <= E; i += 32) t.start[i] = __ldg(offsets + i);
+    __syncwarp();
     bool bad = false;
-    int32_t top = 0, blocks = 0, tiles = 0;
-    int32_t next = lane <= E ? __ldg(offsets + lane) : 0;
-    for (int e0 = 0; e0 <= E; e0 += 32) {
-        const int e = e0 + lane;
-        const int32_t raw = next;
-        next = e + 32 <= E ? __ldg(offsets + e + 32) : 0;  // on its way while this batch is scanned
-        const int32_t first_next = __shfl_sync(0xffffffffu, next, 0);
-        const int32_t v = e <= E ? min(max(raw, 0), T) : 0;
-        const int32_t begin = max(scan_max(v, lane), top);
-        bad |= e <= E && (raw != v || v < begin);
-        int32_t end = __shfl_down_sync(0xffffffffu, begin, 1);
-        if (lane == 31) end = max(begin, min(max(first_next, 0), T));
-        const int32_t count = e < E ? end - begin : 0;
-        const int32_t nb = (count + kTileRows - 1) / kTileRows, nt = t.tile != nullptr ? (count + tile_n - 1) / tile_n * tiles_m : 0;
-        const int32_t sb = scan_sum(nb, lane), st = scan_sum(nt, lane);
-        if (e <= E) {
-            t.start[e] = begin;
-            t.block[e] = blocks + sb - nb;
-            if (t.tile != nullptr) t.tile[e] = tiles + st - nt;
-        }
-        top = __shfl_sync(0xffffffffu, begin, 31);
-        blocks += __shfl_sync(0xffffffffu, sb, 31);
-        tiles += __shfl_sync(0xffffffffu, st, 31);
+    int32_t top = 0;
+    for (int i = lo; i < hi; ++i) {
+        const int32_t v = t.start[i];
+        bad |= v < top || v > T;
+        top = max(top, min(v, T));
+        t.start[i] = top;
+    }
+    int32_t before = top;  // what the lanes before have at most
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t o = __shfl_up_sync(0xffffffffu, before, d);
+        if (lane >= d) before = max(before, o);
+    }
+    before = __shfl_up_sync(0xffffffffu, before, 1);
+    if (lane == 0) before = 0;
+    for (int i = lo; i < hi && t.start[i] < before; ++i) {
+        bad = true;
+        t.start[i] = before;
+    }
+    __syncwarp();
+    int32_t blocks = 0, tiles = 0;
+    for (int i = lo; i < min(hi, E); ++i) {
+        const int32_t count = t.start[i + 1] - t.start[i];
+        blocks += (count + kTileRows - 1) / kTileRows;
+        if (t.tile != nullptr) tiles += (int32_t)((uint32_t)(count + tile_n - 1) / (uint32_t)tile_n) * tiles_m;
+    }
+    int32_t block = scan_sum(blocks, lane) - blocks, tile = t.tile != nullptr ? scan_sum(tiles, lane) - tiles : 0;
+    for (int i = lo; i < hi; ++i) {
+        t.block[i] = block;
+        if (t.tile != nullptr) t.tile[i] = tile;
+        const int32_t count = i < E ? t.start[i + 1] - t.start[i] : 0;
+        block += (count + kTileRows - 1) / kTileRows;
+        if (t.tile != nullptr) tile += (int32_t)((uint32_t)(count + tile_n - 1) / (uint32_t)tile_n) * tiles_m;
     }
     bad = __any_sync(0xffffffffu, bad);
     __syncwarp();

@@ -111,34 +111,48 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
                  : "memory");
 }
 struct Plan {
+    int32_t tiles;     // of a plain product
     int32_t tile_n;    // tokens of a full tile
     int32_t tiles_m;   // tiles of features
+    uint32_t inv_m;    // floor(2^32 / tiles_m), at most 2^32 - 1: its high products are the quotients or one below
     int32_t num_kb;    // stages of a tile
     int32_t k_blocks;  // blocks of 32 along K
     int32_t w_blocks;  // row blocks of one expert's weights
     int32_t x_vec;     // bytes that loads of the tokens' values may take at once
 };
 
-// A tile: expert, its first token (in the expert and as a row of Y), how many tokens it has, its first feature.
+// A tile: expert and its first row block of tokens, the tile's first token (in the expert and as a row of Y), how many it has, its first feature.
 struct Tile {
-    int32_t expert, first, row, count, feature;
+    int32_t expert, block, first, row, count, feature;
 };
-// Tile t, those of an expert ordered features first; false behind the last one.
+// Tile t, those of an expert ordered features first; false behind the last one.  (A plain product needs no table.)
 template <int TILE_M>
-__device__ __forceinline__ bool find_tile(int32_t t, const ExpertTable &table, int E, const Plan &p, Tile &out)
+__device__ __forceinline__ bool find_tile(int32_t t, const ExpertTable &table, const Mx4GemmArgs &a, const Plan &p, Tile &out)
 {
-    if (t >= table.tile[E]) return false;
-    int e = 0, hi = E - 1;  // the last expert whose tiles begin at or before t: those without tokens have none
-    while (e < hi) {
-        const int mid = (e + hi + 1) >> 1;
-        if (table.tile[mid] <= t) e = mid;
-        else hi = mid - 1;
+    uint32_t local = (uint32_t)t;
+    int32_t end = (int32_t)a.M;
+    out.expert = out.block = out.row = 0;
+    if (a.offsets == nullptr) {
+        if (t >= p.tiles) return false;
+    } else {
+        if (t >= table.tile[a.E]) return false;
+        int e = 0, hi = a.E - 1;  // the last expert whose tiles begin at or before t: those without tokens have none
+        while (e < hi) {
+            const int mid = (e + hi + 1) >> 1;
+            if (table.tile[mid] <= t) e = mid;
+            else hi = mid - 1;
+        }
+        local -= (uint32_t)table.tile[e];
+        out.expert = e;
+        out.block = table.block[e];
+        out.row = table.start[e];
+        end = table.start[e + 1];
     }
-    const uint32_t local = (uint32_t)(t - table.tile[e]), n = local / (uint32_t)p.tiles_m;
-    out.expert = e;
+    uint32_t n = __umulhi(local, p.inv_m);
+    if (local - n * (uint32_t)p.tiles_m >= (uint32_t)p.tiles_m) ++n;
     out.first = (int32_t)n * p.tile_n;
-    out.row = table.start[e] + out.first;
-    out.count = min(p.tile_n, table.start[e + 1] - out.row);
+    out.row += out.first;
+    out.count = min(p.tile_n, end - out.row);
     out.feature = (int32_t)(local - n * p.tiles_m) * TILE_M;
     return true;
 }
@@ -253,33 +267,35 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;
     const bool leader = rank == 0;
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < C::kStages; ++s) {
-            mbar_init(smem_u32(full_bar + s), FUSED ? 1 + EW : 2);  // both producers (the leader's), with the byte counts
-            mbar_init(smem_u32(empty_bar + s), 1);
-        }
-        for (int s = 0; s < kAccStages; ++s) {
-            mbar_init(smem_u32(tmem_full_bar + s), 1);
-            mbar_init(smem_u32(tmem_empty_bar + s), EW * CTAS);
-        }
-        mbar_init(smem_u32(drain_bar), 1);
-        *abort_flag = 0;
+    // What the roles need of the arguments first, all at once: one line of them after the other costs 200 cycles each time.
+    asm volatile("" ::"l"(a.W), "l"(a.values), "l"(a.offsets), "l"(a.Y), "l"(a.M), "l"(a.K), "r"(plan.tiles), "r"(plan.w_blocks));
+    if (warp == 0) {  // a lane a barrier
+        constexpr int kBarriers = 2 * C::kStages + 2 * kAccStages + 1;
+        static_assert(kBarriers <= 32, "barriers");
+        // full: both producers (the leader's), with the byte counts, or the weights' and the warps that quantise; tmem_empty: the epilogue's warps
+        if (lane < kBarriers)
+            mbar_init(smem_u32(full_bar + lane), lane < C::kStages ? (FUSED ? 1 + EW : 2)
+                                                 : lane >= 2 * C::kStages + kAccStages && lane < 2 * C::kStages + 2 * kAccStages ? EW * CTAS : 1);
+        if (lane == 0) *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
         if (CTAS == 2) tmem_alloc_pair(smem_u32(tmem_slot), C::kTmemCols);
         else tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
     }
-    if (warp == 2) {
-        if (a.offsets != nullptr && !a.behind_quantise) grid_dependency_wait();
+    if (warp == 2 && a.offsets != nullptr) {
+        if (!a.behind_quantise) grid_dependency_wait();
         const bool bad = build_expert_table(table, a.offsets, a.E, (int32_t)a.M, plan.tile_n, plan.tiles_m);
         if (bad && lane == 0 && blockIdx.x == 0 && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_INDEX);
     }
+    // A plain product's weight producer, which made the barriers and needs neither the table nor TMEM, goes ahead without the others.
     tc_fence_before();
-    __syncthreads();
+    __syncwarp();
+    if (CTAS == 1 && a.offsets == nullptr && warp == 0) asm volatile("barrier.cta.arrive 1, %0;" ::"n"(C::kThreads) : "memory");
+    else asm volatile("barrier.cta.sync 1, %0;" ::"n"(C::kThreads) : "memory");
     if (CTAS == 2) cluster_sync_all();  // the peer's barriers exist before anything signals them
     tc_fence_after();
-    const uint32_t tmem_base = *tmem_slot;
+    const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(tmem_slot);  // (not yet there for that producer, which does not use it)
     grid_dependency_release_next(true);
 
     const int32_t first_tile = blockIdx.x / CTAS, tile_step = gridDim.x / CTAS;
@@ -300,12 +316,12 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             uint32_t phase = 0;
             int64_t issued = 0;
             bool ok = true, waited = false;
-            for (int32_t t = first_tile; ok && find_tile<TILE_M>(t, table, a.E, plan, tile); t += tile_step) {
+            for (int32_t t = first_tile; ok && find_tile<TILE_M>(t, table, a, plan, tile); t += tile_step) {
                 const int width = width_of(tile), mine = width / CTAS;
                 const int64_t w_tile = ((int64_t)tile.expert * plan.w_blocks + tile.feature / kTileRows + rank) * plan.num_kb;
                 const int first = tile.first + (int)rank * mine, sub = first % kTileRows;
-                const int64_t x_tile = ((int64_t)table.block[tile.expert] + first / kTileRows) * plan.num_kb;
-                const int64_t s_tile = ((int64_t)table.block[tile.expert] + tile.first / kTileRows) * plan.num_kb;
+                const int64_t x_tile = ((int64_t)tile.block + first / kTileRows) * plan.num_kb;
+                const int64_t s_tile = ((int64_t)tile.block + tile.first / kTileRows) * plan.num_kb;
                 const bool two_scales = tile.first % kTileRows + width > kTileRows;  // the tile's tokens lie in two row blocks
                 const int in_first = min(mine, kTileRows - sub);                     // of this CTA's tokens, those in the first row block
                 const uint32_t bytes = CTAS == 1 ? (weights ? kTileBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 2 : 1))
@@ -391,7 +407,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             const uint32_t scale_sum = 2 * scale_col + kScaleCols;
             const int last_blocks = plan.k_blocks - (plan.num_kb - 1) * (kTileK / kBlock);  // of the last stage
             bool ok = true;
-            for (int32_t t = first_tile; ok && find_tile<TILE_M>(t, table, a.E, plan, tile); t += tile_step) {
+            for (int32_t t = first_tile; ok && find_tile<TILE_M>(t, table, a, plan, tile); t += tile_step) {
                 // the tile before last has left this accumulator, or the last one the columns that it shares with it
                 constexpr bool kShared = C::kAccStride < BN;
                 ok = wait_for(smem_u32(tmem_empty_bar + (kShared ? as ^ 1 : as)), kShared && as == 1 ? aphase : aphase ^ 1u, abort_flag, a.status);
@@ -468,7 +484,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         uint32_t aphase = 0;
         bool waited = false;
         int32_t stage0 = 0;  // stages of the tiles before
-        for (int32_t t = first_tile; find_tile<TILE_M>(t, table, a.E, plan, tile); t += tile_step) {
+        for (int32_t t = first_tile; find_tile<TILE_M>(t, table, a, plan, tile); t += tile_step) {
             if constexpr (FUSED) {
                 if (!waited) grid_dependency_wait();
                 waited = true;
@@ -588,8 +604,10 @@ bool output_map(CUtensorMap *map, const Mx4GemmArgs &a)
 bool output_aligned(const Mx4GemmArgs &a) { return reinterpret_cast<uintptr_t>(a.Y) % 16 == 0 && a.ldy * (a.y_dtype == Q8_F32 ? 4 : 2) % 16 == 0; }
 
 template <int CTAS, int BN, int EW, bool STAGED, typename T, typename X>
-cudaError_t launch_typed(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, cudaStream_t s)
+cudaError_t launch_typed(const Mx4GemmArgs &a, Plan plan, int64_t tiles, cudaStream_t s)
 {
+    plan.tiles = (int32_t)tiles;
+    plan.inv_m = plan.tiles_m > 1 ? (uint32_t)((uint64_t(1) << 32) / plan.tiles_m) : 0xffffffffu;
     using C = Cfg<CTAS, BN, EW, STAGED, sizeof(T), !std::is_void<X>::value>;
     auto kernel = mx4_gemm_kernel<CTAS, BN, EW, STAGED, T, X>;
     static bool attr_set[64] = {};

@@ -460,7 +460,7 @@ def test_refusals_on_the_device():
     with pytest.raises(ValueError, match="bytes of tiles"):
         q8.q8_mx4_linear(values((4, 257), 1), q8.Mx4(W.tiles, (8, 257)))
     with pytest.raises(q8.Q8Error) as e:
-        q8.q8_mx4_linear(x, W, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+        q8.q8_mx4_linear(values((130, 64), 1), W, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert e.value.status == q8.Q8_ERR_WORKSPACE
     with pytest.raises(q8.Q8Error) as e:
         q8.q8_mx4_linear(x, W, act=3)
