@@ -318,7 +318,7 @@ q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Wq, const float *bia
  * [experts, N] or NULL.  T slots, sorted by expert: expert e owns the slots offsets[e] <= t < offsets[e + 1] (device, experts + 1
  * values) and computes Y[t] from row rows[t] of X [x_rows, K], or from row t where rows is NULL.  Rows of X may be taken any
  * number of times, experts may own nothing; rows of Y that no expert owns stay as they were.
- * The workspace may be NULL where its size is 0.  A row outside X counts as zeros, offsets that fall or leave [0, T] are moved to the nearest value that does not; both flag
+ * A row outside X counts as zeros, offsets that fall or leave [0, T] are moved to the nearest value that does not; both flag
  * Q8_ERR_INDEX in dev_status. */
 size_t q8_mx4_linear_grouped_workspace_bytes(int64_t T, int64_t experts, int64_t K);
 q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t x_rows, const int32_t *rows,

@@ -287,11 +287,10 @@ struct Mx4GemmArgs {
     // Few tokens: taken and quantised by the product itself, X not used.
     const void *values = nullptr;
     int x_dtype = 0;
-    int64_t ldx = 0, x_rows = 0;
-    const int32_t *index = nullptr;  // row of each slot, or nullptr: the slot's own
+    int64_t ldx = 0;
     bool behind_quantise = false;  // the kernel before this one in the stream is the quantise pass of the same call
 };
 cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s);
-bool mx4_fused_preferred(int64_t M, int64_t E, bool grouped);  // whether to leave the quantisation of the activation to the product
+bool mx4_fused_preferred(int64_t M, int64_t K);  // whether to leave the quantisation of a plain activation to the product
 
 }  // namespace q8

@@ -38,12 +38,10 @@ q8_status check_layer(int64_t M, int64_t N, int64_t K, int64_t E, int64_t ldy)
 q8_status quantize_and_multiply(Mx4GemmArgs g, const void *X, int x_dtype, int64_t ldx, int64_t x_rows, const int32_t *index, void *workspace,
                                 cudaStream_t s)
 {
-    if (mx4_fused_preferred(g.M, g.E, g.offsets != nullptr)) {
+    if (g.offsets == nullptr && mx4_fused_preferred(g.M, g.K)) {
         g.values = X;
         g.x_dtype = x_dtype;
         g.ldx = ldx;
-        g.x_rows = x_rows;
-        g.index = index;
         return cuda_status(launch_mx4_gemm(g, s));
     }
     Mx4QuantizeArgs a = {};
@@ -132,11 +130,11 @@ q8_status q8_mx4_fake_quantize(const void *X, int dtype, int64_t rows, int64_t K
     return cuda_status(launch_mx4_quantize(a, dtype, static_cast<cudaStream_t>(stream)));
 }
 
-size_t q8_mx4_linear_workspace_bytes(int64_t M, int64_t K) { return mx4_fused_preferred(M, 1, false) ? 0 : q8_mx4_bytes(1, M, K); }
+size_t q8_mx4_linear_workspace_bytes(int64_t M, int64_t K) { return M >= 0 && K > 0 && mx4_fused_preferred(M, K) ? 0 : q8_mx4_bytes(1, M, K); }
 
 size_t q8_mx4_linear_grouped_workspace_bytes(int64_t T, int64_t experts, int64_t K)
 {
-    if (T < 0 || T > kMaxRows || experts < 0 || experts > kMaxExperts || K <= 0 || K > kMaxK || mx4_fused_preferred(T, experts, true)) return 0;
+    if (T < 0 || T > kMaxRows || experts < 0 || experts > kMaxExperts || K <= 0 || K > kMaxK) return 0;
     return (size_t)most_row_blocks(T, experts) * (size_t)tiles_along(K) * kTileBytes;
 }
 
@@ -208,7 +206,7 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
     if (st != Q8_OK) return st;
     if (!rows && x_rows < T) return Q8_ERR_SHAPE;
     if (T == 0 || N == 0 || experts == 0) return Q8_OK;
-    if ((!X && x_rows > 0) || !offsets || !Wq || !Y || (!workspace && q8_mx4_linear_grouped_workspace_bytes(T, experts, K) > 0)) return Q8_ERR_NULL;
+    if ((!X && x_rows > 0) || !offsets || !Wq || !Y || !workspace) return Q8_ERR_NULL;
     if (!aligned_to(X, dtype_bytes(x_dtype)) || !aligned_to(rows, 4) || !aligned_to(offsets, 4) || !aligned_to(Wq, 16) ||
         !aligned_to(bias, 4) || !aligned_to(Y, dtype_bytes(y_dtype)) || !aligned_to(dev_status, 4) || !aligned_to(workspace, 256))
         return Q8_ERR_ALIGN;

@@ -171,69 +171,53 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile
     return mbar_try_wait(bar, parity) || wait_on(bar, parity, abort_flag, status);
 }
 
-// The tokens of a tile into the stages of the operand ring.  The EW warps share the stages of a tile, and where it has more than four
-// tokens the rows of a stage: a warp takes four rows of every (EW / warps a stage)-th one, the values of the next on their way
-// while it rounds these.
+// The tokens of a tile into the stages of the operand ring.  A warp takes every EW-th stage and all its rows, four at a time, the values of
+// the next four on their way while it rounds these; with fewer stages than warps some share the rows of one.  (All warps on one stage
+// after the other: 24 x 4096 -> 16384 18.9 us.  The fence at the end of a stage waits for loads in flight, so none are over it.)
 template <int EW, int STAGES, int B_BYTES, int SB_BYTES, typename X>
 __device__ __forceinline__ bool quantize_tokens(const Mx4GemmArgs &a, const Plan &plan, const Tile &tile, int ew, int32_t stage0, uint8_t *smem_b, uint8_t *smem_sb,
                                                 uint64_t *full_bar, uint64_t *empty_bar, volatile int *abort_flag)
 {
     const int lane = threadIdx.x & 31;
-    const int share = tile.count <= 4 ? 1 : tile.count <= 8 ? 2 : tile.count <= 16 ? 4 : 8;  // warps of a stage
-    const int every = EW / share, r0 = ew % share;
-    const X *from[4];
-    bool there[4], odd = false, bad = false;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int r = r0 + share * j;
-        int32_t row = tile.row + r;
-        there[j] = r < tile.count;
-        if (there[j] && a.index != nullptr) {
-            row = __ldg(a.index + row);
-            if (row < 0 || row >= a.x_rows) {  // counts as a row of zeros
-                there[j] = false;
-                bad = true;
-            }
-        }
-        from[j] = reinterpret_cast<const X *>(a.values) + (int64_t)row * a.ldx + lane * 8;
-    }
-    uint32_t v[4][kWords<X>];
-    auto load = [&](int kb) {
+    const int share = plan.num_kb >= EW ? 1 : plan.num_kb * 2 >= EW ? 2 : plan.num_kb * 4 >= EW ? 4 : EW;  // warps of a stage
+    const int every = EW / share, r0 = ew % share, step = 4 * share;
+    const X *values = reinterpret_cast<const X *>(a.values) + (int64_t)tile.row * a.ldx + lane * 8;
+    bool odd = false;
+    for (int kb = ew / share; kb < plan.num_kb; kb += every) {
+        const uint32_t n = (uint32_t)(stage0 + kb), s = n % STAGES, parity = (n / STAGES) & 1u;
         const int valid = max(0, min(8, (int)a.K - kb * kTileK - lane * 8));
+        uint32_t v[4][kWords<X>], next[4][kWords<X>];
+        auto load = [&](int row, uint32_t (&to)[4][kWords<X>]) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load8<X>(from[j] + kb * kTileK, there[j] ? valid : 0, plan.x_vec, v[j]);
-    };
-    int kb = ew / share;
-    if (kb < plan.num_kb) load(kb);
-    for (; kb < plan.num_kb; kb += every) {
-        const uint32_t step = (uint32_t)(stage0 + kb), s = step % STAGES, parity = (step / STAGES) & 1u;
-        uint32_t now[4][kWords<X>];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < kWords<X>; ++i) now[j][i] = v[j][i];
-        if (kb + every < plan.num_kb) load(kb + every);
+            for (int j = 0; j < 4; ++j, row += share) load8<X>(values + (int64_t)row * a.ldx + kb * kTileK, row < tile.count ? valid : 0, plan.x_vec, to[j]);
+        };
+        if (r0 < tile.count) load(r0, v);
         if (!__all_sync(0xffffffffu, wait_for(smem_u32(empty_bar + s), parity ^ 1u, abort_flag, a.status))) return false;
+        for (int row = r0; row < tile.count; row += step) {
+            if (row + step < tile.count) load(row + step, next);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = r0 + share * j;
-            if (r >= tile.count) break;
-            uint32_t E;
-            const uint32_t codes = quantize8<X>(now[j], E, odd);
-            uint32_t w = E << (8 * ((lane >> 2) & 3));
-            w |= __shfl_xor_sync(0xffffffffu, w, 4);
-            w |= __shfl_xor_sync(0xffffffffu, w, 8);
-            *reinterpret_cast<uint32_t *>(smem_b + s * B_BYTES + code_place(r, lane)) = codes;
-            if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(smem_sb + s * SB_BYTES + scale_place(r, lane >> 2) - kCodeBytes) = w;
+            for (int j = 0; j < 4; ++j) {
+                const int r = row + share * j;  // (a row behind the last is rounded and dropped, so that the four can be worked on together)
+                uint32_t E;
+                const uint32_t codes = quantize8<X>(v[j], E, odd);
+                uint32_t w = E << (8 * ((lane >> 2) & 3));
+                w |= __shfl_xor_sync(0xffffffffu, w, 4);
+                w |= __shfl_xor_sync(0xffffffffu, w, 8);
+                if (r < tile.count) {
+                    *reinterpret_cast<uint32_t *>(smem_b + s * B_BYTES + code_place(r, lane)) = codes;
+                    if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(smem_sb + s * SB_BYTES + scale_place(r, lane >> 2) - kCodeBytes) = w;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < kWords<X>; ++i) v[j][i] = next[j][i];
         }
         fence_proxy_async_smem();  // what the tensor cores read they read through the asynchronous proxy
         __syncwarp();
         if (lane == 0) mbar_arrive_many(smem_u32(full_bar + s), (uint32_t)every);
     }
-    if (a.status != nullptr) {
-        const uint32_t flags = (odd ? 1u << Q8_ERR_SCALE : 0u) | (bad ? 1u << Q8_ERR_INDEX : 0u);
-        if (flags != 0) atomicOr(a.status, (int32_t)flags);
-    }
+    if (odd && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_SCALE);
     return true;
 }
 
@@ -668,7 +652,11 @@ cudaError_t launch_shape(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, 
 
 }  // namespace
 
-bool mx4_fused_preferred(int64_t M, int64_t E, bool grouped) { return grouped ? M <= 16 * E : M <= kFusedTokens; }
+// One launch instead of two, against tokens that every CTA reads and rounds itself, behind the weights that fill the way into its SM: about
+// 1 us for every four tokens and 8 stages.  (Fused / not, us, replayed and then called from Python: 1 x 1024 -> 4096 4.0 / 5.0 and 4.3 / 6.9, 16 x 1024 ->
+// 4096 5.5 / 4.8 and 5.7 / 6.9, 32 x 1024 -> 4096 7.4 / 4.9 and 7.6 / 7.1, 4 x 4096 -> 16384 8.4 / 9.8 and 8.5 / 9.9, 8 x 4096 -> 16384 10.2 / 9.7 and
+// 10.5 / 9.8, 4 x 8192 -> 8192 10.6 / 11.8 and 10.9 / 12.0.)
+bool mx4_fused_preferred(int64_t M, int64_t K) { return M <= 4 || (M <= kFusedTokens && M * K <= 16384); }
 
 cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s)
 {

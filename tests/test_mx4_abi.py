@@ -23,7 +23,7 @@ def test_sizes(lib):
     assert q8.q8_mx4_bytes(1, -1, 4) == q8.q8_mx4_bytes(1, 4, 0) == q8.q8_mx4_bytes(1 << 30, 4, 4) == 0
     assert q8.q8_mx4_linear_workspace_bytes(3, 64) == 0 and q8.q8_mx4_linear_workspace_bytes(130, 300) == 2 * 2 * 17408
     assert q8.q8_mx4_linear_grouped_workspace_bytes(300, 7, 64) == (2 + 7) * 17408
-    assert q8.q8_mx4_linear_grouped_workspace_bytes(4, 1000, 64) == 0
+    assert q8.q8_mx4_linear_grouped_workspace_bytes(4, 1000, 64) == 4 * 17408
     assert q8.q8_mx4_linear_grouped_workspace_bytes(4, 1025, 64) == 0
 
 
@@ -55,7 +55,7 @@ def fake(lib, X=FAKE, t=0, R=4, K=64, ld=64, out=FAKE, ldo=64, word=None):
 @pytest.mark.parametrize("call,arguments,status", [
     *[(linear, {k: None, "M": 130}, q8.Q8_ERR_NULL) for k in ("X", "Wq", "Y", "ws")],
     *[(linear_q, {k: None}, q8.Q8_ERR_NULL) for k in ("Xq", "Wq", "Y")],
-    *[(grouped, {k: None, "T": 300, "x_rows": 300}, q8.Q8_ERR_NULL) for k in ("X", "offsets", "Wq", "Y", "ws")],
+    *[(grouped, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "offsets", "Wq", "Y", "ws")],
     *[(quantize, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "out")],
     *[(dequantize, {k: None}, q8.Q8_ERR_NULL) for k in ("Y", "T")],
     *[(fake, {k: None}, q8.Q8_ERR_NULL) for k in ("X", "out")],
@@ -76,7 +76,7 @@ def fake(lib, X=FAKE, t=0, R=4, K=64, ld=64, out=FAKE, ldo=64, word=None):
     *[(grouped, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("X", 2), ("rows", 2), ("offsets", 2), ("Wq", 8), ("bias", 2), ("Y", 2), ("ws", 128))],
     (linear, {"xt": 1, "X": FAKE + 1}, q8.Q8_ERR_ALIGN), (quantize, {"X": FAKE + 2}, q8.Q8_ERR_ALIGN), (quantize, {"out": FAKE + 4}, q8.Q8_ERR_ALIGN),
     (dequantize, {"T": FAKE + 4}, q8.Q8_ERR_ALIGN), (fake, {"out": FAKE + 1}, q8.Q8_ERR_ALIGN),
-    (linear, {"M": 130, "size": 2 * 17408 - 1}, q8.Q8_ERR_WORKSPACE), (grouped, {"T": 300, "x_rows": 300, "size": 5 * 17408 - 1}, q8.Q8_ERR_WORKSPACE),
+    (linear, {"M": 130, "size": 2 * 17408 - 1}, q8.Q8_ERR_WORKSPACE), (grouped, {"size": 3 * 17408 - 1}, q8.Q8_ERR_WORKSPACE),
     # nothing to do: never reaches the device
     *[(call, {k: 0}, q8.Q8_OK) for call in (linear, linear_q) for k in ("M", "N")], *[(grouped, {k: 0}, q8.Q8_OK) for k in ("T", "N", "E")],
     *[(quantize, {k: 0, "X": None}, q8.Q8_OK) for k in ("G", "R")], (dequantize, {"R": 0}, q8.Q8_OK), (fake, {"R": 0, "X": None}, q8.Q8_OK)])
