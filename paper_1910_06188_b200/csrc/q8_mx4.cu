@@ -51,7 +51,7 @@ __device__ __forceinline__ void store8(T *p, int valid, int vec, const float (&v
 
 // (Rows and tasks are counted in 32 bits: with 64-bit divisions the indices took as many instructions as the arithmetic.)
 template <typename T, int KIND>
-__global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs a, uint32_t tasks, uint32_t chunks, uint32_t row_lanes, int vec, int vec_out)
+__global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs a, uint32_t tasks, uint32_t chunks, uint32_t splits, uint32_t row_lanes, int vec, int vec_out)
 {
     constexpr int R = kRows<KIND>;
     constexpr bool kSlots = KIND == kSlots1 || KIND == kSlots4;
@@ -69,90 +69,116 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
         __syncthreads();
     }
     if (task >= tasks) return;
-    const uint32_t line = task / chunks, chunk = task - line * chunks;
+    const uint32_t line = task / splits, part = task - line * splits;  // a part of the tiles of a row: one, or every splits-th
     const int32_t rows = (int32_t)a.rows;
-    int32_t first, end = rows;
-    uint8_t *tile = nullptr;
-    uint32_t r0 = 0;
-    if (KIND == kMatrix) {  // the row r0 of a block of 128, r0 < row_lanes, and those 32, 64 and 96 further
-        const uint32_t block = line / row_lanes;
-        r0 = line - block * row_lanes;
-        uint32_t in_group = block;
-        first = 0;
-        if (a.groups > 1) {
-            const uint32_t blocks = (uint32_t)(rows + kTileRows - 1) / kTileRows, group = block / blocks;
-            in_group = block - group * blocks;
-            first = (int32_t)group * rows;
-            end = first + rows;
-        }
-        first += (int32_t)(in_group * kTileRows + r0);
-        tile = a.out + ((int64_t)block * chunks + chunk) * kTileBytes;
-    } else {
-        first = (int32_t)line * R;
-    }
-    const int32_t k0 = (int32_t)chunk * kChunk + lane * 8, valid = max(0, min(8, (int32_t)a.K - k0));
     bool odd = false;
-    uint32_t v[R][kWords<T>];
-    if (kSlots && a.index != nullptr) {
-        int32_t from[R];
-#pragma unroll
-        for (int j = 0; j < R; ++j) from[j] = first + j < end ? __ldg(a.index + first + j) : 0;
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const bool there = from[j] >= 0 && from[j] < a.x_rows;  // else it counts as a row of zeros
-            if (!there && first + j >= table.start[0] && first + j < table.start[a.E]) bad_index = true;
-            load8<T>(reinterpret_cast<const T *>(a.X) + from[j] * a.ld + k0, there && first + j < end ? valid : 0, vec, v[j]);
-        }
-    } else {
-        const T *x = reinterpret_cast<const T *>(a.X) + first * a.ld + k0;
-#pragma unroll
-        for (int j = 0; j < R; ++j, x += kRowStep * a.ld) load8<T>(x, first + j * kRowStep < end ? valid : 0, vec, v[j]);
-    }
-    uint32_t words[R];
-    int expert = 0;
-    if (kSlots) {  // the expert that owns the first slot: the last one that starts at or before it
-        int hi = a.E;
+    // The codes and scales of one row: the bytes of four blocks are gathered from every fourth of 16 lanes.
+    auto quantize_row = [&](const uint32_t (&v)[kWords<T>], uint32_t &word) {
+        uint32_t E;
+        const uint32_t codes = quantize8<T>(v, E, odd);
+        word = E << (8 * ((lane >> 2) & 3));
+        word |= __shfl_xor_sync(0xffffffffu, word, 4);
+        word |= __shfl_xor_sync(0xffffffffu, word, 8);
+        return codes;
+    };
+    if constexpr (kSlots) {
+        // R slots in a row; what a slot's index and expert say is worked out once for all of its tiles.
+        const int32_t first = (int32_t)line * R;
+        int expert = 0, hi = a.E;  // the expert that owns the first slot: the last one that starts at or before it
         while (expert < hi) {
             const int mid = (expert + hi) >> 1;
             if (table.start[mid + 1] <= first) expert = mid + 1;
             else hi = mid;
         }
-    }
+        const T *x[R];
+        uint8_t *to[R];
+        bool there[R];
+        uint32_t r[R];
 #pragma unroll
-    for (int j = 0; j < R; ++j) {
-        const int32_t row = first + j * kRowStep;
-        uint32_t E;
-        const uint32_t codes = quantize8<T>(v[j], E, odd);
-        if (KIND == kFake) {
-            if (row < end) {
-                float back[8];
-                unpack_e2m1(codes, back);
-                const float s = scale_value(E);
+        for (int j = 0; j < R; ++j) {
+            const int32_t slot = first + j;
+            int64_t from = slot;
+            if (a.index != nullptr && slot < rows) from = __ldg(a.index + slot);
+            while (expert < a.E && table.start[expert + 1] <= slot) ++expert;
+            const bool owned = slot < rows && expert < a.E && slot >= table.start[expert];
+            there[j] = owned && from >= 0 && from < a.x_rows;  // else it counts as a row of zeros
+            bad_index |= owned && !there[j];
+            x[j] = reinterpret_cast<const T *>(a.X) + (there[j] ? from : 0) * a.ld + lane * 8;
+            const uint32_t in_expert = owned ? (uint32_t)(slot - table.start[expert]) : 0u;
+            r[j] = in_expert % kTileRows;
+            to[j] = owned ? a.out + (int64_t)(table.block[expert] + in_expert / kTileRows) * chunks * kTileBytes : nullptr;
+        }
+        uint32_t v[R][kWords<T>], next[R][kWords<T>];
+        auto load = [&](uint32_t chunk, uint32_t (&w)[R][kWords<T>]) {
+            const int32_t valid = max(0, min(8, (int32_t)a.K - (int32_t)chunk * kChunk - lane * 8));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) back[i] = __fmul_rn(back[i], s);
-                store8(reinterpret_cast<T *>(a.Xhat) + row * a.ldo + k0, valid, vec_out, back);
+            for (int j = 0; j < R; ++j) load8<T>(x[j] + (int64_t)chunk * kChunk, there[j] ? valid : 0, vec, w[j]);
+        };
+        load(part, v);
+        for (uint32_t chunk = part; chunk < chunks; chunk += splits) {
+            if (chunk + splits < chunks) load(chunk + splits, next);
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                uint32_t word;
+                const uint32_t codes = quantize_row(v[j], word);
+                if (to[j] != nullptr) {
+                    uint8_t *tile = to[j] + (int64_t)chunk * kTileBytes;
+                    *reinterpret_cast<uint32_t *>(tile + code_place((int)r[j], lane)) = codes;
+                    if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(tile + scale_place((int)r[j], lane >> 2)) = word;
+                }
             }
-            continue;
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+#pragma unroll
+                for (int i = 0; i < kWords<T>; ++i) v[j][i] = next[j][i];
         }
-        // the bytes of four blocks, gathered from every fourth of 16 lanes
-        uint32_t w = E << (8 * ((lane >> 2) & 3));
-        w |= __shfl_xor_sync(0xffffffffu, w, 4);
-        w |= __shfl_xor_sync(0xffffffffu, w, 8);
-        words[j] = w;
-        if (KIND == kMatrix) {
-            if (row < end) *reinterpret_cast<uint32_t *>(tile + code_place((int)r0, lane) + 32 * 128 * j) = codes;
-        } else if (row < end) {
-            while (expert < a.E && table.start[expert + 1] <= row) ++expert;
-            if (expert < a.E && row >= table.start[expert]) {
-                const uint32_t in_expert = (uint32_t)(row - table.start[expert]), r = in_expert % kTileRows;
-                uint8_t *t = a.out + ((int64_t)(table.block[expert] + in_expert / kTileRows) * chunks + chunk) * kTileBytes;
-                *reinterpret_cast<uint32_t *>(t + code_place((int)r, lane)) = codes;
-                if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(t + scale_place((int)r, lane >> 2)) = w;
+    } else {
+        int32_t first, end = rows;
+        uint8_t *tile = nullptr;
+        uint32_t r0 = 0;
+        if (KIND == kMatrix) {  // the row r0 of a block of 128, r0 < row_lanes, and those 32, 64 and 96 further
+            const uint32_t block = line / row_lanes;
+            r0 = line - block * row_lanes;
+            uint32_t in_group = block;
+            first = 0;
+            if (a.groups > 1) {
+                const uint32_t blocks = (uint32_t)(rows + kTileRows - 1) / kTileRows, group = block / blocks;
+                in_group = block - group * blocks;
+                first = (int32_t)group * rows;
+                end = first + rows;
+            }
+            first += (int32_t)(in_group * kTileRows + r0);
+            tile = a.out + ((int64_t)block * chunks + part) * kTileBytes;
+        } else {
+            first = (int32_t)line * R;
+        }
+        const int32_t k0 = (int32_t)part * kChunk + lane * 8, valid = max(0, min(8, (int32_t)a.K - k0));
+        uint32_t v[R][kWords<T>], words[R];
+        const T *x = reinterpret_cast<const T *>(a.X) + first * a.ld + k0;
+#pragma unroll
+        for (int j = 0; j < R; ++j, x += kRowStep * a.ld) load8<T>(x, first + j * kRowStep < end ? valid : 0, vec, v[j]);
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int32_t row = first + j * kRowStep;
+            if constexpr (KIND == kFake) {
+                uint32_t E;
+                const uint32_t codes = quantize8<T>(v[j], E, odd);
+                if (row < end) {
+                    float back[8];
+                    unpack_e2m1(codes, back);
+                    const float s = scale_value(E);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) back[i] = __fmul_rn(back[i], s);
+                    store8(reinterpret_cast<T *>(a.Xhat) + row * a.ldo + k0, valid, vec_out, back);
+                }
+            } else {
+                const uint32_t codes = quantize_row(v[j], words[j]);
+                if (row < end) *reinterpret_cast<uint32_t *>(tile + code_place((int)r0, lane) + 32 * 128 * j) = codes;
             }
         }
-    }
-    if constexpr (KIND == kMatrix) {
-        if ((lane & 15) == 0) *reinterpret_cast<uint4 *>(tile + scale_place((int)r0, lane >> 2)) = make_uint4(words[0], words[1], words[2], words[3]);
+        if constexpr (KIND == kMatrix) {
+            if ((lane & 15) == 0) *reinterpret_cast<uint4 *>(tile + scale_place((int)r0, lane >> 2)) = make_uint4(words[0], words[1], words[2], words[3]);
+        }
     }
     if (a.status != nullptr) {
         const uint32_t flags = (odd ? 1u << Q8_ERR_SCALE : 0u) | (bad_index ? 1u << Q8_ERR_INDEX : 0u);
@@ -205,11 +231,16 @@ template <typename T, int KIND>
 cudaError_t launch_kind(const Mx4QuantizeArgs &a, cudaStream_t s)
 {
     const int64_t chunks = ceil_div(a.K, kChunk), row_lanes = a.rows < 32 ? a.rows : 32;
-    const int64_t tasks = (KIND == kMatrix ? a.groups * ceil_div(a.rows, kTileRows) * row_lanes : ceil_div(a.rows, kRows<KIND>)) * chunks;
+    const int64_t lines = KIND == kMatrix ? a.groups * ceil_div(a.rows, kTileRows) * row_lanes : ceil_div(a.rows, kRows<KIND>);
+    int64_t splits = chunks;
+    if (KIND == kSlots4) {  // as many warps as the device holds, a warp as many tiles of its rows as that leaves
+        const int64_t room = 24 * sm_count() / lines;
+        splits = room < 1 ? 1 : room < chunks ? room : chunks;
+    }
     dim3 grid;
-    cudaError_t e = grid_of(tasks, &grid);
+    cudaError_t e = grid_of(lines * splits, &grid);
     if (e != cudaSuccess) return e;
-    return launch_overlapping_tail(mx4_quantize_kernel<T, KIND>, grid, dim3(kThreads), 0, s, a, tasks, chunks, row_lanes,
+    return launch_overlapping_tail(mx4_quantize_kernel<T, KIND>, grid, dim3(kThreads), 0, s, a, lines * splits, chunks, splits, row_lanes,
                                    value_alignment(a.X, a.ld, sizeof(T)), value_alignment(a.Xhat, a.ldo, sizeof(T)));
 }
 

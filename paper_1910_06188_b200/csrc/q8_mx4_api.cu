@@ -30,7 +30,7 @@ q8_status check_layer(int64_t M, int64_t N, int64_t K, int64_t E, int64_t ldy)
     if (M > kMaxRows || N > kMaxRows || K > kMaxK || E > kMaxExperts || ldy < N || ldy > kMaxPitch) return Q8_ERR_SHAPE;
     if (E > 0 && N > kMaxRows / E) return Q8_ERR_SHAPE;
     // tiles are counted in 32 bits
-    if (((M + 63) / 64 + E) * ((N + 127) / 128) > 0x7fffffff) return Q8_ERR_SHAPE;
+    if (((M + 63) / 64 + E) * ((N + 127) / 128) > 0x7fff0000) return Q8_ERR_SHAPE;
     return Q8_OK;
 }
 

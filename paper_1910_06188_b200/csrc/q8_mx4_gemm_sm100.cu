@@ -41,6 +41,11 @@ constexpr int kFusedStages = 9;
 constexpr int kFusedTokens = 32;                // of a tile
 constexpr int kStoreRows = 32;               // tokens of a staged block of 32 features
 
+// A tile: expert and its first row block of tokens, the tile's first token (in the expert and as a row of Y), how many it has, its first feature.
+struct __align__(16) Tile {
+    int32_t expert, block, first, row, count, feature, pad[2];
+};
+constexpr int kListed = 64;  // tiles of a CTA that are worked out at the start
 template <int CTAS, int BN, int EW, bool STAGED, int SIZE, bool FUSED>
 struct Cfg {
     static constexpr int kThreads = 96 + 32 * EW;
@@ -48,14 +53,14 @@ struct Cfg {
     static constexpr int kSbBytes = (FUSED ? 1 : 2) * kScaleBytes;  // two row blocks: a tile of 192 may start in the middle of one
     static constexpr int kStageBytes = kTileBytes + kBBytes + kSbBytes;
     static constexpr int kStagingBytes = STAGED ? EW * kStoreRows * 32 * SIZE : 0;
-    static constexpr int kTableBytes = 3 * (kMaxExperts + 1) * 4 + 4;
+    static constexpr int kTableBytes = 3 * (kMaxExperts + 1) * 4 + 4 + kListed * (int)sizeof(Tile);
     static constexpr int kBudget = 227 * 1024 - 1024 - kTableBytes - kStagingBytes - 512;
     static constexpr int kStages = FUSED ? kFusedStages : kBudget / kStageBytes > 8 ? 8 : kBudget / kStageBytes;
     // Two accumulators of 256 columns leave no room for the scales: they share 48 columns, which the epilogue empties first.
     static constexpr int kAccStride = BN == 256 ? 512 - 2 * kScaleCols - 256 : BN;
     static constexpr int kScaleCol0 = kAccStride + BN;
     static constexpr int kTmemCols = kScaleCol0 + 2 * kScaleCols <= 128 ? 128 : kScaleCol0 + 2 * kScaleCols <= 256 ? 256 : 512;
-    static constexpr int kBarrierBytes = (2 * kStages + 2 * kAccStages + 1) * 8 + 16;
+    static constexpr int kBarrierBytes = (2 * kStages + 2 * kAccStages + 1) * 8 + 32;
     static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStagingBytes + kTableBytes + kBarrierBytes;
     static_assert(kScaleCol0 + 2 * kScaleCols <= 512, "TMEM columns");
     static_assert(kSmemBytes <= 232448 && kStages >= 3, "shared memory budget");
@@ -121,10 +126,6 @@ struct Plan {
     int32_t x_vec;     // bytes that loads of the tokens' values may take at once
 };
 
-// A tile: expert and its first row block of tokens, the tile's first token (in the expert and as a row of Y), how many it has, its first feature.
-struct Tile {
-    int32_t expert, block, first, row, count, feature;
-};
 // Tile t, those of an expert ordered features first; false behind the last one.  (A plain product needs no table.)
 template <int TILE_M>
 __device__ __forceinline__ bool find_tile(int32_t t, const ExpertTable &table, const Mx4GemmArgs &a, const Plan &p, Tile &out)
@@ -223,13 +224,13 @@ __device__ __forceinline__ bool quantize_tokens(const Mx4GemmArgs &a, const Plan
 
 template <int CTAS, int BN, int EW, bool STAGED, typename T, typename X>
 __global__ void __launch_bounds__(96 + 32 * EW, 1)
-mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_x32, const __grid_constant__ CUtensorMap map_x16,
+mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_x64, const __grid_constant__ CUtensorMap map_x32,
                 const __grid_constant__ CUtensorMap map_s, const __grid_constant__ CUtensorMap map_y, Mx4GemmArgs a, Plan plan)
 {
     constexpr bool FUSED = !std::is_void<X>::value;
     using C = Cfg<CTAS, BN, EW, STAGED, sizeof(T), FUSED>;
     constexpr int TILE_M = kTileRows * CTAS;
-    constexpr int kStep = 16 * CTAS;  // widths of tiles are multiples of this
+    constexpr int kStep = CTAS == 2 ? 64 : 16;  // widths of tiles are multiples of this
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *smem_a = smem;  // codes and scales of the weights
@@ -247,6 +248,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     table.start = reinterpret_cast<int32_t *>(tmem_slot + 4);
     table.block = table.start + kMaxExperts + 1;
     table.tile = table.block + kMaxExperts + 1;
+    Tile *list = reinterpret_cast<Tile *>((reinterpret_cast<uintptr_t>(table.tile + kMaxExperts + 1) + 15) & ~uintptr_t(15));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;
@@ -267,11 +269,27 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         if (CTAS == 2) tmem_alloc_pair(smem_u32(tmem_slot), C::kTmemCols);
         else tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
     }
-    if (warp == 2 && a.offsets != nullptr) {
-        if (!a.behind_quantise) grid_dependency_wait();
-        const bool bad = build_expert_table(table, a.offsets, a.E, (int32_t)a.M, plan.tile_n, plan.tiles_m);
-        if (bad && lane == 0 && blockIdx.x == 0 && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_INDEX);
+    const int32_t first_tile = blockIdx.x / CTAS, tile_step = gridDim.x / CTAS;
+    if (warp == 2) {
+        if (a.offsets != nullptr) {
+            if (!a.behind_quantise) grid_dependency_wait();
+            const bool bad = build_expert_table(table, a.offsets, a.E, (int32_t)a.M, plan.tile_n, plan.tiles_m);
+            if (bad && lane == 0 && blockIdx.x == 0 && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_INDEX);
+        }
+        // A lane a tile: looked up by every role for every tile, between two of them, they took 400 cycles each time.
+#pragma unroll 1
+        for (int i = lane; i < kListed; i += 32) {
+            Tile found;
+            if (!find_tile<TILE_M>(first_tile + i * tile_step, table, a, plan, found)) found.count = 0;
+            list[i] = found;
+        }
     }
+    // The i-th tile of this CTA; false behind the last one.
+    auto get_tile = [&](int32_t i, Tile &tile) {
+        if (i >= kListed) return find_tile<TILE_M>(first_tile + i * tile_step, table, a, plan, tile);
+        tile = list[i];
+        return tile.count > 0;
+    };
     // A plain product's weight producer, which made the barriers and needs neither the table nor TMEM, goes ahead without the others.
     tc_fence_before();
     __syncwarp();
@@ -282,7 +300,6 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(tmem_slot);  // (not yet there for that producer, which does not use it)
     grid_dependency_release_next(true);
 
-    const int32_t first_tile = blockIdx.x / CTAS, tile_step = gridDim.x / CTAS;
     Tile tile;
     auto width_of = [&](const Tile &t) { return (t.count + kStep - 1) / kStep * kStep; };
     if (warp == 0 || (warp == 2 && !FUSED)) {
@@ -300,7 +317,9 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             uint32_t phase = 0;
             int64_t issued = 0;
             bool ok = true, waited = false;
-            for (int32_t t = first_tile; ok && find_tile<TILE_M>(t, table, a, plan, tile); t += tile_step) {
+            // (a plain product's weight producer does not wait for the list)
+            const bool ahead = CTAS == 1 && a.offsets == nullptr && weights;
+            for (int32_t i = 0; ok && (ahead ? find_tile<TILE_M>(first_tile + i * tile_step, table, a, plan, tile) : get_tile(i, tile)); ++i) {
                 const int width = width_of(tile), mine = width / CTAS;
                 const int64_t w_tile = ((int64_t)tile.expert * plan.w_blocks + tile.feature / kTileRows + rank) * plan.num_kb;
                 const int first = tile.first + (int)rank * mine, sub = first % kTileRows;
@@ -343,14 +362,16 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                             tma_load_2d_pair(smem_u32(smem_a + s * kTileBytes), &map_w, 0, (int32_t)(w_tile + kb) * kRowsPerTile, fb_leader);
                             tma_load_2d_pair(dst_s, &map_s, 0, (int32_t)(s_tile + kb) * kRowsPerTile + kTileRows, fb_leader);
                         } else {
+                            // 32, 64, 96 or 128 rows, in a box or two that end with the row block or with the tile's half
                             if (mine == kTileRows) {
                                 tma_load_2d_pair(dst_b, &map_x, 0, (int32_t)(x_tile + kb) * kRowsPerTile, fb_leader);
                             } else {
-                                const int box = mine % 32 == 0 ? 32 : 16;
+                                int box;
                                 for (int r = 0; r < mine; r += box) {
                                     const bool second = r >= in_first;
                                     const int32_t at = (int32_t)(x_tile + kb + (second ? plan.num_kb : 0)) * kRowsPerTile + (second ? r - in_first : sub + r);
-                                    tma_load_2d_pair(dst_b + r * 128, box == 32 ? &map_x32 : &map_x16, 0, at, fb_leader);
+                                    box = (second ? mine : in_first) - r >= 64 ? 64 : 32;
+                                    tma_load_2d_pair(dst_b + r * 128, box == 64 ? &map_x64 : &map_x32, 0, at, fb_leader);
                                 }
                             }
                             if (two_scales)
@@ -391,7 +412,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             const uint32_t scale_sum = 2 * scale_col + kScaleCols;
             const int last_blocks = plan.k_blocks - (plan.num_kb - 1) * (kTileK / kBlock);  // of the last stage
             bool ok = true;
-            for (int32_t t = first_tile; ok && find_tile<TILE_M>(t, table, a, plan, tile); t += tile_step) {
+            for (int32_t i = 0; ok && get_tile(i, tile); ++i) {
                 // the tile before last has left this accumulator, or the last one the columns that it shares with it
                 constexpr bool kShared = C::kAccStride < BN;
                 ok = wait_for(smem_u32(tmem_empty_bar + (kShared ? as ^ 1 : as)), kShared && as == 1 ? aphase : aphase ^ 1u, abort_flag, a.status);
@@ -468,7 +489,7 @@ mx4_gemm_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         uint32_t aphase = 0;
         bool waited = false;
         int32_t stage0 = 0;  // stages of the tiles before
-        for (int32_t t = first_tile; find_tile<TILE_M>(t, table, a, plan, tile); t += tile_step) {
+        for (int32_t n = 0; get_tile(n, tile); ++n) {
             if constexpr (FUSED) {
                 if (!waited) grid_dependency_wait();
                 waited = true;
@@ -604,11 +625,11 @@ cudaError_t launch_typed(const Mx4GemmArgs &a, Plan plan, int64_t tiles, cudaStr
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
-    CUtensorMap mw = {}, mx = {}, mx32 = {}, mx16 = {}, ms = {}, my = {};
+    CUtensorMap mw = {}, mx = {}, mx64 = {}, mx32 = {}, ms = {}, my = {};
     if (CTAS == 2) {
         const int64_t w_tiles = (int64_t)a.E * plan.w_blocks * plan.num_kb;
         const int64_t x_tiles = (a.offsets != nullptr ? most_row_blocks(a.M, a.E) : ceil_div(a.M, kTileRows)) * plan.num_kb;
-        if (!tiles_map(&mw, a.W, w_tiles, kTileBytes / 128) || !tiles_map(&mx, a.X, x_tiles, kTileRows) || !tiles_map(&mx32, a.X, x_tiles, 32) || !tiles_map(&mx16, a.X, x_tiles, 16) ||
+        if (!tiles_map(&mw, a.W, w_tiles, kTileBytes / 128) || !tiles_map(&mx, a.X, x_tiles, kTileRows) || !tiles_map(&mx64, a.X, x_tiles, 64) || !tiles_map(&mx32, a.X, x_tiles, 32) ||
             !tiles_map(&ms, a.X, x_tiles, kScaleBytes / 128))
             return cudaErrorInvalidValue;
     }
@@ -637,7 +658,7 @@ cudaError_t launch_typed(const Mx4GemmArgs &a, Plan plan, int64_t tiles, cudaStr
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = CTAS == 2 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, mw, mx, mx32, mx16, ms, my, a, plan);
+    return cudaLaunchKernelEx(&cfg, kernel, mw, mx, mx64, mx32, ms, my, a, plan);
 }
 
 template <int CTAS, int BN, int EW, bool STAGED, typename X = void>
@@ -690,7 +711,7 @@ cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s)
     // widest tile that still gives every SM one
     p.tile_n = 192;
     for (int n : {128, 64})
-        if (mean <= n || (a.E == 1 && ceil_div(a.M, p.tile_n) * p.tiles_m < sms)) p.tile_n = n;
+        if (mean <= n || (ceil_div(a.M, p.tile_n) + extra / 2) * p.tiles_m < sms) p.tile_n = n;
     const int64_t tiles = (ceil_div(a.M, p.tile_n) + extra) * p.tiles_m;  // at most
     if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
     return p.tile_n == 64 ? launch_shape<1, 64, 8, false>(a, p, tiles, s)
