@@ -21,36 +21,80 @@ enum Kind { kMatrix, kFake, kSlots1, kSlots4 };
 template <int KIND>
 constexpr int kRows = KIND == kSlots1 ? 1 : 4;
 
-template <typename T>
-__device__ __forceinline__ void store8(T *p, int valid, int vec, const float (&v)[8])
+// The other way: columns k0 .. k0 + 7 of a row from every lane.  Unaligned, a lane stores the aligned 16 or 32 bytes that end with its first
+// values and begin with the last ones of the lane before; the first and last lanes and those at the row's end store value by value.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void store_columns(T *row, int32_t k0, int32_t K, int vec, const float (&v)[8])
 {
-    if (vec >= 16 && valid >= 8) {
-        if (sizeof(T) == 4 && vec >= 32) {
-            asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                         ::"l"(p), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
-                         "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
-                         : "memory");
-        } else if constexpr (sizeof(T) == 4) {
-            __stcs(reinterpret_cast<float4 *>(p), make_float4(v[0], v[1], v[2], v[3]));
-            __stcs(reinterpret_cast<float4 *>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
-        } else {
-            uint32_t w[4];
+    constexpr int N = kWords<T>;
+    uint32_t w[N];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const T h[2] = {from_float<T>(v[2 * i]), from_float<T>(v[2 * i + 1])};
-                memcpy(&w[i], h, 4);
-            }
-            __stcs(reinterpret_cast<uint4 *>(p), make_uint4(w[0], w[1], w[2], w[3]));
+    for (int i = 0; i < N; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            w[i] = __float_as_uint(v[i]);
+        } else {
+            const T h[2] = {from_float<T>(v[2 * i]), from_float<T>(v[2 * i + 1])};
+            memcpy(&w[i], h, 4);
+        }
+    }
+    if constexpr (ALIGNED) {
+        T *p = row + k0;
+        if (k0 + 8 > K || vec == 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k0 + i < K) p[i] = from_float<T>(v[i]);
+        } else if (sizeof(T) == 4 && vec >= 32) {
+            asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                         ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[N - 4]), "r"(w[N - 3]), "r"(w[N - 2]), "r"(w[N - 1])
+                         : "memory");
+        } else {
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) __stcs(reinterpret_cast<uint4 *>(p) + i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
         }
     } else {
+        const int lane = threadIdx.x & 31;
+        const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u, shift = 16u - off;  // bytes
+        uint32_t z[N + 5];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < valid) p[i] = from_float<T>(v[i]);
+        for (int i = 0; i < 4; ++i) z[i] = __shfl_up_sync(0xffffffffu, w[N - 4 + i], 1);
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[4 + i] = w[i];
+        z[N + 4] = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = shift & 16 ? z[i + 4] : z[i];
+#pragma unroll
+        for (int i = N; i < N + 4; ++i) z[i] = shift & 16 ? 0u : z[i];
+#pragma unroll
+        for (int i = 0; i < N + 2; ++i) z[i] = shift & 8 ? z[i + 2] : z[i];
+#pragma unroll
+        for (int i = 0; i < N + 1; ++i) z[i] = shift & 4 ? z[i + 1] : z[i];
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] = __funnelshift_r(z[i], z[i + 1], (shift & 2) * 8);
+        }
+        const int32_t before = (int32_t)(off / sizeof(T)), first = k0 - before;
+        if ((lane > 0 || off == 0) && first + 8 <= K) {
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) __stcs(reinterpret_cast<uint4 *>(row + first) + i, make_uint4(z[4 * i], z[4 * i + 1], z[4 * i + 2], z[4 * i + 3]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                T one;
+                const uint32_t bits = sizeof(T) == 4 ? z[i % N] : z[i / 2] >> (16 * (i & 1));
+                memcpy(&one, &bits, sizeof(T));
+                if (first + i < K && (lane > 0 || first + i >= k0)) row[first + i] = one;
+            }
+        }
+        if (lane == 31) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i >= 8 - before && k0 + i < K) row[k0 + i] = from_float<T>(v[i]);
+        }
     }
 }
 
 // (Rows and tasks are counted in 32 bits: with 64-bit divisions the indices took as many instructions as the arithmetic.)
-template <typename T, int KIND>
+template <typename T, int KIND, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs a, uint32_t tasks, uint32_t chunks, uint32_t splits, uint32_t row_lanes, int vec, int vec_out)
 {
     constexpr int R = kRows<KIND>;
@@ -73,9 +117,10 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     const int32_t rows = (int32_t)a.rows;
     bool odd = false;
     // The codes and scales of one row: the bytes of four blocks are gathered from every fourth of 16 lanes.
-    auto quantize_row = [&](const uint32_t (&v)[kWords<T>], uint32_t &word) {
+    auto quantize_row = [&](Columns<T, ALIGNED> &v, uint32_t &word) {
         uint32_t E;
-        const uint32_t codes = quantize8<T>(v, E, odd);
+        v.settle();
+        const uint32_t codes = quantize8<T>(v.w, E, odd);
         word = E << (8 * ((lane >> 2) & 3));
         word |= __shfl_xor_sync(0xffffffffu, word, 4);
         word |= __shfl_xor_sync(0xffffffffu, word, 8);
@@ -103,16 +148,15 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
             const bool owned = slot < rows && expert < a.E && slot >= table.start[expert];
             there[j] = owned && from >= 0 && from < a.x_rows;  // else it counts as a row of zeros
             bad_index |= owned && !there[j];
-            x[j] = reinterpret_cast<const T *>(a.X) + (there[j] ? from : 0) * a.ld + lane * 8;
+            x[j] = reinterpret_cast<const T *>(a.X) + (there[j] ? from : 0) * a.ld;
             const uint32_t in_expert = owned ? (uint32_t)(slot - table.start[expert]) : 0u;
             r[j] = in_expert % kTileRows;
             to[j] = owned ? a.out + (int64_t)(table.block[expert] + in_expert / kTileRows) * chunks * kTileBytes : nullptr;
         }
-        uint32_t v[R][kWords<T>], next[R][kWords<T>];
-        auto load = [&](uint32_t chunk, uint32_t (&w)[R][kWords<T>]) {
-            const int32_t valid = max(0, min(8, (int32_t)a.K - (int32_t)chunk * kChunk - lane * 8));
+        Columns<T, ALIGNED> v[R], next[R];
+        auto load = [&](uint32_t chunk, Columns<T, ALIGNED> (&w)[R]) {
 #pragma unroll
-            for (int j = 0; j < R; ++j) load8<T>(x[j] + (int64_t)chunk * kChunk, there[j] ? valid : 0, vec, w[j]);
+            for (int j = 0; j < R; ++j) w[j].load(x[j], (int32_t)chunk * kChunk + lane * 8, (int32_t)a.K, there[j], vec);
         };
         load(part, v);
         for (uint32_t chunk = part; chunk < chunks; chunk += splits) {
@@ -128,9 +172,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
                 }
             }
 #pragma unroll
-            for (int j = 0; j < R; ++j)
-#pragma unroll
-                for (int i = 0; i < kWords<T>; ++i) v[j][i] = next[j][i];
+            for (int j = 0; j < R; ++j) v[j] = next[j];
         }
     } else {
         int32_t first, end = rows;
@@ -152,25 +194,24 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
         } else {
             first = (int32_t)line * R;
         }
-        const int32_t k0 = (int32_t)part * kChunk + lane * 8, valid = max(0, min(8, (int32_t)a.K - k0));
-        uint32_t v[R][kWords<T>], words[R];
-        const T *x = reinterpret_cast<const T *>(a.X) + first * a.ld + k0;
+        const int32_t k0 = (int32_t)part * kChunk + lane * 8;
+        Columns<T, ALIGNED> v[R];
+        uint32_t words[R];
+        const T *x = reinterpret_cast<const T *>(a.X) + first * a.ld;
 #pragma unroll
-        for (int j = 0; j < R; ++j, x += kRowStep * a.ld) load8<T>(x, first + j * kRowStep < end ? valid : 0, vec, v[j]);
+        for (int j = 0; j < R; ++j, x += kRowStep * a.ld) v[j].load(x, k0, (int32_t)a.K, first + j * kRowStep < end, vec);
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             const int32_t row = first + j * kRowStep;
             if constexpr (KIND == kFake) {
                 uint32_t E;
-                const uint32_t codes = quantize8<T>(v[j], E, odd);
-                if (row < end) {
-                    float back[8];
-                    unpack_e2m1(codes, back);
-                    const float s = scale_value(E);
+                float back[8];
+                v[j].settle();
+                unpack_e2m1(quantize8<T>(v[j].w, E, odd), back);
+                const float s = scale_value(E);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) back[i] = __fmul_rn(back[i], s);
-                    store8(reinterpret_cast<T *>(a.Xhat) + row * a.ldo + k0, valid, vec_out, back);
-                }
+                for (int i = 0; i < 8; ++i) back[i] = __fmul_rn(back[i], s);
+                if (row < end) store_columns<T, ALIGNED>(reinterpret_cast<T *>(a.Xhat) + row * a.ldo, k0, (int32_t)a.K, vec_out, back);
             } else {
                 const uint32_t codes = quantize_row(v[j], words[j]);
                 if (row < end) *reinterpret_cast<uint32_t *>(tile + code_place((int)r0, lane) + 32 * 128 * j) = codes;
@@ -186,7 +227,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     }
 }
 
-template <typename T>
+template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads)
 mx4_dequantize_kernel(const uint8_t *tiles, uint32_t groups, uint32_t rows, int32_t K, T *Y, int64_t ldy, uint32_t tasks, uint32_t chunks, int vec)
 {
@@ -196,8 +237,6 @@ mx4_dequantize_kernel(const uint8_t *tiles, uint32_t groups, uint32_t rows, int3
     if (task >= tasks) return;
     const uint32_t line = task / chunks, chunk = task - line * chunks, first = line * 4, all = groups * rows;
     const int32_t k0 = (int32_t)chunk * kChunk + lane * 8;
-    if (k0 >= K) return;
-    const int valid = min(8, K - k0);
     const uint32_t blocks = (rows + kTileRows - 1) / kTileRows;
     uint32_t c[4], E[4];
 #pragma unroll
@@ -207,7 +246,7 @@ mx4_dequantize_kernel(const uint8_t *tiles, uint32_t groups, uint32_t rows, int3
         c[j] = __ldg(reinterpret_cast<const uint32_t *>(tile + code_place((int)(r % kTileRows), lane)));
         E[j] = __ldg(tile + scale_place((int)(r % kTileRows), lane >> 2));
     }
-    T *y = Y + first * ldy + k0;
+    T *y = Y + first * ldy;
 #pragma unroll
     for (uint32_t j = 0; j < 4; ++j, y += ldy) {
         if (first + j >= all) break;
@@ -216,7 +255,7 @@ mx4_dequantize_kernel(const uint8_t *tiles, uint32_t groups, uint32_t rows, int3
         const float s = E[j] == 255 ? __uint_as_float(0x7fc00000u) : scale_value(E[j]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], s);
-        store8(y, valid, vec, v);
+        store_columns<T, ALIGNED>(y, k0, K, vec, v);
     }
 }
 
@@ -226,6 +265,8 @@ cudaError_t grid_of(int64_t tasks, dim3 *grid)
     *grid = dim3((unsigned)ceil_div(tasks, kWarps));
     return cudaSuccess;
 }
+
+bool worth_shifting(int64_t rows, int64_t K) { return K >= 256 && rows * K >= (1 << 20); }
 
 template <typename T, int KIND>
 cudaError_t launch_kind(const Mx4QuantizeArgs &a, cudaStream_t s)
@@ -240,8 +281,10 @@ cudaError_t launch_kind(const Mx4QuantizeArgs &a, cudaStream_t s)
     dim3 grid;
     cudaError_t e = grid_of(lines * splits, &grid);
     if (e != cudaSuccess) return e;
-    return launch_overlapping_tail(mx4_quantize_kernel<T, KIND>, grid, dim3(kThreads), 0, s, a, lines * splits, chunks, splits, row_lanes,
-                                   value_alignment(a.X, a.ld, sizeof(T)), value_alignment(a.Xhat, a.ldo, sizeof(T)));
+    const int vec = value_alignment(a.X, a.ld, sizeof(T)), vec_out = value_alignment(a.Xhat, a.ldo, sizeof(T));
+    auto kernel = KIND == kSlots1 || KIND == kSlots4 || (vec > 0 && vec_out > 0) || !worth_shifting(a.groups * a.rows, a.K) ? mx4_quantize_kernel<T, KIND, true>
+                                                                                                                     : mx4_quantize_kernel<T, KIND, false>;
+    return launch_overlapping_tail(kernel, grid, dim3(kThreads), 0, s, a, lines * splits, chunks, splits, row_lanes, vec, vec_out);
 }
 
 template <typename T>
@@ -251,6 +294,14 @@ cudaError_t launch_type(const Mx4QuantizeArgs &a, cudaStream_t s)
     if (a.offsets == nullptr) return launch_kind<T, kMatrix>(a, s);
     // one row to a warp while that leaves room for every warp at once
     return a.rows * ceil_div(a.K, kChunk) <= 16 * sm_count() ? launch_kind<T, kSlots1>(a, s) : launch_kind<T, kSlots4>(a, s);
+}
+
+template <typename T>
+cudaError_t launch_back(T *Y, int64_t ldy, dim3 grid, cudaStream_t s, const uint8_t *tiles, int64_t groups, int64_t rows, int64_t K, int64_t tasks, int64_t chunks)
+{
+    const int vec = value_alignment(Y, ldy, sizeof(T));
+    auto kernel = vec > 0 || !worth_shifting(groups * rows, K) ? mx4_dequantize_kernel<T, true> : mx4_dequantize_kernel<T, false>;
+    return launch_overlapping_tail(kernel, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, Y, ldy, tasks, chunks, vec);
 }
 
 }  // namespace
@@ -272,11 +323,10 @@ cudaError_t launch_mx4_dequantize(const uint8_t *tiles, int64_t groups, int64_t 
     dim3 grid;
     cudaError_t e = grid_of(tasks, &grid);
     if (e != cudaSuccess) return e;
-    const int vec = value_alignment(Y, ldy, dtype == Q8_F32 ? 4 : 2);
     switch (dtype) {
-        case Q8_F32: return launch_overlapping_tail(mx4_dequantize_kernel<float>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<float *>(Y), ldy, tasks, chunks, vec);
-        case Q8_F16: return launch_overlapping_tail(mx4_dequantize_kernel<__half>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<__half *>(Y), ldy, tasks, chunks, vec);
-        default: return launch_overlapping_tail(mx4_dequantize_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, s, tiles, groups, rows, K, static_cast<__nv_bfloat16 *>(Y), ldy, tasks, chunks, vec);
+        case Q8_F32: return launch_back(static_cast<float *>(Y), ldy, grid, s, tiles, groups, rows, K, tasks, chunks);
+        case Q8_F16: return launch_back(static_cast<__half *>(Y), ldy, grid, s, tiles, groups, rows, K, tasks, chunks);
+        default: return launch_back(static_cast<__nv_bfloat16 *>(Y), ldy, grid, s, tiles, groups, rows, K, tasks, chunks);
     }
 }
 

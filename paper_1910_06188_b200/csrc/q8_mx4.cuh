@@ -152,29 +152,94 @@ __device__ __forceinline__ float inverse_scale(uint32_t E) { return __uint_as_fl
 template <typename T>
 constexpr int kWords = sizeof(T) == 4 ? 8 : 4;
 
-// Eight values from column k0 on; those at or behind `valid` are 0.
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, int valid, int vec, uint32_t (&w)[kWords<T>])
+// `count` values from p on, those outside [from, to) left out as 0, into words.
+template <typename T, int WORDS>
+__device__ __forceinline__ void load_single(const T *p, int from, int to, uint32_t *w)
 {
-    if (sizeof(T) == 4 && vec >= 32 && valid >= 8) {
-        asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[kWords<T> - 4]), "=r"(w[kWords<T> - 3]), "=r"(w[kWords<T> - 2]), "=r"(w[kWords<T> - 1])
-                     : "l"(p));
-    } else if (vec >= 16 && valid >= 8) {
 #pragma unroll
-        for (int i = 0; i < kWords<T> / 4; ++i) {
-            const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
-            w[4 * i] = a.x; w[4 * i + 1] = a.y; w[4 * i + 2] = a.z; w[4 * i + 3] = a.w;
+    for (int i = 0; i < WORDS; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            w[i] = i >= from && i < to ? reinterpret_cast<const uint32_t *>(p)[i] : 0u;
+        } else {
+            const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+            const uint32_t lo = 2 * i >= from && 2 * i < to ? h[2 * i] : 0u, hi = 2 * i + 1 >= from && 2 * i + 1 < to ? h[2 * i + 1] : 0u;
+            w[i] = lo | hi << 16;
         }
-    } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = i < valid ? reinterpret_cast<const uint32_t *>(p)[i] : 0u;
-    } else {
-        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (2 * i < valid ? (uint32_t)h[2 * i] : 0u) | (2 * i + 1 < valid ? (uint32_t)h[2 * i + 1] << 16 : 0u);
     }
 }
+__device__ __forceinline__ void load16(const void *p, uint32_t *w)
+{
+    const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(p));
+    w[0] = a.x;
+    w[1] = a.y;
+    w[2] = a.z;
+    w[3] = a.w;
+}
+
+// What a lane of a warp that takes 256 columns of a row reads of its columns k0 .. k0 + 7 (k0 = 8 lane + a multiple of 256), columns at
+// and behind K being 0.  ALIGNED: rows begin at multiples of 16 (vec) or 32 bytes.  Else a lane reads the aligned 16 or 32 bytes that its
+// first value lies in, the last lane the 16 behind them too, and settle() moves the bytes to their places; what of that is not of the
+// row is not read.  (Value by value, rows of 3532 bf16 took 6 times as long as rows of 3536.)
+template <typename T, bool ALIGNED>
+struct Columns {
+    uint32_t w[kWords<T>], behind[ALIGNED ? 1 : 4];
+    uint32_t shift;  // bytes
+
+    __device__ __forceinline__ void load(const T *row, int32_t k0, int32_t K, bool there, int vec)
+    {
+        constexpr int kBytes = 8 * (int)sizeof(T);
+        if (!there) K = 0;
+        if constexpr (ALIGNED) {
+            const T *p = row + k0;
+            if (k0 + 8 > K || vec == 0) {
+                load_single<T, kWords<T>>(p, 0, K - k0, w);
+            } else if (sizeof(T) == 4 && vec >= 32) {
+                asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[kWords<T> - 4]), "=r"(w[kWords<T> - 3]), "=r"(w[kWords<T> - 2]), "=r"(w[kWords<T> - 1])
+                             : "l"(p));
+            } else {
+#pragma unroll
+                for (int i = 0; i < kWords<T> / 4; ++i) load16(reinterpret_cast<const uint4 *>(p) + i, w + 4 * i);
+            }
+        } else {
+            shift = (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u;
+            const int32_t first = k0 - (int32_t)(shift / sizeof(T));  // the value that the aligned bytes begin with
+            const T *p = row + first;
+            if (first >= 0 && first + 8 <= K) {
+#pragma unroll
+                for (int i = 0; i < kBytes / 16; ++i) load16(reinterpret_cast<const uint4 *>(p) + i, w + 4 * i);
+            } else {
+                load_single<T, kWords<T>>(p, -first, K - first, w);
+            }
+            if ((threadIdx.x & 31) == 31) {
+                constexpr int kNext = 16 / (int)sizeof(T);
+                if (first + 8 + kNext <= K) load16(p + 8, behind);
+                else load_single<T, 4>(p + 8, 0, K - first - 8, behind);
+            }
+        }
+    }
+    // The eight values (the whole warp together).
+    __device__ __forceinline__ void settle()
+    {
+        if constexpr (!ALIGNED) {
+            constexpr int N = kWords<T>;
+            uint32_t z[N + 4];
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] = w[i];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                z[N + i] = __shfl_down_sync(0xffffffffu, w[i], 1);
+                if ((threadIdx.x & 31) == 31) z[N + i] = behind[i];
+            }
+#pragma unroll
+            for (int i = 0; i < N + 2; ++i) z[i] = shift & 8 ? z[i + 2] : z[i];
+#pragma unroll
+            for (int i = 0; i < N + 1; ++i) z[i] = shift & 4 ? z[i + 1] : z[i];
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = sizeof(T) == 4 ? z[i] : __funnelshift_r(z[i], z[i + 1], (shift & 2) * 8);
+        }
+    }
+};
 template <typename T>
 __device__ __forceinline__ void unpack8(const uint32_t (&w)[kWords<T>], float (&v)[8])
 {

@@ -188,15 +188,14 @@ __device__ __forceinline__ bool quantize_tokens(const Mx4GemmArgs &a, const Plan
     const int lane = threadIdx.x & 31;
     const int share = plan.num_kb >= EW ? 1 : plan.num_kb * 2 >= EW ? 2 : plan.num_kb * 4 >= EW ? 4 : EW;  // warps of a stage
     const int every = EW / share, r0 = ew % share, step = 4 * share;
-    const X *values = reinterpret_cast<const X *>(a.values) + (int64_t)tile.row * a.ldx + lane * 8;
+    const X *values = reinterpret_cast<const X *>(a.values) + (int64_t)tile.row * a.ldx;
     bool odd = false;
     for (int kb = ew / share; kb < plan.num_kb; kb += every) {
         const uint32_t n = (uint32_t)(stage0 + kb), s = n % STAGES, parity = (n / STAGES) & 1u;
-        const int valid = max(0, min(8, (int)a.K - kb * kTileK - lane * 8));
-        uint32_t v[4][kWords<X>], next[4][kWords<X>];
-        auto load = [&](int row, uint32_t (&to)[4][kWords<X>]) {
+        Columns<X, true> v[4], next[4];
+        auto load = [&](int row, Columns<X, true> (&to)[4]) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j, row += share) load8<X>(values + (int64_t)row * a.ldx + kb * kTileK, row < tile.count ? valid : 0, plan.x_vec, to[j]);
+            for (int j = 0; j < 4; ++j, row += share) to[j].load(values + (int64_t)row * a.ldx, kb * kTileK + lane * 8, (int32_t)a.K, row < tile.count, plan.x_vec);
         };
         if (r0 < tile.count) load(r0, v);
         if (!__all_sync(0xffffffffu, wait_for(smem_u32(empty_bar + s), parity ^ 1u, abort_flag, a.status))) return false;
@@ -206,7 +205,7 @@ __device__ __forceinline__ bool quantize_tokens(const Mx4GemmArgs &a, const Plan
             for (int j = 0; j < 4; ++j) {
                 const int r = row + share * j;  // (a row behind the last is rounded and dropped, so that the four can be worked on together)
                 uint32_t E;
-                const uint32_t codes = quantize8<X>(v[j], E, odd);
+                const uint32_t codes = quantize8<X>(v[j].w, E, odd);
                 uint32_t w = E << (8 * ((lane >> 2) & 3));
                 w |= __shfl_xor_sync(0xffffffffu, w, 4);
                 w |= __shfl_xor_sync(0xffffffffu, w, 8);
@@ -216,9 +215,7 @@ __device__ __forceinline__ bool quantize_tokens(const Mx4GemmArgs &a, const Plan
                 }
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < kWords<X>; ++i) v[j][i] = next[j][i];
+            for (int j = 0; j < 4; ++j) v[j] = next[j];
         }
         fence_proxy_async_smem();  // what the tensor cores read they read through the asynchronous proxy
         __syncwarp();
@@ -496,7 +493,8 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
             if constexpr (FUSED) {
                 if (!waited) grid_dependency_wait();
                 waited = true;
-                if (!quantize_tokens<EW, C::kStages, C::kBBytes, C::kSbBytes, X>(a, plan, tile, ew, stage0, smem_b, smem_sb, full_bar, empty_bar, abort_flag)) break;
+                const bool done = quantize_tokens<EW, C::kStages, C::kBBytes, C::kSbBytes, X>(a, plan, tile, ew, stage0, smem_b, smem_sb, full_bar, empty_bar, abort_flag);
+                if (!done) break;
                 stage0 += plan.num_kb;
             }
             const int feature0 = tile.feature + (int)rank * kTileRows + quarter * 32, feature = feature0 + lane;

@@ -162,6 +162,29 @@ def test_slope_of_the_rounding():
     assert (y[-1] - y[0]) / (t[-1, 0] - t[0, 0]) == 1
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("K", [1, 7, 8, 9, 31, 100, 255, 256, 257, 263, 264, 511, 770, 1035])
+def test_rows_at_any_address(K, dtype):
+    """Every place of a row's beginning and end in the 16 bytes that are read and written at once: values, and nothing beside them."""
+    for offset in range(0, 9):
+        for ld in (K + 9, K + 10, 2 * K + 12, 16 * (K // 16 + 2)):
+            x = values((9, ld), K + offset, dtype)
+            x[:, :offset], x[:, offset + K:] = float("nan"), float("nan")  # what is not of the rows does not reach them
+            rows = x[:, offset:offset + K]
+            word = status_word()
+            t = q8.q8_mx4_quantize(rows, dev_status=word)
+            check_codes(t, rows)
+            out = torch.full((11, ld + 3), 5.0, dtype=dtype, device="cuda")
+            inner = out[1:10, offset + 1:offset + 1 + K]
+            q8.q8_mx4_fake_quantize(rows, inner, dev_status=word)
+            want = torch.from_numpy(ref.rounded(rows)).to(dtype)
+            assert torch.equal(inner.cpu(), want) and word.item() == 0
+            rest = out.clone()
+            rest[1:10, offset + 1:offset + 1 + K] = 5.0
+            assert (rest == 5.0).all()
+            assert torch.equal(q8.q8_mx4_dequantize(t, dtype).cpu(), want)
+
+
 # ---------------------------------------------------------------- the layer
 def run_layer(M, N, K, dtype, act, with_bias, seed=0, ld=None, out=None):
     x = values((M, ld or K), seed, dtype, 0.5)[:, :K]
@@ -202,8 +225,10 @@ def test_linear_types(M, dtype, out):
 
 
 @pytest.mark.parametrize("ld", [1000, 1008, 1001])
-def test_linear_rows_of_a_wider_tensor(ld):
-    run_layer(100, 256, 1000, torch.bfloat16, q8.Q8_ACT_NONE, True, ld=ld)
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_linear_rows_of_a_wider_tensor(ld, dtype):
+    for M in (1, 3, 13, 100):
+        run_layer(M, 256, 1000, dtype, q8.Q8_ACT_NONE, True, ld=ld)
 
 
 def test_linear_long_rows():
