@@ -49,7 +49,7 @@ template <int CTAS, int BN, int EW, bool FUSED>
 struct Cfg {
     static constexpr int kThreads = 96 + 32 * EW;
     static constexpr int kBBytes = BN / CTAS * 128;
-    static constexpr int kSbBytes = (FUSED ? 1 : 2) * kScaleBytes;  // two row blocks: a tile of 192 may start in the middle of one
+    static constexpr int kSbBytes = (BN > kTileRows ? 2 : 1) * kScaleBytes;  // of each row block that a tile's tokens may lie in
     static constexpr int kStageBytes = kTileBytes + kBBytes + kSbBytes;
     static constexpr int kTableBytes = 3 * (kMaxExperts + 1) * 4 + 4 + kListed * (int)sizeof(Tile);
     static constexpr int kBudget = 227 * 1024 - 1024 - kTableBytes - 512;
@@ -62,7 +62,7 @@ struct Cfg {
     static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kTableBytes + kBarrierBytes;
     static_assert(kScaleCol0 + 2 * kScaleCols <= 512, "TMEM columns");
     static_assert(kSmemBytes <= 232448 && kStages >= 3, "shared memory budget");
-    static_assert(BN % (FUSED ? 32 : 64) == 0 && (!FUSED || (CTAS == 1 && BN == kFusedTokens && EW == 8)) && (BN <= 192 || (BN == 256 && CTAS == 2 && (EW == 8 || EW == 16))) && kBBytes % 1024 == 0, "tile width");
+    static_assert(kBBytes % 1024 == 0 && (FUSED ? CTAS == 1 && BN == kFusedTokens : CTAS == 1 ? BN == 64 || BN == 128 : BN == 256) && (EW == 8 || EW == 16), "tile");
     // Instruction descriptor of kind::mxf4: E2M1 operands, both K-major, UE8M0 scales, M = 128 or 256 for the pair; N / 8 in bits
     // 17..22, which half of a scale word serves in bits 4..5 (B) and 29..30 (A).
     static constexpr uint32_t kInstrDesc = (1u << 7) | (1u << 10) | (1u << 23) | ((uint32_t)CTAS << 27);
@@ -254,8 +254,6 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;
     const bool leader = rank == 0;
-    // What the roles need of the arguments first, all at once: one line of them after the other costs 200 cycles each time.
-    asm volatile("" ::"l"(a.W), "l"(a.values), "l"(a.offsets), "l"(a.Y), "l"(a.M), "l"(a.K), "r"(plan.tiles), "r"(plan.w_blocks));
     if (warp == 0) {  // a lane a barrier
         constexpr int kBarriers = 2 * C::kStages + 2 * kAccStages + 1;
         static_assert(kBarriers <= 32, "barriers");
@@ -291,7 +289,7 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
         tile = list[i];
         return tile.count > 0;
     };
-    // A plain product's weight producer, which made the barriers and needs neither the table nor TMEM, goes ahead without the others.
+    // A plain product's weight producer, which made the barriers and needs neither the list nor TMEM, goes ahead without the others.
     tc_fence_before();
     __syncwarp();
     if (CTAS == 1 && a.offsets == nullptr && warp == 0) asm volatile("barrier.cta.arrive 1, %0;" ::"n"(C::kThreads) : "memory");
@@ -328,12 +326,11 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
                 const int64_t s_tile = ((int64_t)tile.block + tile.first / kTileRows) * plan.num_kb;
                 const bool two_scales = tile.first % kTileRows + width > kTileRows;  // the tile's tokens lie in two row blocks
                 const int in_first = min(mine, kTileRows - sub);                     // of this CTA's tokens, those in the first row block
-                const uint32_t bytes = CTAS == 1 ? (weights ? kTileBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 2 : 1))
+                const uint32_t bytes = CTAS == 1 ? (weights ? kTileBytes : (uint32_t)mine * 128 + kScaleBytes)
                                                  : 2 * (weights ? kTileBytes + kScaleBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 1 : 0));
                 if (!waited && !(weights && early)) grid_dependency_wait();
                 waited = true;
-                const uint8_t *w = a.W + w_tile * kTileBytes, *x = a.X + x_tile * kTileBytes, *xs = a.X + s_tile * kTileBytes + kCodeBytes;
-                const int64_t next_block = (int64_t)plan.num_kb * kTileBytes;
+                const uint8_t *w = a.W + w_tile * kTileBytes, *x = a.X + x_tile * kTileBytes;
                 bool ready = mbar_try_wait(smem_u32(empty_bar + s), phase ^ 1u);
                 for (int kb = 0; kb < plan.num_kb; ++kb) {
                     ok = ready || wait_on(smem_u32(empty_bar + s), phase ^ 1u, abort_flag, a.status);
@@ -348,12 +345,9 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
                             bulk_load(smem_u32(smem_a + s * kTileBytes), w, kTileBytes, fb);
                             w += kTileBytes;
                         } else {
-                            bulk_load(dst_b, x + sub * 128, (uint32_t)in_first * 128, fb);
-                            if (in_first < mine) bulk_load(dst_b + in_first * 128, x + next_block, (uint32_t)(mine - in_first) * 128, fb);
-                            bulk_load(dst_s, xs, kScaleBytes, fb);
-                            if (two_scales) bulk_load(dst_s + kScaleBytes, xs + next_block, kScaleBytes, fb);
+                            bulk_load(dst_b, x + sub * 128, (uint32_t)mine * 128, fb);
+                            bulk_load(dst_s, x + kCodeBytes, kScaleBytes, fb);
                             x += kTileBytes;
-                            xs += kTileBytes;
                         }
                     } else {
                         if (leader) mbar_expect_tx(fb, bytes);
@@ -649,6 +643,18 @@ cudaError_t launch_shape(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, 
 
 }  // namespace
 
+// Microseconds of `rounds` tiles one after the other: set-up, and for each tile its stages and what is not hidden under the next one's.
+// Fitted to 300 products (100 to 8192 tokens, K = 256 to 4096, 256 to 4096 features, bf16 without and fp32 with GELU) timed with
+// each width, 5 % off for single CTAs, 11 % for pairs.  Taking the fastest by it costs 0.6 % on average; 192 wide tiles of one CTA, or pairs as soon as
+// each has work, 5.8 % and up to 45 % (4096 x 4096 -> 1024: 64 / 128 / 192 wide 16.0 / 11.2 / 14.9 us, pairs 10.3).
+double tile_cost(int n, int64_t rounds, int num_kb, bool gelu)
+{
+    const double start = n == 64 ? 2.2 : n == 128 ? 2.3 : 2.5;
+    const double stage = n == 64 ? 0.183 : n == 128 ? 0.210 : 0.290;
+    const double tile = gelu ? (n == 64 ? 0.89 : n == 128 ? 1.53 : 2.99) : (n == 64 ? 0.54 : n == 128 ? 0.87 : 1.80);
+    return start + (double)rounds * (stage * num_kb + tile);
+}
+
 // One launch instead of two, against tokens that every CTA reads and rounds itself, behind the weights that fill the way into its SM: about
 // 1 us for every four tokens and 8 stages.  (Fused / not, us, replayed and then called from Python: 1 x 1024 -> 4096 4.0 / 5.0 and 4.3 / 6.9, 16 x 1024 ->
 // 4096 5.5 / 4.8 and 5.7 / 6.9, 32 x 1024 -> 4096 7.4 / 4.9 and 7.6 / 7.1, 4 x 4096 -> 16384 8.4 / 9.8 and 8.5 / 9.9, 8 x 4096 -> 16384 10.2 / 9.7 and
@@ -662,10 +668,9 @@ cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s)
     p.k_blocks = (int32_t)ceil_div(a.K, kBlock);
     p.w_blocks = (int32_t)ceil_div(a.N, kTileRows);
     p.tiles_m = p.w_blocks;
-    const int64_t hit = a.E < a.M ? a.E : a.M;        // experts with tokens, at most
-    const int64_t mean = ceil_div(a.M, a.E);
-    const int sms = sm_count();
-    const int64_t extra = a.E > 1 ? hit : 0;  // tiles of tokens that are not full, at most
+    const int64_t hit = a.E < a.M ? a.E : a.M;  // experts with tokens, at most
+    const int64_t extra = a.E > 1 ? hit : 0;    // tiles of tokens that are not full, at most
+    const int64_t pairs = ceil_div(a.N, 2 * kTileRows);
     if (a.values != nullptr) {
         p.tile_n = kFusedTokens;
         p.x_vec = value_alignment(a.values, a.ldx, a.x_dtype == Q8_F32 ? 4 : 2);
@@ -676,24 +681,26 @@ cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s)
             default: return launch_shape<1, kFusedTokens, 8, __nv_bfloat16>(a, p, tiles, s);
         }
     }
-    // pairs once each has work
-    const int64_t pairs = ceil_div(a.N, 2 * kTileRows);
-    if (mean > 128 && ceil_div(a.M, 256) * pairs >= sms / 2) {
-        p.tile_n = 256;
-        p.tiles_m = (int32_t)pairs;
-        const int64_t tiles = (ceil_div(a.M, 256) + extra) * pairs;
-        // GELU keeps 16 warps busy; without it 8 with more registers are faster (24576 x 1024 -> 4096 bf16, 8 / 16 warps: 60 / 62 us, with GELU 95 / 82;
-        // 8192 x 2048 -> 8192 60 / 67 and 80 / 77).
-        return a.act == Q8_ACT_GELU ? launch_shape<2, 256, 16>(a, p, tiles, s) : launch_shape<2, 256, 8>(a, p, tiles, s);
+    // The width of a tile whose rounds over the device take the shortest time.
+    const int sms = sm_count();
+    int best = 0;
+    double best_cost = 0.0;
+    for (int n : {64, 128, 256}) {
+        const int64_t tokens = ceil_div(a.M, n) + extra / 2, tiles = (tokens > hit ? tokens : hit) * (n == 256 ? pairs : p.w_blocks);
+        const double cost = tile_cost(n, ceil_div(tiles, n == 256 ? sms / 2 : sms), p.num_kb, a.act == Q8_ACT_GELU);
+        if (best == 0 || cost < best_cost) {
+            best = n;
+            best_cost = cost;
+        }
     }
-    // widest tile that still gives every SM one
-    p.tile_n = 192;
-    for (int n : {128, 64})
-        if (mean <= n || (ceil_div(a.M, p.tile_n) + extra / 2) * p.tiles_m < sms) p.tile_n = n;
-    const int64_t tiles = (ceil_div(a.M, p.tile_n) + extra) * p.tiles_m;  // at most
-    if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
-    return p.tile_n == 64 ? launch_shape<1, 64, 8>(a, p, tiles, s)
-                          : p.tile_n == 128 ? launch_shape<1, 128, 8>(a, p, tiles, s) : launch_shape<1, 192, 8>(a, p, tiles, s);
+    p.tile_n = best;
+    if (best == 256) p.tiles_m = (int32_t)pairs;
+    const int64_t tiles = (ceil_div(a.M, best) + extra) * p.tiles_m;  // at most
+    if (best == 64) return launch_shape<1, 64, 8>(a, p, tiles, s);
+    if (best == 128) return launch_shape<1, 128, 8>(a, p, tiles, s);
+    // GELU keeps 16 warps busy; without it 8 with more registers are faster (24576 x 1024 -> 4096 bf16, 8 / 16 warps: 60 / 62 us, with GELU 95 / 82;
+    // 8192 x 2048 -> 8192 60 / 67 and 80 / 77).
+    return a.act == Q8_ACT_GELU ? launch_shape<2, 256, 16>(a, p, tiles, s) : launch_shape<2, 256, 8>(a, p, tiles, s);
 }
 
 }  // namespace q8
