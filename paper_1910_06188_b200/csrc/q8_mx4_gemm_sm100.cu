@@ -276,11 +276,13 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
             if (bad && lane == 0 && blockIdx.x == 0 && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_INDEX);
         }
         // A lane a tile: looked up by every role for every tile, between two of them, they took 400 cycles each time.
+        const int32_t all = a.offsets != nullptr ? table.tile[a.E] : plan.tiles;
 #pragma unroll 1
         for (int i = lane; i < kListed; i += 32) {
             Tile found;
             if (!find_tile<TILE_M>(first_tile + i * tile_step, table, a, plan, found)) found.count = 0;
             list[i] = found;
+            if (first_tile + (i - lane + 31) * tile_step >= all) break;  // (the last of these 32 ended the list)
         }
     }
     // The i-th tile of this CTA; false behind the last one.
@@ -552,9 +554,9 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
         }
     }
 
-    grid_dependency_wait();  // also where a CTA had no tile: this kernel ends after the one before it
     // ---------------- teardown (reached by every thread, also when aborting) ----------------
-    __syncwarp();
+    __syncwarp();            // (the idle lanes of a producer wait here: in the next line they would hold up the one that works)
+    grid_dependency_wait();  // also where a CTA had no tile: this kernel ends after the one before it
     tc_fence_before();
     __syncthreads();
     if (CTAS == 2) {
