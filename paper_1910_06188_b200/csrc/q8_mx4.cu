@@ -101,9 +101,11 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     constexpr bool kSlots = KIND == kSlots1 || KIND == kSlots4;
     constexpr int kRowStep = KIND == kMatrix ? 32 : 1;
     __shared__ int32_t table_words[kSlots ? 2 * (kMaxExperts + 1) : 1];
-    // The product behind this pass reads weights and offsets at once, so it starts when everything before this kernel has ended.
+    // The product behind slots reads offsets and weights at once, so it starts when everything before this kernel has ended; the one behind a
+    // matrix reads nothing before this kernel's end and may be set up as early as can be (16 x 4096 -> 1024 9.1 -> 8.7 us, 64 rows 8.2 -> 7.8).
+    if (!kSlots) grid_dependency_release_next(true);
     grid_dependency_wait();
-    grid_dependency_release_next(true);
+    if (kSlots) grid_dependency_release_next(true);
     const int lane = threadIdx.x & 31;
     const uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5);
     ExpertTable table{table_words, table_words + kMaxExperts + 1, nullptr};

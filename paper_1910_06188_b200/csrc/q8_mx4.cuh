@@ -62,7 +62,7 @@ __device__ __forceinline__ bool build_expert_table(const ExpertTable &t, const i
 {
     const int lane = threadIdx.x & 31;
     const int run = (E + 32) / 32, lo = min(lane * run, E + 1), hi = min(lo + run, E + 1);  // of E + 1 offsets
-    for (int i = lane; i <= E; i += 32) t.start[i] = __ldg(offsets + i);
+    for (int i = lane; i <= E; i += 32) t.start[i] = __ldcg(offsets + i);  // (from L2: the product reads them before its dependency wait)
     __syncwarp();
     bool bad = false;
     int32_t top = 0;
@@ -346,14 +346,13 @@ struct Mx4GemmArgs {
     int y_dtype;
     int64_t M, N, K;
     int act;
-    const int32_t *offsets = nullptr;  // [E + 1], or nullptr with E == 1
+    const int32_t *offsets = nullptr;  // [E + 1], or nullptr with E == 1; with them the kernel before in the stream is the quantise pass of the slots
     int E = 1;
     int32_t *status;
     // Few tokens: taken and quantised by the product itself, X not used.
     const void *values = nullptr;
     int x_dtype = 0;
     int64_t ldx = 0;
-    bool behind_quantise = false;  // the kernel before this one in the stream is the quantise pass of the same call
 };
 cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s);
 bool mx4_fused_preferred(int64_t M, int64_t K);  // whether to leave the quantisation of a plain activation to the product

@@ -59,7 +59,6 @@ q8_status quantize_and_multiply(Mx4GemmArgs g, const void *X, int x_dtype, int64
     const cudaError_t e = launch_mx4_quantize(a, x_dtype, s);
     if (e != cudaSuccess) return Q8_ERR_CUDA;
     g.X = a.out;
-    g.behind_quantise = true;
     return cuda_status(launch_mx4_gemm(g, s));
 }
 

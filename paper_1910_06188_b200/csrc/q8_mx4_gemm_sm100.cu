@@ -271,7 +271,6 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
     const int32_t first_tile = blockIdx.x / CTAS, tile_step = gridDim.x / CTAS;
     if (warp == 2) {
         if (a.offsets != nullptr) {
-            if (!a.behind_quantise) grid_dependency_wait();
             const bool bad = build_expert_table(table, a.offsets, a.E, (int32_t)a.M, plan.tile_n, plan.tiles_m);
             if (bad && lane == 0 && blockIdx.x == 0 && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_INDEX);
         }
@@ -308,10 +307,10 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
         // A pair's loads all report to the leader's barrier, which its MMA warp waits on.  The tensor maps of the pair see tiles as rows of 128
         // bytes: 136 of them to a tile, the last 8 its scales.
         const bool weights = warp == 0;
-        // A quantise pass of the same call has waited for all kernels before it when this one starts, and writes neither weights nor
-        // offsets, so these may be read before it ends: as much as the ring holds.  (Asking for the rest into L2 as well holds up the loads behind it:
-        // 24 x 4096 -> 16384 9.9 -> 10.6 us, 32 slots on 64 experts 9.5 -> 12.)
-        const bool early = CTAS == 1 && a.behind_quantise;
+        // The quantise pass in front of a grouped product has waited for all kernels before it when this one starts, and writes neither weights
+        // nor offsets, so these may be read before it ends: as much as the ring holds (32 slots on 64 experts 12.7 -> 11.7 us).  (Asking for
+        // the rest into L2 as well holds up the loads behind it: 24 x 4096 -> 16384 9.9 -> 10.6 us, 32 slots on 64 experts 9.5 -> 12.)
+        const bool early = CTAS == 1 && a.offsets != nullptr;
         // One lane does all of it: a warp that waits together and then lets one lane issue takes 500 cycles a stage, more than the products.
         if (elect_one()) {
             int s = 0;
