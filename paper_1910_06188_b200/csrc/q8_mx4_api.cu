@@ -34,6 +34,16 @@ q8_status check_layer(int64_t M, int64_t N, int64_t K, int64_t E, int64_t ldy)
     return Q8_OK;
 }
 
+// Whether rows of `a` and of `b` bytes, pa and pb bytes apart, have any byte in common.  (Rows side by side in one wider matrix do not.)
+bool rows_overlap(const void *x, int64_t rows_x, int64_t a, int64_t pa, const void *y, int64_t rows_y, int64_t b, int64_t pb)
+{
+    const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), y0 = reinterpret_cast<uintptr_t>(y);
+    if (rows_x == 0 || rows_y == 0 || x0 + (uintptr_t)((rows_x - 1) * pa + a) <= y0 || y0 + (uintptr_t)((rows_y - 1) * pb + b) <= x0) return false;
+    if (pa != pb) return true;
+    const int64_t d = (int64_t)(y0 >= x0 ? (y0 - x0) % (uintptr_t)pa : (pa - (int64_t)((x0 - y0) % (uintptr_t)pa)) % pa);
+    return d < a || d + b > pa;
+}
+
 // The activation into the workspace and the product from there, or both in one kernel where the tokens are few.
 q8_status quantize_and_multiply(Mx4GemmArgs g, const void *X, int x_dtype, int64_t ldx, int64_t x_rows, const int32_t *index, void *workspace,
                                 cudaStream_t s)
@@ -116,7 +126,8 @@ q8_status q8_mx4_fake_quantize(const void *X, int dtype, int64_t rows, int64_t K
     if (rows == 0) return Q8_OK;
     if (!X || !Xhat) return Q8_ERR_NULL;
     if (!aligned_to(X, dtype_bytes(dtype)) || !aligned_to(Xhat, dtype_bytes(dtype)) || !aligned_to(dev_status, 4)) return Q8_ERR_ALIGN;
-    if (X == Xhat && ldx != ldo) return Q8_ERR_ARG;
+    const int64_t size = (int64_t)dtype_bytes(dtype);
+    if ((X != Xhat || ldx != ldo) && rows_overlap(X, rows, K * size, ldx * size, Xhat, rows, K * size, ldo * size)) return Q8_ERR_ARG;
     Mx4QuantizeArgs a = {};
     a.X = X;
     a.ld = ldx;
@@ -179,6 +190,8 @@ q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *
         !aligned_to(Y, dtype_bytes(y_dtype)) || !aligned_to(dev_status, 4) || !aligned_to(workspace, 256))
         return Q8_ERR_ALIGN;
     if (workspace_bytes < q8_mx4_linear_workspace_bytes(M, K)) return Q8_ERR_WORKSPACE;
+    const int64_t xs = (int64_t)dtype_bytes(x_dtype), ys = (int64_t)dtype_bytes(y_dtype);
+    if (rows_overlap(X, M, K * xs, ldx * xs, Y, M, N * ys, ldy * ys)) return Q8_ERR_ARG;
     Mx4GemmArgs g = {};
     g.W = Wq;
     g.bias = bias;
@@ -210,6 +223,8 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
         !aligned_to(bias, 4) || !aligned_to(Y, dtype_bytes(y_dtype)) || !aligned_to(dev_status, 4) || !aligned_to(workspace, 256))
         return Q8_ERR_ALIGN;
     if (workspace_bytes < q8_mx4_linear_grouped_workspace_bytes(T, experts, K)) return Q8_ERR_WORKSPACE;
+    const int64_t xs = (int64_t)dtype_bytes(x_dtype), ys = (int64_t)dtype_bytes(y_dtype);
+    if (rows_overlap(X, x_rows, K * xs, ldx * xs, Y, T, N * ys, ldy * ys)) return Q8_ERR_ARG;
     Mx4GemmArgs g = {};
     g.W = Wq;
     g.bias = bias;

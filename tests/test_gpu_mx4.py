@@ -245,6 +245,30 @@ def test_linear_scales_of_all_sizes():
     ref.assert_layer(Y, ref.rounded(x), ref.rounded(w), None, q8.Q8_ACT_NONE)
 
 
+@pytest.mark.parametrize("M,K", [(3, 2048), (200, 4096), (300, 96)])
+def test_linear_blocks_of_all_sizes_in_a_row(M, K):
+    """Sums in which some blocks are far larger than others, so that fp32 cannot hold them exactly."""
+    g = torch.Generator().manual_seed(K)
+    x = torch.randn(M, K // 32, 32, generator=g) * torch.exp(4 * torch.randn(M, K // 32, 1, generator=g))
+    w = torch.randn(260, K // 32, 32, generator=g) * torch.exp(4 * torch.randn(260, K // 32, 1, generator=g))
+    x, w = x.flatten(1).cuda(), w.flatten(1).cuda()
+    ref.assert_layer(q8.q8_mx4_linear(x, q8.q8_mx4_quantize(w)), ref.rounded(x), ref.rounded(w), None, q8.Q8_ACT_NONE)
+
+
+def test_linear_columns_of_one_matrix():
+    """Input and output side by side in one buffer; an output on top of the input is refused."""
+    for M in (3, 40, 300):
+        both = torch.zeros(M, 512 + 384, device="cuda")
+        both[:, :512] = values((M, 512), M, spread=0.5)
+        x, w = both[:, :512].clone(), weights((384, 512), 2)
+        q8.q8_mx4_linear(both[:, :512], q8.q8_mx4_quantize(w), Y=both[:, 512:])
+        assert torch.equal(both[:, :512], x)
+        ref.assert_layer(both[:, 512:], ref.rounded(x), ref.rounded(w), None, q8.Q8_ACT_NONE)
+        with pytest.raises(q8.Q8Error) as e:
+            q8.q8_mx4_linear(both[:, :512], q8.q8_mx4_quantize(w), Y=both[:, 500:884])
+        assert e.value.status == q8.Q8_ERR_ARG
+
+
 def test_linear_zero_rows_and_infinities():
     x, w = values((40, 192), 1, spread=0.0), weights((130, 192), 2)
     x[3], x[4, 64:96] = 0, 0

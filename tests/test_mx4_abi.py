@@ -8,6 +8,7 @@ from paper_1910_06188_b200 import build
 from tests import mx4_reference as ref
 
 FAKE = 0x10000  # never dereferenced
+FAR = 0x10000000
 MANY = 1 << 60
 
 
@@ -27,7 +28,7 @@ def test_sizes(lib):
     assert q8.q8_mx4_linear_grouped_workspace_bytes(4, 1025, 64) == 0
 
 
-def linear(lib, X=FAKE, xt=0, ldx=64, Wq=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, M=4, N=8, K=64, ws=FAKE, size=MANY, word=None):
+def linear(lib, X=FAKE, xt=0, ldx=64, Wq=FAKE, bias=None, act=0, Y=FAR, yt=0, ldy=8, M=4, N=8, K=64, ws=FAKE, size=MANY, word=None):
     return lib.q8_mx4_linear(X, xt, ldx, Wq, bias, act, Y, yt, ldy, M, N, K, ws, size, word, None)
 
 
@@ -35,7 +36,7 @@ def linear_q(lib, Xq=FAKE, Wq=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, M=4, 
     return lib.q8_mx4_linear_q(Xq, Wq, bias, act, Y, yt, ldy, M, N, K, word, None)
 
 
-def grouped(lib, X=FAKE, xt=0, ldx=64, x_rows=4, rows=None, offsets=FAKE, E=3, Wq=FAKE, bias=None, act=0, Y=FAKE, yt=0, ldy=8, T=4, N=8, K=64,
+def grouped(lib, X=FAKE, xt=0, ldx=64, x_rows=4, rows=None, offsets=FAKE, E=3, Wq=FAKE, bias=None, act=0, Y=FAR, yt=0, ldy=8, T=4, N=8, K=64,
             ws=FAKE, size=MANY, word=None):
     return lib.q8_mx4_linear_grouped(X, xt, ldx, x_rows, rows, offsets, E, Wq, bias, act, Y, yt, ldy, T, N, K, ws, size, word, None)
 
@@ -48,7 +49,7 @@ def dequantize(lib, T=FAKE, G=1, R=4, K=64, Y=FAKE, t=0, ld=64):
     return lib.q8_mx4_dequantize(T, G, R, K, Y, t, ld, None)
 
 
-def fake(lib, X=FAKE, t=0, R=4, K=64, ld=64, out=FAKE, ldo=64, word=None):
+def fake(lib, X=FAKE, t=0, R=4, K=64, ld=64, out=FAR, ldo=64, word=None):
     return lib.q8_mx4_fake_quantize(X, t, R, K, ld, out, ldo, word, None)
 
 
@@ -62,7 +63,12 @@ def fake(lib, X=FAKE, t=0, R=4, K=64, ld=64, out=FAKE, ldo=64, word=None):
     *[(call, {k: 3}, q8.Q8_ERR_ARG) for call in (linear, grouped) for k in ("xt", "yt", "act")],
     *[(call, {"t": 7}, q8.Q8_ERR_ARG) for call in (quantize, dequantize, fake)],
     (linear_q, {"act": -1}, q8.Q8_ERR_ARG), (linear_q, {"yt": 3}, q8.Q8_ERR_ARG),
-    (fake, {"X": FAKE, "out": FAKE, "ldo": 65}, q8.Q8_ERR_ARG),
+    # outputs that overlap an input: in place with another pitch, one row or one value into it, as the input's columns, of another pitch
+    (fake, {"out": FAKE, "ldo": 65}, q8.Q8_ERR_ARG), (fake, {"out": FAKE + 256}, q8.Q8_ERR_ARG), (fake, {"out": FAKE + 4}, q8.Q8_ERR_ARG),
+    (fake, {"ld": 100, "ldo": 100, "out": FAKE + 4 * 40}, q8.Q8_ERR_ARG), (fake, {"ld": 100, "ldo": 100, "out": FAKE - 4 * 20}, q8.Q8_ERR_ARG),
+    (linear, {"Y": FAKE}, q8.Q8_ERR_ARG), (linear, {"Y": FAKE + 4 * 255, "ldy": 64}, q8.Q8_ERR_ARG), (linear, {"Y": FAKE - 4 * 25}, q8.Q8_ERR_ARG),
+    (linear, {"M": 130, "Y": FAKE + 4 * 64 * 129}, q8.Q8_ERR_ARG), (linear, {"ldx": 72, "ldy": 72, "Y": FAKE + 4 * 60}, q8.Q8_ERR_ARG),
+    (grouped, {"Y": FAKE + 8}, q8.Q8_ERR_ARG), (grouped, {"rows": FAKE, "x_rows": 100, "Y": FAKE + 4 * 64 * 99}, q8.Q8_ERR_ARG),
     *[(call, bad, q8.Q8_ERR_SHAPE) for call in (linear, linear_q) for bad in (
         {"M": -1}, {"N": -1}, {"K": 0}, {"K": -5}, {"K": (1 << 24) + 1, "ldx": 1 << 30} if call is linear else {"K": (1 << 24) + 1}, {"ldy": 7},
         {"M": 1 << 31}, {"N": 1 << 31, "ldy": 1 << 32}, {"M": 1 << 30, "N": 1 << 30, "ldy": 1 << 30})],
@@ -71,11 +77,11 @@ def fake(lib, X=FAKE, t=0, R=4, K=64, ld=64, out=FAKE, ldo=64, word=None):
         {"T": -1}, {"T": 5}, {"E": -1}, {"E": 1025}, {"x_rows": -1}, {"x_rows": 3}, {"K": 0}, {"ldx": 1}, {"ldy": 7}, {"N": 1 << 30, "ldy": 1 << 30})],
     *[(quantize, bad, q8.Q8_ERR_SHAPE) for bad in ({"G": -1}, {"R": -1}, {"K": 0}, {"ld": 63}, {"G": 1 << 20, "R": 1 << 20})],
     (dequantize, {"ld": 1}, q8.Q8_ERR_SHAPE), (fake, {"ld": 1}, q8.Q8_ERR_SHAPE), (fake, {"ldo": 1}, q8.Q8_ERR_SHAPE),
-    *[(linear, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("X", 2), ("Wq", 8), ("bias", 2), ("Y", 2), ("ws", 128), ("word", 2))],
+    *[(linear, {k: (FAR if k == "Y" else FAKE) + o}, q8.Q8_ERR_ALIGN) for k, o in (("X", 2), ("Wq", 8), ("bias", 2), ("Y", 2), ("ws", 128), ("word", 2))],
     *[(linear_q, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("Xq", 8), ("Wq", 8), ("bias", 2), ("Y", 2), ("word", 2))],
-    *[(grouped, {k: FAKE + o}, q8.Q8_ERR_ALIGN) for k, o in (("X", 2), ("rows", 2), ("offsets", 2), ("Wq", 8), ("bias", 2), ("Y", 2), ("ws", 128))],
+    *[(grouped, {k: (FAR if k == "Y" else FAKE) + o}, q8.Q8_ERR_ALIGN) for k, o in (("X", 2), ("rows", 2), ("offsets", 2), ("Wq", 8), ("bias", 2), ("Y", 2), ("ws", 128))],
     (linear, {"xt": 1, "X": FAKE + 1}, q8.Q8_ERR_ALIGN), (quantize, {"X": FAKE + 2}, q8.Q8_ERR_ALIGN), (quantize, {"out": FAKE + 4}, q8.Q8_ERR_ALIGN),
-    (dequantize, {"T": FAKE + 4}, q8.Q8_ERR_ALIGN), (fake, {"out": FAKE + 1}, q8.Q8_ERR_ALIGN),
+    (dequantize, {"T": FAKE + 4}, q8.Q8_ERR_ALIGN), (fake, {"out": FAR + 1}, q8.Q8_ERR_ALIGN),
     (linear, {"M": 130, "size": 2 * 17408 - 1}, q8.Q8_ERR_WORKSPACE), (grouped, {"size": 3 * 17408 - 1}, q8.Q8_ERR_WORKSPACE),
     # nothing to do: never reaches the device
     *[(call, {k: 0}, q8.Q8_OK) for call in (linear, linear_q) for k in ("M", "N")], *[(grouped, {k: 0}, q8.Q8_OK) for k in ("T", "N", "E")],
