@@ -1,9 +1,9 @@
 // Quantisation to microscaled 4-bit floating point, back, and both at once (training), streaming passes bound by HBM.
 //
-// A lane takes 8 neighbouring values of a row, so four lanes share a block: its maximum is an integer maximum of the lanes'
-// magnitude bits and two shuffles, the scale an exponent, the codes four conversions of two values each.  A warp takes 256 columns of
+// A lane takes 8 neighbouring values of a row, so four lanes share a block: the exponent of its maximum is the largest of the lanes', two
+// shuffles, the scale that exponent less 2, the codes four conversions of two values each.  A warp takes 256 columns of
 // up to four rows, whose loads are all issued before the first is used.  For a plain matrix these are the rows r, r + 32,
-// r + 64 and r + 96 that lie side by side in an atom of scales: the four bytes of each leave as one 16-byte store.
+// r + 64 and r + 96 that lie side by side in an atom of scales, whose scales leave as 16 bytes of four lanes.
 
 #include "q8_mx4.cuh"
 
@@ -93,6 +93,17 @@ __device__ __forceinline__ void store_columns(T *row, int32_t k0, int32_t K, int
     }
 }
 
+template <typename T, bool ALIGNED, int R>
+__device__ __forceinline__ void settle_rows(Columns<T, ALIGNED> (&v)[R], uint32_t (&words)[R][kWords<T>])
+{
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        v[j].settle();
+#pragma unroll
+        for (int i = 0; i < kWords<T>; ++i) words[j][i] = v[j].w[i];
+    }
+}
+
 // (Rows and tasks are counted in 32 bits: with 64-bit divisions the indices took as many instructions as the arithmetic.)
 template <typename T, int KIND, bool ALIGNED>
 __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs a, uint32_t tasks, uint32_t chunks, uint32_t splits, uint32_t row_lanes, int vec, int vec_out)
@@ -118,16 +129,6 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     const uint32_t line = task / splits, part = task - line * splits;  // a part of the tiles of a row: one, or every splits-th
     const int32_t rows = (int32_t)a.rows;
     bool odd = false;
-    // The codes and scales of one row: the bytes of four blocks are gathered from every fourth of 16 lanes.
-    auto quantize_row = [&](Columns<T, ALIGNED> &v, uint32_t &word) {
-        uint32_t E;
-        v.settle();
-        const uint32_t codes = quantize8<T>(v.w, E, odd);
-        word = E << (8 * ((lane >> 2) & 3));
-        word |= __shfl_xor_sync(0xffffffffu, word, 4);
-        word |= __shfl_xor_sync(0xffffffffu, word, 8);
-        return codes;
-    };
     if constexpr (kSlots) {
         // R slots in a row; what a slot's index and expert say is worked out once for all of its tiles.
         const int32_t first = (int32_t)line * R;
@@ -160,19 +161,35 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
 #pragma unroll
             for (int j = 0; j < R; ++j) w[j].load(x[j], (int32_t)chunk * kChunk + lane * 8, (int32_t)a.K, there[j], vec);
         };
+        // where this lane's scales go: those of one row for each (lane / 4) % 4, or of the only one
+        const int mine = R == 1 ? 0 : (lane >> 2) & 3;
+        uint8_t *scales_to = to[0];
+        int scales_row = (int)r[0];
+#pragma unroll
+        for (int j = 1; j < R; ++j) {
+            scales_to = mine == j ? to[j] : scales_to;
+            scales_row = mine == j ? (int)r[j] : scales_row;
+        }
+        if ((lane & (R == 1 ? 15 : 3)) != 0) scales_to = nullptr;
         load(part, v);
         for (uint32_t chunk = part; chunk < chunks; chunk += splits) {
             if (chunk + splits < chunks) load(chunk + splits, next);
-#pragma unroll
-            for (int j = 0; j < R; ++j) {
-                uint32_t word;
-                const uint32_t codes = quantize_row(v[j], word);
-                if (to[j] != nullptr) {
-                    uint8_t *tile = to[j] + (int64_t)chunk * kTileBytes;
-                    *reinterpret_cast<uint32_t *>(tile + code_place((int)r[j], lane)) = codes;
-                    if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(tile + scale_place((int)r[j], lane >> 2)) = word;
-                }
+            uint32_t words[R][kWords<T>], codes[R];
+            settle_rows(v, words);
+            const uint32_t e = quantize_rows<T, R>(words, codes, odd);
+            uint32_t scales;
+            if constexpr (R == 1) {
+                scales = e << (8 * ((lane >> 2) & 3));
+                scales |= __shfl_xor_sync(0xffffffffu, scales, 4);
+                scales |= __shfl_xor_sync(0xffffffffu, scales, 8);
+            } else {
+                scales = scale_words(e, lane);
             }
+            const int64_t at = (int64_t)chunk * kTileBytes;
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+                if (to[j] != nullptr) *reinterpret_cast<uint32_t *>(to[j] + at + code_place((int)r[j], lane)) = codes[j];
+            if (scales_to != nullptr) *reinterpret_cast<uint32_t *>(scales_to + at + scale_place(scales_row, (lane >> 4) * 4)) = scales;
 #pragma unroll
             for (int j = 0; j < R; ++j) v[j] = next[j];
         }
@@ -198,29 +215,29 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
         }
         const int32_t k0 = (int32_t)part * kChunk + lane * 8;
         Columns<T, ALIGNED> v[R];
-        uint32_t words[R];
         const T *x = reinterpret_cast<const T *>(a.X) + first * a.ld;
 #pragma unroll
         for (int j = 0; j < R; ++j, x += kRowStep * a.ld) v[j].load(x, k0, (int32_t)a.K, first + j * kRowStep < end, vec);
+        uint32_t words[R][kWords<T>], codes[R];
+        settle_rows(v, words);
+        const uint32_t e = quantize_rows<T, R>(words, codes, odd);
+        if constexpr (KIND == kFake) {
 #pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const int32_t row = first + j * kRowStep;
-            if constexpr (KIND == kFake) {
-                uint32_t E;
+            for (int j = 0; j < R; ++j) {
                 float back[8];
-                v[j].settle();
-                unpack_e2m1(quantize8<T>(v[j].w, E, odd), back);
-                const float s = scale_value(E);
+                unpack_e2m1(codes[j], back);
+                const float s = scale_value(e >> (8 * j) & 0xffu);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) back[i] = __fmul_rn(back[i], s);
+                const int32_t row = first + j;
                 if (row < end) store_columns<T, ALIGNED>(reinterpret_cast<T *>(a.Xhat) + row * a.ldo, k0, (int32_t)a.K, vec_out, back);
-            } else {
-                const uint32_t codes = quantize_row(v[j], words[j]);
-                if (row < end) *reinterpret_cast<uint32_t *>(tile + code_place((int)r0, lane) + 32 * 128 * j) = codes;
             }
-        }
-        if constexpr (KIND == kMatrix) {
-            if ((lane & 15) == 0) *reinterpret_cast<uint4 *>(tile + scale_place((int)r0, lane >> 2)) = make_uint4(words[0], words[1], words[2], words[3]);
+        } else {
+            const uint32_t scales = scale_words(e, lane);
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+                if (first + 32 * j < end) *reinterpret_cast<uint32_t *>(tile + code_place((int)r0, lane) + 32 * 128 * j) = codes[j];
+            if ((lane & 3) == 0) *reinterpret_cast<uint32_t *>(tile + scale_place((int)r0, (lane >> 4) * 4) + (lane & 12)) = scales;
         }
     }
     if (a.status != nullptr) {

@@ -144,9 +144,8 @@ __device__ __forceinline__ void unpack_e2m1(uint32_t codes, float (&v)[8])
         v[i] = __fmul_rn(__uint_as_float((c & 7) << 22 | (c & 8) << 28), __uint_as_float(253u << 23));
     }
 }
-// 2^(E - 127) and its inverse, E <= 252 (an exponent of 0 is the subnormal 2^-127).
+// 2^(E - 127) (an exponent of 0 is the subnormal 2^-127).
 __device__ __forceinline__ float scale_value(uint32_t E) { return __uint_as_float(E == 0 ? 0x00400000u : E << 23); }
-__device__ __forceinline__ float inverse_scale(uint32_t E) { return __uint_as_float((254u - E) << 23); }
 
 // Eight values as they lie in memory: four words of two, or eight words of one.
 template <typename T>
@@ -261,52 +260,87 @@ __device__ __forceinline__ void unpack8(const uint32_t (&w)[kWords<T>], float (&
         }
     }
 }
-// The fp32 bits of max|v|; at least those of an infinity where one of the values is NaN or infinite.
+// The exponent field (of fp32) of max|v|; 255 where one of the values is NaN or infinite.
 template <typename T>
-__device__ __forceinline__ uint32_t max_bits(const uint32_t (&w)[kWords<T>])
+__device__ __forceinline__ uint32_t top_field(const uint32_t (&w)[kWords<T>])
 {
     if constexpr (sizeof(T) == 4) {
         float m = __uint_as_float(w[0]);
 #pragma unroll
         for (int i = 1; i < 8; ++i) asm("max.NaN.xorsign.abs.f32 %0, %0, %1;" : "+f"(m) : "f"(__uint_as_float(w[i])));
-        return __float_as_uint(m) & 0x7fffffffu;
+        return __float_as_uint(m) << 1 >> 24;
     } else {  // magnitudes order like their bits, two to a word
         uint32_t m = w[0] & 0x7fff7fffu;
 #pragma unroll
         for (int i = 1; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
-        m = max(m & 0xffffu, m >> 16);
-        if constexpr (std::is_same<T, __half>::value) return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));  // (NaN stays NaN)
-        else return m << 16;
+        m = __vmaxu2(m, m >> 16);
+        if constexpr (std::is_same<T, __half>::value) return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m))) >> 23;
+        else return (m >> 7) & 0xffu;
     }
 }
-
-// E of the block that this lane and its three neighbours hold, and the lane's codes.  NaN becomes 0; neither NaN nor an infinity is
-// in the maximum (`odd` says that there was one).
+// The same without what is not a number; NaN becomes 0.
 template <typename T>
-__device__ __forceinline__ uint32_t quantize8(const uint32_t (&w)[kWords<T>], uint32_t &E, bool &odd)
+__device__ __forceinline__ uint32_t top_finite_field(uint32_t (&w)[kWords<T>])
 {
     float v[8];
     unpack8<T>(w, v);
-    uint32_t top = max_bits<T>(w);
-    if (__any_sync(0xffffffffu, top >= 0x7f800000u)) {  // once more, without what is not a number
-        odd = true;
-        top = 0;
+    uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t bits = __float_as_uint(v[i]) & 0x7fffffffu;
-            if (bits > 0x7f800000u) v[i] = 0.0f;
-            if (bits < 0x7f800000u) top = max(top, bits);
-        }
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t bits = __float_as_uint(v[i]) & 0x7fffffffu;
+        if (bits > 0x7f800000u) w[sizeof(T) == 4 ? i : i / 2] &= sizeof(T) == 4 ? 0u : i & 1 ? 0xffffu : 0xffff0000u;
+        if (bits < 0x7f800000u) top = max(top, bits);
     }
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const uint32_t field = top >> 23;
-    E = field > 2 ? field - 2 : 0;
-    const float inv = inverse_scale(E);
-    const uint64_t inv2 = ptx::pack_f32x2(inv, inv);
+    return top >> 23;
+}
+
+// E of the block that this lane and its three neighbours hold of R rows (1 or 4), a byte a row, and the lane's codes of each row.  NaN becomes
+// 0; neither NaN nor an infinity is in a maximum (`odd` says that there was one).  The rows share their shuffles, two exponents to a word:
+// that, one test for all four of what is not a number, and the four by four bytes of scale_words() take 50 instructions a row less than rows by themselves.
+template <typename T, int R>
+__device__ __forceinline__ uint32_t quantize_rows(uint32_t (&w)[R][kWords<T>], uint32_t (&codes)[R], bool &odd)
+{
+    static_assert(R == 1 || R == 4, "rows");
+    constexpr int N = R == 1 ? 1 : 2;
+    uint32_t f[R], pair[N];
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(v[i], v[i + 1]), inv2), v[i], v[i + 1]);
-    return pack_e2m1(v);
+    for (int j = 0; j < R; ++j) f[j] = top_field<T>(w[j]);
+    uint32_t all = f[0];
+#pragma unroll
+    for (int j = 1; j < R; ++j) all = max(all, f[j]);
+    if (__any_sync(0xffffffffu, all == 255)) {
+        odd = true;
+#pragma unroll
+        for (int j = 0; j < R; ++j) f[j] = top_finite_field<T>(w[j]);
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        pair[n] = R == 1 ? f[0] : __byte_perm(f[2 * n % R], f[(2 * n + 1) % R], 0x5410);
+        pair[n] = __vmaxu2(pair[n], __shfl_xor_sync(0xffffffffu, pair[n], 1));
+        pair[n] = __vmaxu2(pair[n], __shfl_xor_sync(0xffffffffu, pair[n], 2));
+        pair[n] = __vmaxu2(pair[n], 0x00020002u) - 0x00020002u;  // the fields less 2, at least 0: E
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const uint32_t rest = 0x00fe00feu - pair[j / 2];  // 254 - E
+        const float inv = __uint_as_float(j & 1 ? (rest & 0x00ff0000u) << 7 : rest << 23);
+        const uint64_t inv2 = ptx::pack_f32x2(inv, inv);
+        float v[8];
+        unpack8<T>(w[j], v);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(v[i], v[i + 1]), inv2), v[i], v[i + 1]);
+        codes[j] = pack_e2m1(v);
+    }
+    return R == 1 ? pair[0] & 0xffu : __byte_perm(pair[0], pair[N - 1], 0x6420);
+}
+// The scale word of row i of the four for the lanes with (lane / 4) % 4 = i: the bytes of the four blocks that every 16 lanes hold, from the
+// bytes of four rows that each lane has (a four by four transposition in two exchanges).
+__device__ __forceinline__ uint32_t scale_words(uint32_t e, int lane)
+{
+    uint32_t q = __shfl_xor_sync(0xffffffffu, e, 4);
+    e = __byte_perm(e, q, lane & 4 ? 0x3715 : 0x6240);
+    q = __shfl_xor_sync(0xffffffffu, e, 8);
+    return __byte_perm(e, q, lane & 8 ? 0x3276 : 0x5410);
 }
 
 // The largest access of up to 32 bytes that the rows are aligned for.  (fp32 in two halves of 16 bytes writes half sectors: dequantising

@@ -201,19 +201,19 @@ __device__ __forceinline__ bool quantize_tokens(const Mx4GemmArgs &a, const Plan
         if (!__all_sync(0xffffffffu, wait_for(smem_u32(empty_bar + s), parity ^ 1u, abort_flag, a.status))) return false;
         for (int row = r0; row < tile.count; row += step) {
             if (row + step < tile.count) load(row + step, next);
+            // (rows behind the last are rounded and dropped, so that the four can be worked on together)
+            uint32_t words[4][kWords<X>], codes[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = row + share * j;  // (a row behind the last is rounded and dropped, so that the four can be worked on together)
-                uint32_t E;
-                const uint32_t codes = quantize8<X>(v[j].w, E, odd);
-                uint32_t w = E << (8 * ((lane >> 2) & 3));
-                w |= __shfl_xor_sync(0xffffffffu, w, 4);
-                w |= __shfl_xor_sync(0xffffffffu, w, 8);
-                if (r < tile.count) {
-                    *reinterpret_cast<uint32_t *>(smem_b + s * B_BYTES + code_place(r, lane)) = codes;
-                    if ((lane & 15) == 0) *reinterpret_cast<uint32_t *>(smem_sb + s * SB_BYTES + scale_place(r, lane >> 2) - kCodeBytes) = w;
-                }
-            }
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < kWords<X>; ++i) words[j][i] = v[j].w[i];
+            const uint32_t scales = scale_words(quantize_rows<X, 4>(words, codes, odd), lane);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (row + share * j < tile.count) *reinterpret_cast<uint32_t *>(smem_b + s * B_BYTES + code_place(row + share * j, lane)) = codes[j];
+            const int mine = row + share * ((lane >> 2) & 3);
+            if ((lane & 3) == 0 && mine < tile.count)
+                *reinterpret_cast<uint32_t *>(smem_sb + s * SB_BYTES + scale_place(mine, (lane >> 4) * 4) - kCodeBytes) = scales;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = next[j];
         }
