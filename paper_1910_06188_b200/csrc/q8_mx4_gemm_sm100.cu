@@ -15,6 +15,9 @@
 // Few tokens (X not void): no quantise pass; the epilogue warps first quantise the tokens of the tile into the operand stages themselves,
 // while the weights, which are what such a product waits for, are on their way.
 //
+// A plain product with few tiles and a long K: the K axis of a tile is split over a cluster of CTAs, whose sums are joined through distributed
+// shared memory, each CTA finishing a share of the tokens (join()).
+//
 // CTAS = 2 (cta_group::2): a pair of SMs shares a tile of 256 features; each loads its own 128 rows of weights, half of the tokens and the
 // scales of all of them.  A plain product is the grouped one with a single expert.  Every wait on an mbarrier is bounded: after
 // ~2 s the CTA raises Q8_ERR_TIMEOUT in the status word, all roles leave their loops, copies and products in flight are waited for
@@ -121,6 +124,7 @@ struct Plan {
     int32_t num_kb;    // stages of a tile
     int32_t k_blocks;  // blocks of 32 along K
     int32_t w_blocks;  // row blocks of one expert's weights
+    int32_t split;     // CTAs that share the K axis of a tile
     int32_t x_vec;     // bytes that loads of the tokens' values may take at once
 };
 
@@ -182,16 +186,16 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile
 // the next four on their way while it rounds these; with fewer stages than warps some share the rows of one.  (All warps on one stage
 // after the other: 24 x 4096 -> 16384 18.9 us.  The fence at the end of a stage waits for loads in flight, so none are over it.)
 template <int EW, int STAGES, int B_BYTES, int SB_BYTES, typename X>
-__device__ __forceinline__ bool quantize_tokens(const Mx4GemmArgs &a, const Plan &plan, const Tile &tile, int ew, int32_t stage0, uint8_t *smem_b, uint8_t *smem_sb,
+__device__ __forceinline__ bool quantize_tokens(const Mx4GemmArgs &a, const Plan &plan, const Tile &tile, int32_t kb_lo, int32_t kb_hi, int ew, int32_t stage0, uint8_t *smem_b, uint8_t *smem_sb,
                                                 uint64_t *full_bar, uint64_t *empty_bar, volatile int *abort_flag)
 {
     const int lane = threadIdx.x & 31;
-    const int share = plan.num_kb >= EW ? 1 : plan.num_kb * 2 >= EW ? 2 : plan.num_kb * 4 >= EW ? 4 : EW;  // warps of a stage
+    const int stages = kb_hi - kb_lo, share = stages >= EW ? 1 : stages * 2 >= EW ? 2 : stages * 4 >= EW ? 4 : EW;  // warps of a stage
     const int every = EW / share, r0 = ew % share, step = 4 * share;
     const X *values = reinterpret_cast<const X *>(a.values) + (int64_t)tile.row * a.ldx;
     bool odd = false;
-    for (int kb = ew / share; kb < plan.num_kb; kb += every) {
-        const uint32_t n = (uint32_t)(stage0 + kb), s = n % STAGES, parity = (n / STAGES) & 1u;
+    for (int kb = kb_lo + ew / share; kb < kb_hi; kb += every) {
+        const uint32_t n = (uint32_t)(stage0 + kb - kb_lo), s = n % STAGES, parity = (n / STAGES) & 1u;
         Columns<X, true> v[4], next[4];
         auto load = [&](int row, Columns<X, true> (&to)[4]) {
 #pragma unroll
@@ -223,6 +227,55 @@ __device__ __forceinline__ bool quantize_tokens(const Mx4GemmArgs &a, const Plan
     }
     if (odd && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_SCALE);
     return true;
+}
+
+__device__ __forceinline__ void store_remote(uint32_t cluster_addr, float v)
+{
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
+}
+// The sums of a tile whose K axis a cluster shares: CTA r of S finishes the tokens from r ceil(count / S) on.  Every CTA stores what it has of each
+// token in shared memory of the CTA that finishes it (the operand ring, which no CTA uses any more after the first barrier), and that one adds
+// the parts in their order.  All threads of the cluster.
+template <int EW, typename T>
+__device__ __forceinline__ void join(const Mx4GemmArgs &a, const Plan &plan, const Tile &tile, int32_t part, uint32_t tmem_base, float *parts)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, group = (warp - 3) >> 2, place = quarter * 32 + lane;
+    __syncwarp();
+    cluster_sync_all();
+    const int share = (tile.count + plan.split - 1) / plan.split;
+    if (warp >= 3) {
+        tc_fence_after();
+        for (int col = group * 32; col < tile.count; col += 8 * EW) {
+            uint32_t v[32];
+            tmem_ld_32x32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)col, v);
+            tmem_ld_wait();
+            int owner = col / share, in = col - owner * share;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                if (col + j < tile.count) store_remote(map_to_cta(smem_u32(parts + (part * share + in) * kTileRows + place), (uint32_t)owner), __uint_as_float(v[j]));
+                if (++in == share) {
+                    in = 0;
+                    ++owner;
+                }
+            }
+        }
+        tc_fence_before();
+    }
+    __syncwarp();
+    cluster_sync_all();
+    const int feature = tile.feature + place;
+    if (warp >= 3 && feature < a.N) {
+        const float bias = a.bias != nullptr ? __ldg(a.bias + feature) : 0.0f;
+        const int first = part * share, mine = min(share, tile.count - first);
+        for (int i = group; i < mine; i += EW / 4) {
+            float y = parts[i * kTileRows + place];
+            for (int q = 1; q < plan.split; ++q) y += parts[(q * share + i) * kTileRows + place];
+            y += bias;
+            float other;
+            if (a.act == Q8_ACT_GELU) gelu_fast_x2(pack_f32x2(y, y), y, other);
+            reinterpret_cast<T *>(a.Y)[(int64_t)(tile.row + first + i) * a.ldy + feature] = from_float<T>(y);
+        }
+    }
 }
 
 template <int CTAS, int BN, int EW, typename T, typename X>
@@ -268,7 +321,10 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
         if (CTAS == 2) tmem_alloc_pair(smem_u32(tmem_slot), C::kTmemCols);
         else tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
     }
-    const int32_t first_tile = blockIdx.x / CTAS, tile_step = gridDim.x / CTAS;
+    const int32_t split = CTAS == 1 ? plan.split : 1, unit = CTAS * split;  // CTAs of a tile
+    const int32_t first_tile = blockIdx.x / unit, tile_step = gridDim.x / unit;
+    const int32_t part = split > 1 ? blockIdx.x % split : 0;  // stages of the tile that are this CTA's
+    const int32_t kb_lo = split > 1 ? part * plan.num_kb / split : 0, kb_hi = split > 1 ? (part + 1) * plan.num_kb / split : plan.num_kb;
     if (warp == 2) {
         if (a.offsets != nullptr) {
             const bool bad = build_expert_table(table, a.offsets, a.E, (int32_t)a.M, plan.tile_n, plan.tiles_m);
@@ -331,9 +387,9 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
                                                  : 2 * (weights ? kTileBytes + kScaleBytes : (uint32_t)mine * 128 + kScaleBytes * (two_scales ? 1 : 0));
                 if (!waited && !(weights && early)) grid_dependency_wait();
                 waited = true;
-                const uint8_t *w = a.W + w_tile * kTileBytes, *x = a.X + x_tile * kTileBytes;
+                const uint8_t *w = a.W + (w_tile + kb_lo) * kTileBytes, *x = a.X + (x_tile + kb_lo) * kTileBytes;
                 bool ready = mbar_try_wait(smem_u32(empty_bar + s), phase ^ 1u);
-                for (int kb = 0; kb < plan.num_kb; ++kb) {
+                for (int kb = kb_lo; kb < kb_hi; ++kb) {
                     ok = ready || wait_on(smem_u32(empty_bar + s), phase ^ 1u, abort_flag, a.status);
                     if (!ok) break;
                     const int s_next = s + 1 == C::kStages ? 0 : s + 1;
@@ -423,7 +479,7 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
                 const uint32_t sub_col = (uint32_t)sub >> 5;
                 const bool two_blocks = sub + width > kTileRows;
                 bool ready = mbar_try_wait(smem_u32(full_bar + s), phase);
-                for (int kb = 0; kb < plan.num_kb; ++kb) {
+                for (int kb = kb_lo; kb < kb_hi; ++kb) {
                     ok = ready || wait_on(smem_u32(full_bar + s), phase, abort_flag, a.status);
                     if (!ok) break;
                     const int s_next = s + 1 == C::kStages ? 0 : s + 1;
@@ -448,19 +504,19 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
                     if (kb + 1 < plan.num_kb || last_blocks == kTileK / kBlock) {  // (a whole tile: without a test at every instruction)
                         scales(0);
                         scales(1);
-                        product(0, kb != 0);
+                        product(0, kb != kb_lo);
                         product(1, 1);
                         product(2, 1);
                         product(3, 1);
                     } else {
                         scales(0);
                         if (last_blocks > 4) scales(1);
-                        product(0, kb != 0);
+                        product(0, kb != kb_lo);
 #pragma unroll 1
                         for (int k = 1; 2 * k < last_blocks; ++k) product(k, 1);
                     }
                     commit(empty_bar + s);
-                    if (kb + 1 == plan.num_kb) commit(tmem_full_bar + as);
+                    if (kb + 1 == kb_hi) commit(tmem_full_bar + as);
                     s = s_next;
                     if (s == 0) phase ^= 1u;
                 }
@@ -488,9 +544,9 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
             if constexpr (FUSED) {
                 if (!waited) grid_dependency_wait();
                 waited = true;
-                const bool done = quantize_tokens<EW, C::kStages, C::kBBytes, C::kSbBytes, X>(a, plan, tile, ew, stage0, smem_b, smem_sb, full_bar, empty_bar, abort_flag);
+                const bool done = quantize_tokens<EW, C::kStages, C::kBBytes, C::kSbBytes, X>(a, plan, tile, kb_lo, kb_hi, ew, stage0, smem_b, smem_sb, full_bar, empty_bar, abort_flag);
                 if (!done) break;
-                stage0 += plan.num_kb;
+                stage0 += kb_hi - kb_lo;
             }
             const int feature0 = tile.feature + (int)rank * kTileRows + quarter * 32, feature = feature0 + lane;
             const bool mine = feature < a.N;
@@ -500,6 +556,7 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
             const bool ok = __all_sync(0xffffffffu, wait_for(smem_u32(tmem_full_bar + as), aphase, abort_flag, a.status));
             if (!ok) break;
             tc_fence_after();
+            if (CTAS == 1 && split > 1) break;  // (its only tile: on to the join)
             const uint32_t acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(as * C::kAccStride);
             auto release = [&]() {
                 tc_fence_before();
@@ -551,6 +608,10 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
             if (!released) release();
             if (++as == kAccStages) { as = 0; aphase ^= 1u; }
         }
+    }
+
+    if constexpr (CTAS == 1) {
+        if (split > 1) join<EW, T>(a, plan, list[0], part, tmem_base, reinterpret_cast<float *>(smem));
     }
 
     // ---------------- teardown (reached by every thread, also when aborting) ----------------
@@ -606,12 +667,12 @@ cudaError_t launch_typed(const Mx4GemmArgs &a, Plan plan, int64_t tiles, cudaStr
             !tiles_map(&maps.x32, a.X, x_tiles, 32) || !tiles_map(&maps.s, a.X, x_tiles, kScaleBytes / 128))
             return cudaErrorInvalidValue;
     }
-    const int64_t units = sm_count() / CTAS;
-    const int grid = (int)(tiles < units ? tiles : units) * CTAS;
+    const int64_t units = sm_count() / (CTAS * plan.split);
+    const int grid = (int)(tiles < units ? tiles : units) * CTAS * plan.split;
     LaunchInfo &li = last_launch_info();
     li.gemm_kernel = 1;
     li.block_n = plan.tile_n;
-    li.ctas = CTAS;
+    li.ctas = CTAS * plan.split;
     li.epilogue_warps = EW;
     li.grid = grid;
     li.launches += 1;
@@ -624,11 +685,11 @@ cudaError_t launch_typed(const Mx4GemmArgs &a, Plan plan, int64_t tiles, cudaStr
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = CTAS;
+    attr[1].val.clusterDim.x = CTAS * plan.split;
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = CTAS == 2 ? 2 : 1;
+    cfg.numAttrs = CTAS * plan.split > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, maps, a, plan);
 }
 
@@ -643,6 +704,24 @@ cudaError_t launch_shape(const Mx4GemmArgs &a, const Plan &plan, int64_t tiles, 
 }
 
 }  // namespace
+
+// CTAs that share the K axis of each of so many tiles of `tokens` tokens: a stage takes 0.21 us, the join 2.2 and 0.03 more for each token; clusters of 8
+// find room on the device together up to 12 (16 of them take two rounds: 1 x 8192 -> 2048 9.6 -> 11.8 us).  Shared / not, us: 1 x 8192 -> 512 5.7 / 9.4, 64
+// rows 8.5 / 10.2, 1 x 20000 -> 300 6.8 / 19.3, 1 x 4096 -> 1024 5.8 / 6.1, but 64 rows 8.4 / 7.1 and 1 x 2048 -> 256 5.5 / 4.3.
+int split_of(int64_t tiles, int num_kb, int64_t tokens)
+{
+    int best = 1;
+    double most = 0.2;
+    for (int split : {2, 4, 8}) {
+        if (num_kb < 2 * split || tiles * split > (split == 8 ? 96 : 112) || tiles * split > sm_count()) break;
+        const double gain = 0.21 * num_kb * (split - 1) / split - 2.2 - 0.03 * (double)tokens;
+        if (gain > most) {
+            best = split;
+            most = gain;
+        }
+    }
+    return best;
+}
 
 // Microseconds of `rounds` tiles one after the other: set-up, and for each tile its stages and what is not hidden under the next one's.
 // Fitted to 300 products (100 to 8192 tokens, K = 256 to 4096, 256 to 4096 features, bf16 without and fp32 with GELU) timed with
@@ -672,10 +751,12 @@ cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s)
     const int64_t hit = a.E < a.M ? a.E : a.M;  // experts with tokens, at most
     const int64_t extra = a.E > 1 ? hit : 0;    // tiles of tokens that are not full, at most
     const int64_t pairs = ceil_div(a.N, 2 * kTileRows);
+    p.split = 1;
     if (a.values != nullptr) {
         p.tile_n = kFusedTokens;
         p.x_vec = value_alignment(a.values, a.ldx, a.x_dtype == Q8_F32 ? 4 : 2);
-        const int64_t tiles = (ceil_div(a.M, p.tile_n) + extra) * p.tiles_m;
+        const int64_t tiles = ceil_div(a.M, p.tile_n) * p.tiles_m;
+        p.split = split_of(tiles, p.num_kb, a.M);
         switch (a.x_dtype) {
             case Q8_F32: return launch_shape<1, kFusedTokens, 8, float>(a, p, tiles, s);
             case Q8_F16: return launch_shape<1, kFusedTokens, 8, __half>(a, p, tiles, s);
@@ -697,6 +778,7 @@ cudaError_t launch_mx4_gemm(const Mx4GemmArgs &a, cudaStream_t s)
     p.tile_n = best;
     if (best == 256) p.tiles_m = (int32_t)pairs;
     const int64_t tiles = (ceil_div(a.M, best) + extra) * p.tiles_m;  // at most
+    if (best == 64 && a.offsets == nullptr) p.split = split_of(tiles, p.num_kb, a.M < 64 ? a.M : 64);
     if (best == 64) return launch_shape<1, 64, 8>(a, p, tiles, s);
     if (best == 128) return launch_shape<1, 128, 8>(a, p, tiles, s);
     // GELU keeps 16 warps busy; without it 8 with more registers are faster (24576 x 1024 -> 4096 bf16, 8 / 16 warps: 60 / 62 us, with GELU 95 / 82;

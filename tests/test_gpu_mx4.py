@@ -236,6 +236,13 @@ def test_linear_long_rows():
     run_layer(200, 300, 20001, torch.bfloat16, q8.Q8_ACT_NONE, True)
 
 
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5, 7, 8, 15, 31, 33, 63, 64, 65, 100, 128])
+@pytest.mark.parametrize("N,K", [(1, 2048), (130, 2049), (300, 4096), (1000, 8100), (40, 20000)])
+def test_linear_few_tiles_with_a_long_sum(M, N, K):
+    """The K axis of a tile shared by CTAs, which finish shares of its tokens: more tokens than CTAs, fewer, and none for some."""
+    run_layer(M, N, K, (torch.float32, torch.bfloat16)[M % 2], M % 3 == 0, M % 2 == 1, seed=M)
+
+
 def test_linear_scales_of_all_sizes():
     """Scales from the smallest to the largest exponent; products outside fp32's range are left to it."""
     x, w = values((70, 256), 1, spread=0.0), weights((160, 256), 2)
