@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     constexpr int R = kRows<KIND>;
     constexpr bool kSlots = KIND == kSlots1 || KIND == kSlots4;
     constexpr int kRowStep = KIND == kMatrix ? 32 : 1;
-    extern __shared__ int32_t table_words[];  // of slots: 2 (E + 1)
+    __shared__ int32_t table_words[kSlots ? 2 * (kMaxExperts + 1) : 1];
     // The product behind slots reads offsets and weights at once, so it starts when everything before this kernel has ended; the one behind a
     // matrix reads nothing before this kernel's end and may be set up as early as can be (16 x 4096 -> 1024 9.1 -> 8.7 us, 64 rows 8.2 -> 7.8).
     if (!kSlots) grid_dependency_release_next(true);
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
     if (kSlots) grid_dependency_release_next(true);
     const int lane = threadIdx.x & 31;
     const uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5);
-    ExpertTable table{table_words, table_words + a.E + 1, nullptr};
+    ExpertTable table{table_words, table_words + kMaxExperts + 1, nullptr};
     bool bad_index = false;
     if (kSlots) {
         if (threadIdx.x < 32) bad_index = build_expert_table(table, a.offsets, a.E, (int32_t)a.rows, 1, 1);
@@ -303,8 +303,7 @@ cudaError_t launch_kind(const Mx4QuantizeArgs &a, cudaStream_t s)
     const int vec = value_alignment(a.X, a.ld, sizeof(T)), vec_out = value_alignment(a.Xhat, a.ldo, sizeof(T));
     auto kernel = KIND == kSlots1 || KIND == kSlots4 || (vec > 0 && vec_out > 0) || !worth_shifting(a.groups * a.rows, a.K) ? mx4_quantize_kernel<T, KIND, true>
                                                                                                                      : mx4_quantize_kernel<T, KIND, false>;
-    const size_t smem = KIND == kSlots1 || KIND == kSlots4 ? 2 * (a.E + 1) * sizeof(int32_t) : 0;
-    return launch_overlapping_tail(kernel, grid, dim3(kThreads), smem, s, a, lines * splits, chunks, splits, row_lanes, vec, vec_out);
+    return launch_overlapping_tail(kernel, grid, dim3(kThreads), 0, s, a, lines * splits, chunks, splits, row_lanes, vec, vec_out);
 }
 
 template <typename T>

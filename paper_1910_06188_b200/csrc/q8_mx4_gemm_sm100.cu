@@ -40,6 +40,7 @@ using gemm_detail::gelu_fast_x2;
 constexpr int kAccStages = 2;
 constexpr int kScaleBytes = 2 * kAtomBytes;  // of a tile
 constexpr int kScaleCols = 4 * 2 + 8 * 2;    // TMEM columns of a stage's scales: 128 weight rows, 256 token rows, two atoms each
+constexpr int kFusedStages = 9;
 constexpr int kFusedTokens = 32;                // of a tile
 
 // A tile: expert and its first row block of tokens, the tile's first token (in the expert and as a row of Y), how many it has, its first feature.
@@ -47,28 +48,23 @@ struct __align__(16) Tile {
     int32_t expert, block, first, row, count, feature, pad[2];
 };
 constexpr int kListed = 64;  // tiles of a CTA that are worked out at the start
-constexpr int table_bytes(int E) { return 3 * (E + 1) * 4; }
-
 template <int CTAS, int BN, int EW, bool FUSED>
 struct Cfg {
     static constexpr int kThreads = 96 + 32 * EW;
     static constexpr int kBBytes = BN / CTAS * 128;
     static constexpr int kSbBytes = (BN > kTileRows ? 2 : 1) * kScaleBytes;  // of each row block that a tile's tokens may lie in
     static constexpr int kStageBytes = kTileBytes + kBBytes + kSbBytes;
-    static constexpr int kListBytes = kListed * (int)sizeof(Tile);
-    static constexpr int kBudget = 227 * 1024 - 1024 - kListBytes - table_bytes(kMaxExperts) - 512;
-    // Not all that fits: the quantise pass of the next call starts beside this kernel's last CTAs, if its own find room (32 slots on 64 experts, one
-    // call after the other: 12.0 us where they did not, 9.8 where they did).
-    static constexpr int kMostStages = FUSED ? 9 : CTAS == 2 ? 6 : 7;
-    static constexpr int kStages = kBudget / kStageBytes > kMostStages ? kMostStages : kBudget / kStageBytes;
+    static constexpr int kTableBytes = 3 * (kMaxExperts + 1) * 4 + 4 + kListed * (int)sizeof(Tile);
+    static constexpr int kBudget = 227 * 1024 - 1024 - kTableBytes - 512;
+    static constexpr int kStages = FUSED ? kFusedStages : kBudget / kStageBytes > 8 ? 8 : kBudget / kStageBytes;
     // Two accumulators of 256 columns leave no room for the scales: they share 48 columns, which the epilogue empties first.
     static constexpr int kAccStride = BN == 256 ? 512 - 2 * kScaleCols - 256 : BN;
     static constexpr int kScaleCol0 = kAccStride + BN;
     static constexpr int kTmemCols = kScaleCol0 + 2 * kScaleCols <= 128 ? 128 : kScaleCol0 + 2 * kScaleCols <= 256 ? 256 : 512;
     static constexpr int kBarrierBytes = (2 * kStages + 2 * kAccStages + 1) * 8 + 32;
-    static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kListBytes + kBarrierBytes;  // and the table of the experts that there are
+    static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kTableBytes + kBarrierBytes;
     static_assert(kScaleCol0 + 2 * kScaleCols <= 512, "TMEM columns");
-    static_assert(kSmemBytes + table_bytes(kMaxExperts) <= 232448 && kStages >= 3, "shared memory budget");
+    static_assert(kSmemBytes <= 232448 && kStages >= 3, "shared memory budget");
     static_assert(kBBytes % 1024 == 0 && (FUSED ? CTAS == 1 && BN == kFusedTokens : CTAS == 1 ? BN == 64 || BN == 128 : BN == 256) && (EW == 8 || EW == 16), "tile");
     // Instruction descriptor of kind::mxf4: E2M1 operands, both K-major, UE8M0 scales, M = 128 or 256 for the pair; N / 8 in bits
     // 17..22, which half of a scale word serves in bits 4..5 (B) and 29..30 (A).
@@ -302,11 +298,11 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
     uint64_t *drain_bar = tmem_empty_bar + kAccStages;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drain_bar + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    Tile *list = reinterpret_cast<Tile *>((reinterpret_cast<uintptr_t>(tmem_slot + 4) + 15) & ~uintptr_t(15));
     ExpertTable table;
-    table.start = reinterpret_cast<int32_t *>(list + kListed);
-    table.block = table.start + a.E + 1;
-    table.tile = table.block + a.E + 1;
+    table.start = reinterpret_cast<int32_t *>(tmem_slot + 4);
+    table.block = table.start + kMaxExperts + 1;
+    table.tile = table.block + kMaxExperts + 1;
+    Tile *list = reinterpret_cast<Tile *>((reinterpret_cast<uintptr_t>(table.tile + kMaxExperts + 1) + 15) & ~uintptr_t(15));
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;
@@ -659,7 +655,7 @@ cudaError_t launch_typed(const Mx4GemmArgs &a, Plan plan, int64_t tiles, cudaStr
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!attr_set[dev]) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes + table_bytes(kMaxExperts));
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
@@ -683,7 +679,7 @@ cudaError_t launch_typed(const Mx4GemmArgs &a, Plan plan, int64_t tiles, cudaStr
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(C::kThreads);
-    cfg.dynamicSmemBytes = C::kSmemBytes + table_bytes(a.E);
+    cfg.dynamicSmemBytes = C::kSmemBytes;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
