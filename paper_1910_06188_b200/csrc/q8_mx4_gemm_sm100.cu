@@ -317,6 +317,11 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
         if (lane == 0) *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    // A pair allocates together, so both of its CTAs have started first; after this the peer's barriers exist as well.
+    if (CTAS == 2) {
+        __syncwarp();
+        cluster_sync_all();
+    }
     if (warp == 1) {
         if (CTAS == 2) tmem_alloc_pair(smem_u32(tmem_slot), C::kTmemCols);
         else tmem_alloc(smem_u32(tmem_slot), C::kTmemCols);
@@ -351,7 +356,6 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
     __syncwarp();
     if (CTAS == 1 && a.offsets == nullptr && warp == 0) asm volatile("barrier.cta.arrive 1, %0;" ::"n"(C::kThreads) : "memory");
     else asm volatile("barrier.cta.sync 1, %0;" ::"n"(C::kThreads) : "memory");
-    if (CTAS == 2) cluster_sync_all();  // the peer's barriers exist before anything signals them
     tc_fence_after();
     const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(tmem_slot);  // (not yet there for that producer, which does not use it)
     grid_dependency_release_next(true);
@@ -393,7 +397,7 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
                     ok = ready || wait_on(smem_u32(empty_bar + s), phase ^ 1u, abort_flag, a.status);
                     if (!ok) break;
                     const int s_next = s + 1 == C::kStages ? 0 : s + 1;
-                    ready = mbar_try_wait(smem_u32(empty_bar + s_next), phase ^ (s_next == 0 ? 0u : 1u));  // (its answer is there by the time it is needed)
+                    if (kb + 1 < kb_hi) ready = mbar_try_wait(smem_u32(empty_bar + s_next), phase ^ (s_next == 0 ? 0u : 1u));  // (its answer is there by the time it is needed)
                     const uint32_t fb = smem_u32(full_bar + s);
                     const uint32_t dst_b = smem_u32(smem_b + s * C::kBBytes), dst_s = smem_u32(smem_sb + s * C::kSbBytes);
                     if constexpr (CTAS == 1) {
@@ -483,7 +487,7 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
                     ok = ready || wait_on(smem_u32(full_bar + s), phase, abort_flag, a.status);
                     if (!ok) break;
                     const int s_next = s + 1 == C::kStages ? 0 : s + 1;
-                    ready = mbar_try_wait(smem_u32(full_bar + s_next), phase ^ (s_next == 0 ? 1u : 0u));
+                    if (kb + 1 < kb_hi) ready = mbar_try_wait(smem_u32(full_bar + s_next), phase ^ (s_next == 0 ? 1u : 0u));  // (behind the last tile nothing would end this wait)
                     tc_fence_after();
                     const uint32_t da = a0 + (uint32_t)s * (kTileBytes >> 4), db = b0 + (uint32_t)s * (C::kBBytes >> 4);
                     const uint32_t dsa = sa0 + (uint32_t)s * (kTileBytes >> 4), dsb = sb0 + (uint32_t)s * (C::kSbBytes >> 4);
