@@ -4,6 +4,10 @@
 // shuffles, the scale that exponent less 2, the codes four conversions of two values each.  A warp takes 256 columns of
 // up to four rows, whose loads are all issued before the first is used.  For a plain matrix these are the rows r, r + 32,
 // r + 64 and r + 96 that lie side by side in an atom of scales, whose scales leave as 16 bytes of four lanes.
+//
+// Measured: fp32 is bound by memory (49152 x 1024 into tiles 34.6 us, DRAM 77 %; 4096 x 1024 with the gradient's copy 12.5 us = 82 % of the copy rate), 16-bit
+// values by instructions (8192 x 8192 bf16 30.9 us, ALU pipe 69 %, DRAM 56 %; in training 12288 x 4096 37 us = 5.4 TB/s).  Into tiles and
+// back, 24576 x 1024 bf16: 39 us for two passes, 89 % of the copy rate.
 
 #include "q8_mx4.cuh"
 

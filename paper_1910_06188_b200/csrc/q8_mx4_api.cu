@@ -9,7 +9,9 @@ namespace {
 
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 512;  // rows and tile ends are 32-bit coordinates on the device
 constexpr int64_t kMaxK = int64_t(1) << 24;
-constexpr int64_t kMaxPitch = int64_t(1) << 40;  // in values; row * pitch fits 64 bits with room
+constexpr int64_t kMaxSpan = int64_t(1) << 56;  // rows * pitch, in values: offsets in bytes fit 64 bits with room
+
+bool span_too_long(int64_t rows, int64_t ld) { return ld > kMaxSpan / (rows > 0 ? rows : 1); }
 
 bool aligned_to(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 bool known_dtype(int d) { return d == Q8_F32 || d == Q8_F16 || d == Q8_BF16; }
@@ -19,15 +21,15 @@ q8_status cuda_status(cudaError_t e) { return e == cudaSuccess ? Q8_OK : Q8_ERR_
 // [groups, rows, K] with rows ld values apart
 q8_status check_matrix(int64_t groups, int64_t rows, int64_t K, int64_t ld)
 {
-    if (groups < 0 || rows < 0 || K <= 0 || K > kMaxK || ld < K || ld > kMaxPitch) return Q8_ERR_SHAPE;
+    if (groups < 0 || rows < 0 || K <= 0 || K > kMaxK || ld < K) return Q8_ERR_SHAPE;
     if (groups > kMaxRows || rows > kMaxRows || (rows > 0 && groups > kMaxRows / rows)) return Q8_ERR_SHAPE;
-    return Q8_OK;
+    return span_too_long(groups * rows, ld) ? Q8_ERR_SHAPE : Q8_OK;
 }
 
 q8_status check_layer(int64_t M, int64_t N, int64_t K, int64_t E, int64_t ldy)
 {
     if (M < 0 || N < 0 || K <= 0 || E < 0) return Q8_ERR_SHAPE;
-    if (M > kMaxRows || N > kMaxRows || K > kMaxK || E > kMaxExperts || ldy < N || ldy > kMaxPitch) return Q8_ERR_SHAPE;
+    if (M > kMaxRows || N > kMaxRows || K > kMaxK || E > kMaxExperts || ldy < N || span_too_long(M, ldy)) return Q8_ERR_SHAPE;
     if (E > 0 && N > kMaxRows / E) return Q8_ERR_SHAPE;
     // tiles are counted in 32 bits
     if (((M + 63) / 64 + E) * ((N + 127) / 128) > 0x7fff0000) return Q8_ERR_SHAPE;
@@ -42,6 +44,12 @@ bool rows_overlap(const void *x, int64_t rows_x, int64_t a, int64_t pa, const vo
     if (pa != pb) return true;
     const int64_t d = (int64_t)(y0 >= x0 ? (y0 - x0) % (uintptr_t)pa : (pa - (int64_t)((x0 - y0) % (uintptr_t)pa)) % pa);
     return d < a || d + b > pa;
+}
+
+// The same for rows and one piece of memory, such as tiles or a workspace.
+bool rows_touch(const void *x, int64_t rows, int64_t a, int64_t pa, const void *piece, size_t bytes)
+{
+    return bytes > 0 && rows_overlap(x, rows, a, pa, piece, 1, (int64_t)bytes, (int64_t)bytes);
 }
 
 // The activation into the workspace and the product from there, or both in one kernel where the tokens are few.
@@ -92,6 +100,8 @@ q8_status q8_mx4_quantize(const void *X, int dtype, int64_t groups, int64_t rows
     if (groups == 0 || rows == 0) return Q8_OK;
     if (!X || !T) return Q8_ERR_NULL;
     if (!aligned_to(X, dtype_bytes(dtype)) || !aligned_to(T, 16) || !aligned_to(dev_status, 4)) return Q8_ERR_ALIGN;
+    const int64_t size = (int64_t)dtype_bytes(dtype);
+    if (rows_touch(X, groups * rows, K * size, ldx * size, T, q8_mx4_bytes(groups, rows, K))) return Q8_ERR_ARG;
     Mx4QuantizeArgs a = {};
     a.X = X;
     a.ld = ldx;
@@ -113,6 +123,8 @@ q8_status q8_mx4_dequantize(const uint8_t *T, int64_t groups, int64_t rows, int6
     if (groups == 0 || rows == 0) return Q8_OK;
     if (!Y || !T) return Q8_ERR_NULL;
     if (!aligned_to(Y, dtype_bytes(dtype)) || !aligned_to(T, 16)) return Q8_ERR_ALIGN;
+    const int64_t size = (int64_t)dtype_bytes(dtype);
+    if (rows_touch(Y, groups * rows, K * size, ldy * size, T, q8_mx4_bytes(groups, rows, K))) return Q8_ERR_ARG;
     return cuda_status(launch_mx4_dequantize(T, groups, rows, K, Y, dtype, ldy, static_cast<cudaStream_t>(stream)));
 }
 
@@ -160,6 +172,8 @@ q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Wq, const float *bia
     if (!aligned_to(Xq, 16) || !aligned_to(Wq, 16) || !aligned_to(bias, 4) ||
         !aligned_to(Y, dtype_bytes(y_dtype)) || !aligned_to(dev_status, 4))
         return Q8_ERR_ALIGN;
+    const int64_t ys = (int64_t)dtype_bytes(y_dtype);
+    if (rows_touch(Y, M, N * ys, ldy * ys, Xq, q8_mx4_bytes(1, M, K)) || rows_touch(Y, M, N * ys, ldy * ys, Wq, q8_mx4_bytes(1, N, K))) return Q8_ERR_ARG;
     Mx4GemmArgs g = {};
     g.X = Xq;
     g.W = Wq;
@@ -191,7 +205,10 @@ q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *
         return Q8_ERR_ALIGN;
     if (workspace_bytes < q8_mx4_linear_workspace_bytes(M, K)) return Q8_ERR_WORKSPACE;
     const int64_t xs = (int64_t)dtype_bytes(x_dtype), ys = (int64_t)dtype_bytes(y_dtype);
-    if (rows_overlap(X, M, K * xs, ldx * xs, Y, M, N * ys, ldy * ys)) return Q8_ERR_ARG;
+    const size_t scratch = q8_mx4_linear_workspace_bytes(M, K);
+    if (rows_overlap(X, M, K * xs, ldx * xs, Y, M, N * ys, ldy * ys) || rows_touch(Y, M, N * ys, ldy * ys, Wq, q8_mx4_bytes(1, N, K)) ||
+        rows_touch(Y, M, N * ys, ldy * ys, workspace, scratch) || rows_touch(X, M, K * xs, ldx * xs, workspace, scratch))
+        return Q8_ERR_ARG;
     Mx4GemmArgs g = {};
     g.W = Wq;
     g.bias = bias;
@@ -224,7 +241,10 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
         return Q8_ERR_ALIGN;
     if (workspace_bytes < q8_mx4_linear_grouped_workspace_bytes(T, experts, K)) return Q8_ERR_WORKSPACE;
     const int64_t xs = (int64_t)dtype_bytes(x_dtype), ys = (int64_t)dtype_bytes(y_dtype);
-    if (rows_overlap(X, x_rows, K * xs, ldx * xs, Y, T, N * ys, ldy * ys)) return Q8_ERR_ARG;
+    const size_t scratch = q8_mx4_linear_grouped_workspace_bytes(T, experts, K);
+    if (rows_overlap(X, x_rows, K * xs, ldx * xs, Y, T, N * ys, ldy * ys) || rows_touch(Y, T, N * ys, ldy * ys, Wq, q8_mx4_bytes(experts, N, K)) ||
+        rows_touch(Y, T, N * ys, ldy * ys, workspace, scratch) || rows_touch(X, x_rows, K * xs, ldx * xs, workspace, scratch))
+        return Q8_ERR_ARG;
     Mx4GemmArgs g = {};
     g.W = Wq;
     g.bias = bias;

@@ -90,6 +90,30 @@ def test_refusals(lib, call, arguments, status):
     assert call(lib, **arguments) == status
 
 
+
+TILE = 17408
+
+
+@pytest.mark.parametrize("call,arguments", [
+    # values on their own tiles; an output on tiles or on the workspace, at the first byte and the last; an input on the workspace
+    (quantize, {"out": FAKE}), (quantize, {"out": FAKE + 1008}), (quantize, {"X": FAKE + TILE - 4}), (dequantize, {}), (dequantize, {"Y": FAKE + TILE - 4}),
+    (dequantize, {"Y": FAKE - 1020}),
+    (linear_q, {"Xq": FAR, "Wq": FAKE}), (linear_q, {"Xq": FAKE, "Wq": FAR}), (linear_q, {"Xq": FAR, "Y": FAKE + TILE - 4}),
+    (linear, {"Y": FAR, "Wq": FAR}), (linear, {"Y": FAR + TILE - 4, "Wq": FAR}),
+    (linear, {"M": 130, "Y": FAR, "ws": FAR}), (linear, {"M": 130, "Y": FAR + 2 * TILE - 4, "ws": FAR}), (linear, {"M": 130, "X": FAKE, "ws": FAKE}),
+    (grouped, {"Wq": FAR}), (grouped, {"Y": FAR + 3 * TILE - 4, "Wq": FAR}), (grouped, {"ws": FAR}), (grouped, {"ws": FAKE}),
+    (grouped, {"x_rows": 1000, "rows": FAR, "X": FAKE, "ws": FAKE + 256 * 900})])
+def test_memory_used_twice_is_refused(lib, call, arguments):
+    assert call(lib, **arguments) == q8.Q8_ERR_ARG
+
+
+@pytest.mark.parametrize("call,arguments", [
+    (quantize, {"ld": 1 << 55}), (quantize, {"G": 1 << 10, "R": 1 << 10, "ld": 1 << 37}), (dequantize, {"ld": 1 << 62}), (fake, {"ldo": 1 << 55}),
+    (linear, {"ldx": 1 << 55}), (linear, {"ldy": 1 << 55}), (linear_q, {"ldy": (1 << 63) - 1}), (grouped, {"ldx": 1 << 55}), (grouped, {"ldy": 1 << 55})])
+def test_rows_too_far_apart_are_refused(lib, call, arguments):
+    assert call(lib, **arguments) == q8.Q8_ERR_SHAPE
+
+
 def test_tensors_of_the_host_are_refused(lib):
     W = q8.Mx4(torch.zeros(17408, dtype=torch.uint8), (8, 64))
     with pytest.raises(TypeError, match="X must be a CUDA tensor"):
