@@ -494,6 +494,57 @@ def test_weights_made_right_before_the_layer():
     assert all(torch.equal(a, b) for a, b in zip(got, [v for v in want for _ in range(2)]))
 
 
+
+@pytest.mark.parametrize("M,K,N,act,dtype", [(4096, 2048, 2048, q8.Q8_ACT_NONE, torch.bfloat16), (2304, 512, 1000, q8.Q8_ACT_GELU, torch.float32),
+                                             (300, 1024, 768, q8.Q8_ACT_NONE, torch.float16), (24, 4096, 512, q8.Q8_ACT_NONE, torch.bfloat16)])
+def test_calls_one_after_the_other(M, K, N, act, dtype):
+    """Hundreds of calls that nothing waits between, two inputs in turn: no wait runs out, and each gives what it gave alone."""
+    word = status_word()
+    xs = [values((M, K), s, dtype) for s in (1, 2)]
+    W = q8.q8_mx4_quantize(weights((N, K), 3))
+    want = []
+    for x in xs:
+        want.append(q8.q8_mx4_linear(x, W, act=act, dev_status=word))
+        torch.cuda.synchronize()
+    for _ in range(4):
+        for i in range(200):
+            y = q8.q8_mx4_linear(xs[i % 2], W, act=act, dev_status=word)
+            if i in (0, 63, 198, 199):
+                assert torch.equal(y, want[i % 2])
+        torch.cuda.synchronize()
+    assert word.item() == 0
+
+
+def test_offsets_and_experts_made_right_before_the_layer():
+    """The product reads offsets and weights before its own quantise pass ends, but after the kernels that wrote them."""
+    x = values((700, 512), 1)
+    layers = []
+    for seed, counts in enumerate([(300, 0, 400), (0, 700, 0), (1, 2, 697), (233, 234, 233)]):
+        w = torch.stack([weights((384, 512), 10 * seed + e) for e in range(3)])
+        layers.append((w, torch.tensor(counts, dtype=torch.int32, device="cuda")))
+
+    def offsets_of(counts):
+        return torch.cat([counts.new_zeros(1), counts.cumsum(0, dtype=torch.int32)])
+
+    want = []
+    for w, counts in layers:
+        W, offsets = q8.q8_mx4_quantize(w), offsets_of(counts)
+        torch.cuda.synchronize()
+        want.append(q8.q8_mx4_linear_grouped(x, offsets, W))
+        torch.cuda.synchronize()
+    offsets, W = offsets_of(layers[0][1]), q8.q8_mx4_quantize(layers[0][0])
+    got = []
+    for _ in range(10):
+        for w, counts in layers:
+            fresh = q8.q8_mx4_quantize(w)
+            W.tiles.copy_(fresh.tiles)
+            offsets.copy_(offsets_of(counts))
+            got.append(q8.q8_mx4_linear_grouped(x, offsets, W))
+            offsets.copy_(offsets_of(counts))
+            got.append(q8.q8_mx4_linear_grouped(x, offsets, q8.q8_mx4_quantize(w)))
+    assert all(torch.equal(a, want[i // 2 % 4]) for i, a in enumerate(got))
+
+
 def test_refusals_on_the_device():
     x, w = values((4, 64), 1), weights((8, 64), 2)
     W = q8.q8_mx4_quantize(w)
