@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
         for (int j = 0; j < R; ++j) {
             const int32_t slot = first + j;
             int64_t from = slot;
-            if (a.index != nullptr && slot < rows) from = __ldg(a.index + slot);
+            if (a.index != nullptr && slot < rows) from = __ldcg(a.index + slot);
             while (expert < a.E && table.start[expert + 1] <= slot) ++expert;
             const bool owned = slot < rows && expert < a.E && slot >= table.start[expert];
             there[j] = owned && from >= 0 && from < a.x_rows;  // else it counts as a row of zeros
@@ -266,8 +266,9 @@ mx4_dequantize_kernel(const uint8_t *tiles, uint32_t groups, uint32_t rows, int3
     for (uint32_t j = 0; j < 4; ++j) {
         const uint32_t row = min(first + j, all - 1), group = groups > 1 ? row / rows : 0, r = row - group * rows;
         const uint8_t *tile = tiles + ((int64_t)(group * blocks + r / kTileRows) * chunks + chunk) * kTileBytes;
-        c[j] = __ldg(reinterpret_cast<const uint32_t *>(tile + code_place((int)(r % kTileRows), lane)));
-        E[j] = __ldg(tile + scale_place((int)(r % kTileRows), lane >> 2));
+        // (not as read-only data: a kernel that writes them may end after this one has started)
+        c[j] = __ldcg(reinterpret_cast<const uint32_t *>(tile + code_place((int)(r % kTileRows), lane)));
+        E[j] = __ldcg(tile + scale_place((int)(r % kTileRows), lane >> 2));
     }
     T *y = Y + first * ldy;
 #pragma unroll

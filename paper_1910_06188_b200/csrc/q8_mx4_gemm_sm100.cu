@@ -269,7 +269,7 @@ __device__ __forceinline__ void join(const Mx4GemmArgs &a, const Plan &plan, con
     cluster_sync_all();
     const int feature = tile.feature + place;
     if (warp >= 3 && feature < a.N) {
-        const float bias = a.bias != nullptr ? __ldg(a.bias + feature) : 0.0f;
+        const float bias = a.bias != nullptr ? __ldcg(a.bias + feature) : 0.0f;
         const int first = part * share, mine = min(share, tile.count - first);
         for (int i = group; i < mine; i += EW / 4) {
             float y = parts[i * kTileRows + place];
@@ -558,9 +558,9 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
             }
             const int feature0 = tile.feature + (int)rank * kTileRows + quarter * 32, feature = feature0 + lane;
             const bool mine = feature < a.N;
-            if (!waited) grid_dependency_wait();  // (an earlier kernel may have written the bias, or still read Y)
+            if (!waited) grid_dependency_wait();  // (an earlier kernel may have written the bias, which is not read-only data therefore, or still read Y)
             waited = true;
-            const float bias = mine && a.bias != nullptr ? __ldg(a.bias + (int64_t)tile.expert * a.N + feature) : 0.0f;
+            const float bias = mine && a.bias != nullptr ? __ldcg(a.bias + (int64_t)tile.expert * a.N + feature) : 0.0f;
             const bool ok = __all_sync(0xffffffffu, wait_for(smem_u32(tmem_full_bar + as), aphase, abort_flag, a.status));
             if (!ok) break;
             tc_fence_after();

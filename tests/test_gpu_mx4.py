@@ -545,6 +545,41 @@ def test_offsets_and_experts_made_right_before_the_layer():
     assert all(torch.equal(a, want[i // 2 % 4]) for i, a in enumerate(got))
 
 
+
+@pytest.mark.parametrize("M", [1, 3, 40, 200])
+def test_everything_made_right_before_the_layer(M):
+    """Activation, bias and weights come from kernels of the library right before, call after call in the same memory."""
+    K, N, sets = 256, 384, 5
+    xs, bs, ws = ([q8.q8_mx4_quantize(f(shape, 3 * i + j)) for i in range(sets)] for j, (f, shape) in enumerate(((values, (M, K)), (weights, (1, N)), (weights, (N, K)))))
+    want = []
+    for x, b, w in zip(xs, bs, ws):
+        x, b, w = (q8.q8_mx4_dequantize(t) for t in (x, b, w))
+        torch.cuda.synchronize()
+        w = q8.q8_mx4_quantize(w)
+        torch.cuda.synchronize()
+        want.append(q8.q8_mx4_linear(x, w, b[0]))
+        torch.cuda.synchronize()
+    got = []
+    for i in range(300):
+        x, b, w = (q8.q8_mx4_dequantize(t[i % sets]) for t in (xs, bs, ws))
+        got.append(q8.q8_mx4_linear(x, q8.q8_mx4_quantize(w), b[0]))
+        x = b = w = None  # the next call's are in the same places
+    assert all(torch.equal(y, want[i % sets]) for i, y in enumerate(got))
+
+
+def test_tiles_rewritten_between_readings():
+    tiles = torch.empty(q8.q8_mx4_bytes(1, 200, 512), dtype=torch.uint8, device="cuda")
+    xs = [values((200, 512), s) for s in range(4)]
+    lib, stream = q8.load(), torch.cuda.current_stream().cuda_stream
+    want = [q8.q8_mx4_dequantize(q8.q8_mx4_quantize(x)) for x in xs]
+    torch.cuda.synchronize()
+    got = torch.empty(200, 200, 512, device="cuda")
+    for i in range(200):
+        assert lib.q8_mx4_quantize(xs[i % 4].data_ptr(), q8.Q8_F32, 1, 200, 512, 512, tiles.data_ptr(), None, stream) == q8.Q8_OK
+        assert lib.q8_mx4_dequantize(tiles.data_ptr(), 1, 200, 512, got[i].data_ptr(), q8.Q8_F32, 512, stream) == q8.Q8_OK
+    assert all(torch.equal(got[i], want[i % 4]) for i in range(200))
+
+
 def test_refusals_on_the_device():
     x, w = values((4, 64), 1), weights((8, 64), 2)
     W = q8.q8_mx4_quantize(w)
