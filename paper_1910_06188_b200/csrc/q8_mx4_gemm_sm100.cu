@@ -358,11 +358,15 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
     // A plain product's weight producer, which made the barriers and needs neither the list nor TMEM, goes ahead without the others.
     tc_fence_before();
     __syncwarp();
-    if (CTAS == 1 && a.offsets == nullptr && warp == 0) asm volatile("barrier.cta.arrive 1, %0;" ::"n"(C::kThreads) : "memory");
+    const bool goes_ahead = CTAS == 1 && a.offsets == nullptr && warp == 0;
+    if (goes_ahead) asm volatile("barrier.cta.arrive 1, %0;" ::"n"(C::kThreads) : "memory");
     else asm volatile("barrier.cta.sync 1, %0;" ::"n"(C::kThreads) : "memory");
     tc_fence_after();
     const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(tmem_slot);  // (not yet there for that producer, which does not use it)
-    grid_dependency_release_next(true);
+    // The next kernel may be parked beside single CTAs with up to three rounds of tiles, as beside the 8-bit GEMM, and only once this CTA has its
+    // tensor memory, whose allocation waits without a limit.  Beside longer products and pairs nothing is parked: they let the next one start
+    // when they end.
+    if (!goes_ahead) grid_dependency_release_next(CTAS == 1 && (a.offsets != nullptr ? table.tile[a.E] : plan.tiles) <= 3 * tile_step);
 
     Tile tile;
     auto width_of = [&](const Tile &t) { return (t.count + kStep - 1) / kStep * kStep; };
