@@ -447,6 +447,12 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
                     if (s == 0) phase ^= 1u;
                 }
             }
+            // Every stage has been given back before the CTA ends: the issuer's last commits arrive at these barriers, a pair's at the peer's
+            // too, and nothing else waits for them.
+            for (int i = 0; ok && i < C::kStages; ++i) {
+                ok = wait_for(smem_u32(empty_bar + s), phase ^ 1u, abort_flag, a.status);
+                if (++s == C::kStages) { s = 0; phase ^= 1u; }
+            }
             if (!ok) {
                 // Aborting: this warp's copies land before the CTA gives up its shared memory (bounded: the other producer may have stopped
                 // a stage earlier, and its barrier then never completes).

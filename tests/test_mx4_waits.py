@@ -27,3 +27,10 @@ def test_the_next_kernel_is_let_in_behind_the_allocation(kernel):
     allocated, met, released = (kernel.index(t) for t in ("tmem_alloc(", "barrier.cta.sync 1", "grid_dependency_release_next("))
     assert allocated < met < released
     assert re.search(r"if \(goes_ahead\) asm volatile\(\"barrier\.cta\.arrive", kernel) and "if (!goes_ahead) grid_dependency_release_next(" in kernel
+
+
+def test_every_stage_is_given_back_before_a_cta_ends(kernel):
+    """The issuer's last arrivals, in a pair at the barriers of both CTAs, are waited for while the CTA still owns them (with a limit)."""
+    producers = kernel[kernel.index("if (warp == 0 || (warp == 2 && !FUSED))"):kernel.index("} else if (warp == 1)")]
+    behind = producers[producers.rindex("++issued;"):]
+    assert re.search(r"for \(int i = 0; ok && i < C::kStages; \+\+i\) \{\s*ok = wait_for\(smem_u32\(empty_bar \+ s\), phase \^ 1u, abort_flag, a\.status\);", behind)
