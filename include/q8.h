@@ -55,7 +55,7 @@ typedef enum {
 
 /* Activation applied after dequantisation (Sec. 3 keeps GELU in FP32). */
 #define Q8_ACT_NONE 0
-#define Q8_ACT_GELU 1 /* y * Phi(y), erf form */
+#define Q8_ACT_GELU 1 /* y * Phi(y), erf form, to 1e-7 and rounding; NaN stays NaN, of -infinity the tensor-core kernels give the limit, 0 */
 
 /* Eq. 3 followed by Eq. 1 (one-time weight preparation; also used for embedding tables).
  *   W      [N, K] fp32, read.

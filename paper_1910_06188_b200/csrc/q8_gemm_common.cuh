@@ -25,6 +25,14 @@ constexpr int kStagingBytesPerWarp = 32 * 32 * 4;  // the 32 x 32 fp32 block one
 // instruction, each half rounded like a scalar fmaf) in n = -a = max(-|y|, -5.6), i.e. with the odd
 // coefficients negated, so the last step needs no negation: gelu = n * 2^p + max(y, 0).
 // Per value: three packed FMA-pipe instructions and a half, one ex2, two min/max.
+// What is not finite: NaN stays NaN (the positive part carries it; the clamp below drops it), infinity stays, -infinity gives the limit, 0, within the same
+// 1e-7.
+__device__ __forceinline__ float positive_part(float y)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(y));
+    return r;
+}
 __device__ __forceinline__ void gelu_fast_x2(uint64_t y2, float &out_lo, float &out_hi)
 {
     float y0, y1;
@@ -41,7 +49,7 @@ __device__ __forceinline__ void gelu_fast_x2(uint64_t y2, float &out_lo, float &
     unpack_f32x2(p, p0, p1);
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(p0));
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(p1));
-    const uint64_t r = fma_f32x2(n, pack_f32x2(e0, e1), pack_f32x2(fmaxf(y0, 0.0f), fmaxf(y1, 0.0f)));
+    const uint64_t r = fma_f32x2(n, pack_f32x2(e0, e1), pack_f32x2(positive_part(y0), positive_part(y1)));
     unpack_f32x2(r, out_lo, out_hi);
 }
 

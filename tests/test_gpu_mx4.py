@@ -615,3 +615,38 @@ def test_refusals_on_the_device():
     with pytest.raises(TypeError, match="offsets must be torch.int32"):
         q8.q8_mx4_linear_grouped(x, torch.zeros(3, dtype=torch.int64, device="cuda"), G)
     torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------- what is not finite, behind the product
+@pytest.mark.parametrize("out", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("M,N,K,tokens,ctas", [(2, 300, 64, 32, {1}), (2, 200, 8192, 32, {2, 4, 8}), (5, 200, 8192, 64, {2, 4, 8}), (40, 300, 200, 64, {1}),
+                                               (4096, 2400, 96, 128, {1}), (4096, 2400, 2100, 256, {2})])
+def test_gelu_of_what_is_not_finite(M, N, K, tokens, ctas, out):
+    """A NaN in the bias, or of sums of opposite infinities, stays NaN; +inf stays; of -inf the limit, 0.  In each way a sum takes to Y."""
+    x, w, b = values((M, K), 1, spread=0.0), weights((N, K), 2), weights((N,), 3)
+    b[0], b[1], b[2], b[N - 1] = float("nan"), float("inf"), -float("inf"), float("nan")
+    # row 1: features 5 and 6 overflow to either side, feature 7 has both signs in its sum, and in feature 2 the sum's infinity meets the bias's
+    x[1] = 2.0 ** 101
+    w[2], w[5], w[6], w[7] = 2.0 ** 101, 2.0 ** 101, -2.0 ** 101, 2.0 ** 101
+    w[7, : K // 2] *= -1
+    W = q8.q8_mx4_quantize(w)
+    plain, got = (q8.q8_mx4_linear(x, W, b, act, dtype=out) for act in (q8.Q8_ACT_NONE, q8.Q8_ACT_GELU))
+    info = q8.q8_last_launch_info()
+    assert info["block_n"] == tokens and info["ctas"] in ctas
+    others = [0, *range(2, M)]
+    assert torch.isnan(plain[:, [0, N - 1]]).all() and torch.isposinf(plain[others, 1]).all() and torch.isneginf(plain[others, 2]).all()
+    assert torch.isposinf(plain[1, 5]) and torch.isneginf(plain[1, 6]) and torch.isnan(plain[1, 2])
+    assert torch.equal(torch.isnan(got), torch.isnan(plain)), "NaN where the sums are, and nowhere else"
+    assert torch.equal(torch.isposinf(got), torch.isposinf(plain))
+    low = torch.isneginf(plain)
+    assert low[1, 6] and (got[low].abs() <= 1e-7).all()
+
+
+def test_gelu_of_what_is_not_finite_grouped():
+    x, w, b = values((300, 128), 1, spread=0.0), weights((3, 200, 128), 2), weights((3, 200), 3)
+    b[0, 7], b[2, 199], b[2, 3] = float("nan"), float("nan"), -float("inf")
+    offsets = torch.tensor([0, 100, 140, 300], dtype=torch.int32).cuda()
+    y = q8.q8_mx4_linear_grouped(x, offsets, q8.q8_mx4_quantize(w), b, q8.Q8_ACT_GELU)
+    want = torch.zeros(300, 200, dtype=torch.bool, device="cuda")
+    want[:100, 7], want[140:, 199] = True, True
+    assert torch.equal(torch.isnan(y), want) and (y[140:, 3].abs() <= 1e-7).all()
