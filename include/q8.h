@@ -286,8 +286,8 @@ q8_status q8_attention_status_word(void **dev_status);
  *     0 behind the last block
  * Common to the calls below: dtype is one of Q8_F32, Q8_F16, Q8_BF16; ld* is the distance of two rows in values (at least their
  * length); tiles are 16-byte aligned, values aligned to their type; 1 <= K <= 2^24, rows below 2^31 - 512, rows times ld* up to 2^56;
- * dev_status (may be NULL) is OR-ed into, never cleared; outputs overlap no input (Q8_ERR_ARG); calls that share a workspace must be
- * ordered on the stream.  Zero rows or features are a no-op.  Waits inside the product's kernel are bounded: one that expires flags
+ * dev_status (may be NULL) is OR-ed into, never cleared; outputs and workspaces overlap no input and not each other (Q8_ERR_ARG, also for rows of two
+ * different pitches in one stretch of memory); calls that share a workspace must be ordered on the stream.  Zero rows or features are a no-op.  Waits inside the product's kernel are bounded: one that expires flags
  * Q8_ERR_TIMEOUT in dev_status, and Y is then not to be used. */
 #define Q8_F32 0
 #define Q8_F16 1

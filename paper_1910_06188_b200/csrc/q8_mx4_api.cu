@@ -46,10 +46,30 @@ bool rows_overlap(const void *x, int64_t rows_x, int64_t a, int64_t pa, const vo
     return d < a || d + b > pa;
 }
 
-// The same for rows and one piece of memory, such as tiles or a workspace.
+// The same for rows and one piece of memory, such as tiles, a workspace or a bias.  (A piece between two rows touches neither.)
 bool rows_touch(const void *x, int64_t rows, int64_t a, int64_t pa, const void *piece, size_t bytes)
 {
-    return bytes > 0 && rows_overlap(x, rows, a, pa, piece, 1, (int64_t)bytes, (int64_t)bytes);
+    const int64_t b = (int64_t)bytes;
+    return piece != nullptr && bytes > 0 && rows_overlap(x, rows, a, pa, piece, 1, b, b < pa ? pa : b);
+}
+
+bool pieces_touch(const void *x, size_t a, const void *y, size_t b)
+{
+    const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), y0 = reinterpret_cast<uintptr_t>(y);
+    return x != nullptr && y != nullptr && a > 0 && b > 0 && x0 < y0 + b && y0 < x0 + a;
+}
+
+// Whether a layer would write what it also reads: Y over weights, bias, offsets or rows, the workspace over any of them or over Y.
+bool layer_overlaps(const Mx4GemmArgs &g, const int32_t *index, const void *workspace, size_t scratch)
+{
+    const int64_t size = (int64_t)dtype_bytes(g.y_dtype);
+    const struct { const void *p; size_t bytes; } read[] = {{g.W, q8_mx4_bytes(g.E, g.N, g.K)},
+                                                            {g.bias, (size_t)g.E * (size_t)g.N * sizeof(float)},
+                                                            {g.offsets, ((size_t)g.E + 1) * sizeof(int32_t)},
+                                                            {index, (size_t)g.M * sizeof(int32_t)}};
+    for (const auto &r : read)
+        if (rows_touch(g.Y, g.M, g.N * size, g.ldy * size, r.p, r.bytes) || pieces_touch(workspace, scratch, r.p, r.bytes)) return true;
+    return rows_touch(g.Y, g.M, g.N * size, g.ldy * size, workspace, scratch);
 }
 
 // The activation into the workspace and the product from there, or both in one kernel where the tokens are few.
@@ -172,8 +192,6 @@ q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Wq, const float *bia
     if (!aligned_to(Xq, 16) || !aligned_to(Wq, 16) || !aligned_to(bias, 4) ||
         !aligned_to(Y, dtype_bytes(y_dtype)) || !aligned_to(dev_status, 4))
         return Q8_ERR_ALIGN;
-    const int64_t ys = (int64_t)dtype_bytes(y_dtype);
-    if (rows_touch(Y, M, N * ys, ldy * ys, Xq, q8_mx4_bytes(1, M, K)) || rows_touch(Y, M, N * ys, ldy * ys, Wq, q8_mx4_bytes(1, N, K))) return Q8_ERR_ARG;
     Mx4GemmArgs g = {};
     g.X = Xq;
     g.W = Wq;
@@ -187,6 +205,8 @@ q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Wq, const float *bia
     g.act = act;
     g.E = 1;
     g.status = dev_status;
+    const int64_t ys = (int64_t)dtype_bytes(y_dtype);
+    if (layer_overlaps(g, nullptr, nullptr, 0) || rows_touch(Y, M, N * ys, ldy * ys, Xq, q8_mx4_bytes(1, M, K))) return Q8_ERR_ARG;
     return cuda_status(launch_mx4_gemm(g, static_cast<cudaStream_t>(stream)));
 }
 
@@ -206,9 +226,6 @@ q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *
     if (workspace_bytes < q8_mx4_linear_workspace_bytes(M, K)) return Q8_ERR_WORKSPACE;
     const int64_t xs = (int64_t)dtype_bytes(x_dtype), ys = (int64_t)dtype_bytes(y_dtype);
     const size_t scratch = q8_mx4_linear_workspace_bytes(M, K);
-    if (rows_overlap(X, M, K * xs, ldx * xs, Y, M, N * ys, ldy * ys) || rows_touch(Y, M, N * ys, ldy * ys, Wq, q8_mx4_bytes(1, N, K)) ||
-        rows_touch(Y, M, N * ys, ldy * ys, workspace, scratch) || rows_touch(X, M, K * xs, ldx * xs, workspace, scratch))
-        return Q8_ERR_ARG;
     Mx4GemmArgs g = {};
     g.W = Wq;
     g.bias = bias;
@@ -221,6 +238,9 @@ q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *
     g.act = act;
     g.E = 1;
     g.status = dev_status;
+    if (layer_overlaps(g, nullptr, workspace, scratch) || rows_overlap(X, M, K * xs, ldx * xs, Y, M, N * ys, ldy * ys) ||
+        rows_touch(X, M, K * xs, ldx * xs, workspace, scratch))
+        return Q8_ERR_ARG;
     return quantize_and_multiply(g, X, x_dtype, ldx, M, nullptr, workspace, static_cast<cudaStream_t>(stream));
 }
 
@@ -242,9 +262,6 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
     if (workspace_bytes < q8_mx4_linear_grouped_workspace_bytes(T, experts, K)) return Q8_ERR_WORKSPACE;
     const int64_t xs = (int64_t)dtype_bytes(x_dtype), ys = (int64_t)dtype_bytes(y_dtype);
     const size_t scratch = q8_mx4_linear_grouped_workspace_bytes(T, experts, K);
-    if (rows_overlap(X, x_rows, K * xs, ldx * xs, Y, T, N * ys, ldy * ys) || rows_touch(Y, T, N * ys, ldy * ys, Wq, q8_mx4_bytes(experts, N, K)) ||
-        rows_touch(Y, T, N * ys, ldy * ys, workspace, scratch) || rows_touch(X, x_rows, K * xs, ldx * xs, workspace, scratch))
-        return Q8_ERR_ARG;
     Mx4GemmArgs g = {};
     g.W = Wq;
     g.bias = bias;
@@ -258,6 +275,9 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
     g.offsets = offsets;
     g.E = (int)experts;
     g.status = dev_status;
+    if (layer_overlaps(g, rows, workspace, scratch) || rows_overlap(X, x_rows, K * xs, ldx * xs, Y, T, N * ys, ldy * ys) ||
+        rows_touch(X, x_rows, K * xs, ldx * xs, workspace, scratch))
+        return Q8_ERR_ARG;
     return quantize_and_multiply(g, X, x_dtype, ldx, x_rows, rows, workspace, static_cast<cudaStream_t>(stream));
 }
 

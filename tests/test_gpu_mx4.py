@@ -650,3 +650,17 @@ def test_gelu_of_what_is_not_finite_grouped():
     want = torch.zeros(300, 200, dtype=torch.bool, device="cuda")
     want[:100, 7], want[140:, 199] = True, True
     assert torch.equal(torch.isnan(y), want) and (y[140:, 3].abs() <= 1e-7).all()
+
+
+def test_bias_between_the_rows_of_the_output():
+    """What lies between two rows of Y is not Y's: a bias there is read and stays."""
+    for M in (2, 40):
+        x, w, b = values((M, 256), M, spread=0.5), weights((100, 256), 2), weights((100,), 3)
+        both = torch.zeros(M, 512, device="cuda")
+        both[1, 200:300] = b
+        q8.q8_mx4_linear(x, q8.q8_mx4_quantize(w), both[1, 200:300], Y=both[:, :100])
+        ref.assert_layer(both[:, :100], ref.rounded(x), ref.rounded(w), b, q8.Q8_ACT_NONE)
+        assert torch.equal(both[1, 200:300], b) and (both[0, 100:] == 0).all()
+        with pytest.raises(q8.Q8Error) as e:
+            q8.q8_mx4_linear(x, q8.q8_mx4_quantize(w), both[1, 50:150], Y=both[:, :100])
+        assert e.value.status == q8.Q8_ERR_ARG

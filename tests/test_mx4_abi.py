@@ -107,6 +107,29 @@ def test_memory_used_twice_is_refused(lib, call, arguments):
     assert call(lib, **arguments) == q8.Q8_ERR_ARG
 
 
+# every pointer at a place of its own
+APART = dict(X=1 << 32, Wq=2 << 32, Y=3 << 32, ws=4 << 32)
+GROUPED = dict(APART, offsets=5 << 32, rows=6 << 32, bias=7 << 32)
+
+
+@pytest.mark.parametrize("call,arguments", [
+    # Y [4, 8] fp32 over the bias, its first value and its last, and the other way round; in rows 100 values apart on one row, or with a bias longer than that
+    *[(linear, dict(APART, **more)) for more in (
+        {"bias": APART["Y"]}, {"bias": APART["Y"] + 4 * 31}, {"bias": APART["Y"] - 4 * 7}, {"ldy": 100, "bias": APART["Y"] + 4 * 307},
+        {"ldy": 100, "bias": APART["Y"] + 4 * 93}, {"ldy": 100, "N": 60, "bias": APART["Y"] + 4 * 41})],
+    *[(linear_q, dict(Xq=1 << 32, Wq=2 << 32, Y=3 << 32, bias=(3 << 32) + o)) for o in (0, 4 * 31, -4 * 7)],
+    # a workspace over weights and bias
+    *[(linear, dict(APART, M=130, **more)) for more in (
+        {"ws": APART["Wq"]}, {"ws": APART["Wq"] + 256 * ((TILE - 1) // 256)}, {"ws": APART["Wq"] - 2 * TILE + 256}, {"bias": APART["ws"]},
+        {"bias": APART["ws"] + 2 * TILE - 4}, {"bias": APART["ws"] - 4 * 7})],
+    # the grouped layer: Y, and the workspace (3 tiles), over weights, bias [3, 8], offsets [4] and rows [4]
+    *[(grouped, dict(GROUPED, **{k: GROUPED["Y"] + o})) for k, n in (("bias", 24), ("offsets", 4), ("rows", 4)) for o in (0, 4 * 31, -4 * (n - 1))],
+    *[(grouped, dict(GROUPED, **{k: GROUPED["ws"] + o})) for k, n in (("bias", 24), ("offsets", 4), ("rows", 4)) for o in (0, 3 * TILE - 4, -4 * (n - 1))],
+    (grouped, dict(GROUPED, ws=GROUPED["Wq"])), (grouped, dict(GROUPED, ws=GROUPED["Wq"] + 256)), (grouped, dict(GROUPED, ws=GROUPED["Wq"] - 3 * TILE + 256))])
+def test_outputs_and_workspaces_over_every_input_are_refused(lib, call, arguments):
+    assert call(lib, **arguments) == q8.Q8_ERR_ARG
+
+
 @pytest.mark.parametrize("call,arguments", [
     (quantize, {"ld": 1 << 55}), (quantize, {"G": 1 << 10, "R": 1 << 10, "ld": 1 << 37}), (dequantize, {"ld": 1 << 62}), (fake, {"ldo": 1 << 55}),
     (linear, {"ldx": 1 << 55}), (linear, {"ldy": 1 << 55}), (linear_q, {"ldy": (1 << 63) - 1}), (grouped, {"ldx": 1 << 55}), (grouped, {"ldy": 1 << 55})])
