@@ -664,3 +664,63 @@ def test_bias_between_the_rows_of_the_output():
         with pytest.raises(q8.Q8Error) as e:
             q8.q8_mx4_linear(x, q8.q8_mx4_quantize(w), both[1, 50:150], Y=both[:, :100])
         assert e.value.status == q8.Q8_ERR_ARG
+
+
+# ---------------------------------------------------------------- many rows at any address
+MANY_ROWS = 33 * 128  # whole tiles, so that every byte of them is defined; with K >= 256 over 2^20 values, from which on the kernels move bytes to their places
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("K", [256, 257, 263, 264, 511, 1035])
+def test_many_rows_at_any_address(K, dtype):
+    """test_rows_at_any_address for the kernels that large tensors take: every place of a row in its 16 bytes, rows that all begin at another one, values, and
+    nothing beside them read as theirs or written."""
+    assert K >= 256 and MANY_ROWS * K >= 1 << 20
+    x0 = values((MANY_ROWS, K), K, dtype)
+    aligned = torch.zeros(MANY_ROWS, (K + 31) // 32 * 32, dtype=dtype, device="cuda")
+    aligned[:, :K] = x0
+    t0 = q8.q8_mx4_quantize(aligned[:, :K])  # rows at multiples of 32 bytes: checked against the definition, the others against it
+    check_codes(t0, x0)
+    want = torch.from_numpy(ref.rounded(x0)).to(dtype).cuda()
+    assert torch.equal(q8.q8_mx4_fake_quantize(aligned[:, :K]), want)
+    lib, stream = q8.load(), torch.cuda.current_stream().cuda_stream
+    for offset in range(0, 9):
+        for ld in (K + 9, K + 10, K + 16 - K % 8):
+            whole = torch.full((MANY_ROWS + 2, ld), float("nan"), dtype=dtype, device="cuda")
+            rows = whole[1:-1, offset:offset + K]
+            rows.copy_(x0)
+            word = status_word()
+            t = q8.q8_mx4_quantize(rows, dev_status=word)
+            assert word.item() == 0, "a NaN beside the rows was taken for one of theirs"
+            assert torch.equal(t.tiles, t0.tiles)
+            out = torch.full((MANY_ROWS + 2, ld + 3), 5.0, dtype=dtype, device="cuda")
+            place = (slice(1, -1), slice((offset + 1) % 9, (offset + 1) % 9 + K))
+            guard = out.clone()
+            guard[place] = want
+            q8.q8_mx4_fake_quantize(rows, out[place], dev_status=word)
+            assert torch.equal(out, guard) and word.item() == 0
+            out.fill_(5.0)
+            st = lib.q8_mx4_dequantize(t.tiles.data_ptr(), 1, MANY_ROWS, K, out[place].data_ptr(), q8._MX4_DTYPES[dtype], ld + 3, stream)
+            assert st == q8.Q8_OK and torch.equal(out, guard)
+            q8.q8_mx4_fake_quantize(rows, rows, dev_status=word)  # in place
+            assert word.item() == 0 and torch.equal(rows, want)
+            assert torch.isnan(whole[[0, -1]]).all() and torch.isnan(whole[1:-1, :offset]).all() and torch.isnan(whole[1:-1, offset + K:]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_many_rows_of_odd_length_side_by_side(dtype):
+    """Contiguous tensors whose rows end anywhere, matrices of experts among them, with what is not a number at both ends of rows."""
+    for shape in ((3, 1413, 301), (5000, 257)):
+        x = values(shape, 3, dtype)
+        t = q8.q8_mx4_quantize(x)
+        back = q8.q8_mx4_dequantize(t, dtype)
+        for g in range(shape[0] if len(shape) == 3 else 1):
+            one, again = (x[g], back[g]) if len(shape) == 3 else (x, back)
+            check_codes(t, one, g)
+            assert torch.equal(again, torch.from_numpy(ref.rounded(one)).to(dtype).cuda())
+    for column in (0, 7, 8, 255, 256):
+        y = x.clone()
+        y[::7, column] = float("nan")
+        word = status_word()
+        got = q8.q8_mx4_fake_quantize(y, dev_status=word)
+        assert word.item() == 1 << q8.Q8_ERR_SCALE and torch.equal(got, torch.from_numpy(ref.rounded(y)).to(dtype).cuda())
