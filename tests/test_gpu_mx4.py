@@ -724,3 +724,29 @@ def test_many_rows_of_odd_length_side_by_side(dtype):
         word = status_word()
         got = q8.q8_mx4_fake_quantize(y, dev_status=word)
         assert word.item() == 1 << q8.Q8_ERR_SCALE and torch.equal(got, torch.from_numpy(ref.rounded(y)).to(dtype).cuda())
+
+
+# ---------------------------------------------------------------- sums without rounding
+def on_the_grid(shape, seed):
+    """Values that are their own codes at scale 1: every block has one of 4 or 6."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.tensor(ref.GRID, dtype=torch.float32)[torch.randint(0, 8, shape, generator=g)] * (torch.randint(0, 2, shape, generator=g) * 2 - 1)
+    x[..., ::32] = torch.tensor([4.0, 6.0])[torch.randint(0, 2, x[..., ::32].shape, generator=g)]
+    return x.cuda()
+
+
+@pytest.mark.parametrize("M,N,K", [(2, 130, 20001), (20, 130, 20001), (40, 300, 33), (500, 300, 4100), (1000, 1030, 20001), (4096, 2400, 2100)])
+def test_sums_that_fp32_holds_are_exact(M, N, K):
+    """Products are multiples of 1/4 and their absolute sum is below 36 K <= 720036 < 2^20, so 22 bits hold every partial sum, in whatever order: a wrong code,
+    scale or place of a single value shows, which the tolerance of a long sum hides."""
+    x, w, b = on_the_grid((M, K), 1), on_the_grid((N, K), 2), on_the_grid((N,), 3)
+    W = q8.q8_mx4_quantize(w / 1024)
+    want = (x.double() @ w.double().t() / 1024).float()
+    for dtype in TYPES:
+        assert torch.equal(q8.q8_mx4_linear(x.to(dtype), W, dtype=torch.float32), want)
+    assert torch.equal(q8.q8_mx4_linear(x * 2.0 ** 20, W, b * 1024.0), want * 2.0 ** 20 + b * 1024)
+    cuts = [0, M // 3, M // 3, M - 1, M]
+    W4 = q8.q8_mx4_quantize(torch.stack([w / 1024, w, w / 2, -w / 1024]))
+    y = q8.q8_mx4_linear_grouped(x, torch.tensor(cuts, dtype=torch.int32).cuda(), W4)
+    for (lo, hi), factor in zip(zip(cuts, cuts[1:]), (1, 1024, 512, -1)):
+        assert torch.equal(y[lo:hi], want[lo:hi] * factor)
