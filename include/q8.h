@@ -286,13 +286,16 @@ q8_status q8_attention_status_word(void **dev_status);
  *     0 behind the last block
  * Common to the calls below: dtype is one of Q8_F32, Q8_F16, Q8_BF16; ld* is the distance of two rows in values (at least their
  * length); tiles are 16-byte aligned, values aligned to their type; 1 <= K <= 2^24, rows below 2^31 - 512, rows times ld* up to 2^56;
- * dev_status (may be NULL) is OR-ed into, never cleared; outputs and workspaces overlap no input and not each other (Q8_ERR_ARG, also for rows of two
- * different pitches in one stretch of memory); calls that share a workspace must be ordered on the stream.  Zero rows or features are a no-op.  Waits inside the product's kernel are bounded: one that expires flags
- * Q8_ERR_TIMEOUT in dev_status, and Y is then not to be used. */
+ * dev_status is OR-ed into, never cleared; where it is NULL the calls use a word of the library, one per device, whose address
+ * q8_mx4_status_word returns (poll it with q8_poll_status).  Outputs and workspaces overlap no input and not each other (Q8_ERR_ARG, also for rows of
+ * two different pitches in one stretch of memory); calls that share a workspace must be ordered on the stream.  Zero rows or features are a no-op.
+ * Inside the product's kernel the waits on memory barriers, for copies and products, are bounded: one that expires flags Q8_ERR_TIMEOUT, and Y is then
+ * not to be used.  Waits for the kernel before, for the CTAs of a cluster and for tensor memory have no limit of their own. */
 #define Q8_F32 0
 #define Q8_F16 1
 #define Q8_BF16 2
 size_t q8_mx4_bytes(int64_t groups, int64_t rows, int64_t K);
+q8_status q8_mx4_status_word(void **dev_status);
 
 /* X [groups, rows, K] (group stride rows * ldx) into the tiles T, and back: Y [groups * rows, K] rounded once to its type. */
 q8_status q8_mx4_quantize(const void *X, int dtype, int64_t groups, int64_t rows, int64_t K, int64_t ldx, uint8_t *T,

@@ -57,6 +57,7 @@ SIGNATURES = {
     "q8_add_layernorm_quant": (_int, [_vp, _vp, _vp, _vp, _vp, _f, _i64, _i64, _vp, _vp, _vp, _vp]),
     "q8_attention_quant": (_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp]),
     "q8_mx4_bytes": (_sz, [_i64, _i64, _i64]),
+    "q8_mx4_status_word": (_int, [C.POINTER(C.c_void_p)]),
     "q8_mx4_quantize": (_int, [_vp, _int, _i64, _i64, _i64, _i64, _vp, _vp, _vp]),
     "q8_mx4_dequantize": (_int, [_vp, _i64, _i64, _i64, _vp, _int, _i64, _vp]),
     "q8_mx4_fake_quantize": (_int, [_vp, _int, _i64, _i64, _i64, _vp, _i64, _vp, _vp]),
@@ -703,6 +704,20 @@ def _mx4_output(Y, shape, dtype, like, stream, name: str = "Y"):
 
 def q8_mx4_bytes(groups: int, rows: int, K: int) -> int:
     return int(load().q8_mx4_bytes(groups, rows, K))
+
+
+def q8_mx4_status_word() -> int:
+    """Device address of the current device's status word for MXFP4 calls that are given none."""
+    p = C.c_void_p(0)
+    _check(load().q8_mx4_status_word(C.byref(p)), "q8_mx4_status_word")
+    return int(p.value)
+
+
+def q8_mx4_status(stream=None) -> Tuple[int, int]:
+    """Synchronises, reads and clears the word that MXFP4 calls without a dev_status use; returns (first status code, raw bits)."""
+    raw = C.c_uint32(0)
+    st = load().q8_poll_status(C.c_void_p(q8_mx4_status_word()), C.byref(raw), _stream(stream))
+    return int(st), int(raw.value)
 
 
 def q8_mx4_quantize(X, dev_status=None, stream=None) -> Mx4:

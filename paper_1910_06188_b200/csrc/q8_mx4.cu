@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kThreads) mx4_quantize_kernel(Mx4QuantizeArgs 
             if ((lane & 3) == 0) *reinterpret_cast<uint32_t *>(tile + scale_place((int)r0, (lane >> 4) * 4) + (lane & 12)) = scales;
         }
     }
-    if (a.status != nullptr) {
+    if (a.status != nullptr && lane == 0) {  // (the whole warp has the same)
         const uint32_t flags = (odd ? 1u << Q8_ERR_SCALE : 0u) | (bad_index ? 1u << Q8_ERR_INDEX : 0u);
         if (flags != 0) atomicOr(a.status, (int32_t)flags);
     }

@@ -16,6 +16,21 @@ bool span_too_long(int64_t rows, int64_t ld) { return ld > kMaxSpan / (rows > 0 
 bool aligned_to(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 bool known_dtype(int d) { return d == Q8_F32 || d == Q8_F16 || d == Q8_BF16; }
 size_t dtype_bytes(int d) { return d == Q8_F32 ? 4 : 2; }
+// Where conditions go that the caller gave no word for.
+static __device__ int32_t g_status[1];
+int32_t *own_status_word()
+{
+    static int32_t *cached[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+    if (cached[dev] == nullptr) {
+        void *p = nullptr;
+        if (cudaGetSymbolAddress(&p, g_status) != cudaSuccess) return nullptr;
+        cached[dev] = static_cast<int32_t *>(p);
+    }
+    return cached[dev];
+}
+int32_t *word_or_own(int32_t *dev_status) { return dev_status != nullptr ? dev_status : own_status_word(); }
 q8_status cuda_status(cudaError_t e) { return e == cudaSuccess ? Q8_OK : Q8_ERR_CUDA; }
 
 // [groups, rows, K] with rows ld values apart
@@ -110,6 +125,13 @@ size_t q8_mx4_bytes(int64_t groups, int64_t rows, int64_t K)
     return (size_t)groups * (size_t)ceil_div(rows, kTileRows) * (size_t)tiles_along(K) * kTileBytes;
 }
 
+q8_status q8_mx4_status_word(void **dev_status)
+{
+    if (dev_status == nullptr) return Q8_ERR_NULL;
+    *dev_status = own_status_word();
+    return *dev_status != nullptr ? Q8_OK : Q8_ERR_CUDA;
+}
+
 q8_status q8_mx4_quantize(const void *X, int dtype, int64_t groups, int64_t rows, int64_t K, int64_t ldx, uint8_t *T, int32_t *dev_status,
                           void *stream)
 {
@@ -129,7 +151,7 @@ q8_status q8_mx4_quantize(const void *X, int dtype, int64_t groups, int64_t rows
     a.rows = rows;
     a.K = K;
     a.out = T;
-    a.status = dev_status;
+    a.status = word_or_own(dev_status);
     return cuda_status(launch_mx4_quantize(a, dtype, static_cast<cudaStream_t>(stream)));
 }
 
@@ -168,7 +190,7 @@ q8_status q8_mx4_fake_quantize(const void *X, int dtype, int64_t rows, int64_t K
     a.K = K;
     a.Xhat = Xhat;
     a.ldo = ldo;
-    a.status = dev_status;
+    a.status = word_or_own(dev_status);
     return cuda_status(launch_mx4_quantize(a, dtype, static_cast<cudaStream_t>(stream)));
 }
 
@@ -204,9 +226,9 @@ q8_status q8_mx4_linear_q(const uint8_t *Xq, const uint8_t *Wq, const float *bia
     g.K = K;
     g.act = act;
     g.E = 1;
-    g.status = dev_status;
     const int64_t ys = (int64_t)dtype_bytes(y_dtype);
     if (layer_overlaps(g, nullptr, nullptr, 0) || rows_touch(Y, M, N * ys, ldy * ys, Xq, q8_mx4_bytes(1, M, K))) return Q8_ERR_ARG;
+    g.status = word_or_own(dev_status);
     return cuda_status(launch_mx4_gemm(g, static_cast<cudaStream_t>(stream)));
 }
 
@@ -237,10 +259,10 @@ q8_status q8_mx4_linear(const void *X, int x_dtype, int64_t ldx, const uint8_t *
     g.K = K;
     g.act = act;
     g.E = 1;
-    g.status = dev_status;
     if (layer_overlaps(g, nullptr, workspace, scratch) || rows_overlap(X, M, K * xs, ldx * xs, Y, M, N * ys, ldy * ys) ||
         rows_touch(X, M, K * xs, ldx * xs, workspace, scratch))
         return Q8_ERR_ARG;
+    g.status = word_or_own(dev_status);
     return quantize_and_multiply(g, X, x_dtype, ldx, M, nullptr, workspace, static_cast<cudaStream_t>(stream));
 }
 
@@ -274,10 +296,10 @@ q8_status q8_mx4_linear_grouped(const void *X, int x_dtype, int64_t ldx, int64_t
     g.act = act;
     g.offsets = offsets;
     g.E = (int)experts;
-    g.status = dev_status;
     if (layer_overlaps(g, rows, workspace, scratch) || rows_overlap(X, x_rows, K * xs, ldx * xs, Y, T, N * ys, ldy * ys) ||
         rows_touch(X, x_rows, K * xs, ldx * xs, workspace, scratch))
         return Q8_ERR_ARG;
+    g.status = word_or_own(dev_status);
     return quantize_and_multiply(g, X, x_dtype, ldx, x_rows, rows, workspace, static_cast<cudaStream_t>(stream));
 }
 

@@ -229,7 +229,7 @@ __device__ __forceinline__ bool quantize_tokens(const Mx4GemmArgs &a, const Plan
         __syncwarp();
         if (lane == 0) mbar_arrive_many(smem_u32(full_bar + s), (uint32_t)every);
     }
-    if (odd && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_SCALE);
+    if (odd && lane == 0 && a.status != nullptr) atomicOr(a.status, 1 << Q8_ERR_SCALE);
     return true;
 }
 

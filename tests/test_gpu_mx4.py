@@ -750,3 +750,34 @@ def test_sums_that_fp32_holds_are_exact(M, N, K):
     y = q8.q8_mx4_linear_grouped(x, torch.tensor(cuts, dtype=torch.int32).cuda(), W4)
     for (lo, hi), factor in zip(zip(cuts, cuts[1:]), (1, 1024, 512, -1)):
         assert torch.equal(y[lo:hi], want[lo:hi] * factor)
+
+
+# ---------------------------------------------------------------- conditions without a word of the caller's
+def test_status_of_calls_without_a_word():
+    """What the device finds is to be had of calls that were given no word, and of no others."""
+    x, w = values((40, 192), 1, spread=0.0), weights((130, 192), 2)
+    bad = x.clone()
+    bad[3, 5] = float("nan")
+    W, many = q8.q8_mx4_quantize(w), q8.q8_mx4_quantize(weights((2, 130, 192), 3))
+    offsets, falling = (torch.tensor(v, dtype=torch.int32).cuda() for v in ([0, 20, 40], [0, 30, 20]))
+    outside = torch.full((40,), 40, dtype=torch.int32, device="cuda")
+    scale, index = (q8.Q8_ERR_SCALE, 1 << q8.Q8_ERR_SCALE), (q8.Q8_ERR_INDEX, 1 << q8.Q8_ERR_INDEX)
+    q8.q8_mx4_status()
+    for call, found in (
+            (lambda v, s: q8.q8_mx4_quantize(v, dev_status=s), scale), (lambda v, s: q8.q8_mx4_fake_quantize(v, dev_status=s), scale),
+            (lambda v, s: q8.q8_mx4_linear(v, W, dev_status=s), scale), (lambda v, s: q8.q8_mx4_linear(v[2:5], W, dev_status=s), scale),
+            (lambda v, s: q8.q8_mx4_linear_grouped(v, offsets, many, dev_status=s), scale),
+            (lambda v, s: q8.q8_mx4_linear_grouped(x, offsets if v is x else falling, many, dev_status=s), index),
+            (lambda v, s: q8.q8_mx4_linear_grouped(x, offsets, many, rows=None if v is x else outside, dev_status=s), index)):
+        call(x, None)
+        assert q8.q8_mx4_status() == (q8.Q8_OK, 0)
+        call(bad, None)
+        assert q8.q8_mx4_status() == found and q8.q8_mx4_status() == (q8.Q8_OK, 0)
+        word = status_word()
+        call(bad, word)
+        assert word.item() == found[1] and q8.q8_mx4_status() == (q8.Q8_OK, 0)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call(bad, None)
+            assert q8.q8_mx4_status() == found

@@ -137,6 +137,10 @@ def test_rows_too_far_apart_are_refused(lib, call, arguments):
     assert call(lib, **arguments) == q8.Q8_ERR_SHAPE
 
 
+def test_status_word_needs_a_place(lib):
+    assert lib.q8_mx4_status_word(None) == q8.Q8_ERR_NULL
+
+
 def test_tensors_of_the_host_are_refused(lib):
     W = q8.Mx4(torch.zeros(17408, dtype=torch.uint8), (8, 64))
     with pytest.raises(TypeError, match="X must be a CUDA tensor"):
