@@ -303,9 +303,11 @@ q8_status q8_mx4_quantize(const void *X, int dtype, int64_t groups, int64_t rows
 q8_status q8_mx4_dequantize(const uint8_t *T, int64_t groups, int64_t rows, int64_t K, void *Y, int dtype, int64_t ldy,
                             void *stream);
 /* The same rounding in training: Xhat = the values that X's codes stand for, in X's type (Xhat may be X, with the same ld).  Its
- * gradient is Eq. 5's straight-through one: q8_ste_backward. */
+ * gradient is Eq. 5's straight-through one, d Xhat / d X = 1, in X's type: q8_mx4_ste_backward copies grad_out [numel] to grad_in (a no-op when
+ * the two pointers are equal). */
 q8_status q8_mx4_fake_quantize(const void *X, int dtype, int64_t rows, int64_t K, int64_t ldx, void *Xhat, int64_t ldo,
                                int32_t *dev_status, void *stream);
+q8_status q8_mx4_ste_backward(const void *grad_out, int dtype, int64_t numel, void *grad_in, void *stream);
 
 /* Y = act(X_hat W_hat^T + b): X [M, K] is quantised as it comes in, W [N, K] was by q8_mx4_quantize (groups 1); bias [N] fp32 or NULL,
  * added in fp32, as the products are accumulated; act as in q8_linear; Y [M, N] is rounded once to its type.

@@ -61,6 +61,7 @@ SIGNATURES = {
     "q8_mx4_quantize": (_int, [_vp, _int, _i64, _i64, _i64, _i64, _vp, _vp, _vp]),
     "q8_mx4_dequantize": (_int, [_vp, _i64, _i64, _i64, _vp, _int, _i64, _vp]),
     "q8_mx4_fake_quantize": (_int, [_vp, _int, _i64, _i64, _i64, _vp, _i64, _vp, _vp]),
+    "q8_mx4_ste_backward": (_int, [_vp, _int, _i64, _vp, _vp]),
     "q8_mx4_linear_workspace_bytes": (_sz, [_i64, _i64]),
     "q8_mx4_linear": (_int, [_vp, _int, _i64, _vp, _vp, _int, _vp, _int, _i64, _i64, _i64, _i64, _vp, _sz, _vp, _vp]),
     "q8_mx4_linear_q": (_int, [_vp, _vp, _vp, _int, _vp, _int, _i64, _i64, _i64, _i64, _vp, _vp]),
@@ -94,7 +95,7 @@ _NATIVE_CALLS = ("q8_quantize_weight", "q8_fake_quantize", "q8_ste_backward", "q
                  "q8_linear", "q8_linear_workspace_bytes", "q8_linear_q", "q8_linear_requant", "q8_linear_q_requant",
                  "q8_linear_dyn", "q8_embedding", "q8_add_layernorm", "q8_add_layernorm_quant", "q8_add_layernorm_absmax",
                  "q8_attention", "q8_attention_quant", "q8_attention_absmax", "q8_embed_layernorm", "q8_mx4_quantize",
-                 "q8_mx4_dequantize", "q8_mx4_fake_quantize", "q8_mx4_bytes", "q8_mx4_linear", "q8_mx4_linear_workspace_bytes",
+                 "q8_mx4_dequantize", "q8_mx4_fake_quantize", "q8_mx4_ste_backward", "q8_mx4_bytes", "q8_mx4_linear", "q8_mx4_linear_workspace_bytes",
                  "q8_mx4_linear_q", "q8_mx4_linear_grouped", "q8_mx4_linear_grouped_workspace_bytes")
 
 
@@ -753,7 +754,7 @@ def q8_mx4_dequantize(T: Mx4, dtype: torch.dtype = torch.float32, stream=None) -
 
 
 def q8_mx4_fake_quantize(X, Xhat=None, dev_status=None, stream=None) -> torch.Tensor:
-    """Training-mode MXFP4: the values that the codes of X [rows, K] stand for, in X's type; q8_ste_backward is its gradient."""
+    """Training-mode MXFP4: the values that the codes of X [rows, K] stand for, in X's type; q8_mx4_ste_backward is its gradient."""
     if stream is None:
         r = (_native_module or _native()).mx4_fake_quantize(X, Xhat, dev_status)
         if r is not NotImplemented:
@@ -768,6 +769,21 @@ def q8_mx4_fake_quantize(X, Xhat=None, dev_status=None, stream=None) -> torch.Te
                                      _stream(stream))
     _check(st, "q8_mx4_fake_quantize")
     return Xhat
+
+
+def q8_mx4_ste_backward(grad_out, grad_in=None, stream=None) -> torch.Tensor:
+    """The gradient of q8_mx4_fake_quantize, straight through (Eq. 5): the incoming gradient, fp32, fp16 or bf16, contiguous."""
+    if stream is None:
+        r = (_native_module or _native()).mx4_ste_backward(grad_out, grad_in)
+        if r is not NotImplemented:
+            return r
+    if grad_out.dtype not in _MX4_DTYPES:
+        raise TypeError(f"grad_out must be float32, float16 or bfloat16, got {grad_out.dtype}")
+    grad_in = _mx4_output(grad_in, grad_out.shape, grad_out.dtype, grad_out, stream, "grad_in")
+    g, o = _ptr(grad_out, grad_out.dtype, "grad_out"), _ptr(grad_in, grad_out.dtype, "grad_in")
+    _mx4_same_device(grad_out, grad_in)
+    _check(load().q8_mx4_ste_backward(g, _MX4_DTYPES[grad_out.dtype], grad_out.numel(), o, _stream(stream)), "q8_mx4_ste_backward")
+    return grad_in
 
 
 def q8_mx4_linear_workspace_bytes(M: int, K: int) -> int:

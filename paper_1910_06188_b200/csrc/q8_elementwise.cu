@@ -576,16 +576,18 @@ __global__ void __launch_bounds__(kThreads) fake_quantize_kernel(const float *x,
 
 // ------------------------------------------------------------------ Eq. 5: the gradient passes unchanged
 // (A kernel of its own so that it starts under the tail of the one before it; 4096 x 3072 17.3 us = 5.8 TB/s with its launch, the
-// runtime's copy 19.0.)
-__global__ void __launch_bounds__(kStreamThreads) copy_kernel(const float *__restrict__ from, int64_t n, float *__restrict__ to)
+// runtime's copy 19.0.)  T: a value as it lies in memory, of 4 or 2 bytes.
+template <typename T>
+__global__ void __launch_bounds__(kStreamThreads) copy_kernel(const T *__restrict__ from, int64_t n, T *__restrict__ to)
 {
+    constexpr int kEach = 16 / (int)sizeof(T);
     grid_dependency_release_next(n <= kSmallProblemElems);
     grid_dependency_wait();
     const float4 *f4 = reinterpret_cast<const float4 *>(from);
     float4 *t4 = reinterpret_cast<float4 *>(to);
-    const int64_t n4 = n >> 2;
+    const int64_t n4 = n / kEach;
     for_each_batch<kStreamBatch>(n4, [&](int64_t i) { return __ldcs(f4 + i); }, [&](int64_t i, float4 v) { __stcs(t4 + i, v); });
-    if (blockIdx.x == 0 && threadIdx.x < (n & 3)) to[(n4 << 2) + threadIdx.x] = from[(n4 << 2) + threadIdx.x];
+    if (blockIdx.x == 0 && threadIdx.x < n % kEach) to[n4 * kEach + threadIdx.x] = from[n4 * kEach + threadIdx.x];
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -775,19 +777,23 @@ static bool on_current_device(const void *p)
     return false;
 }
 
-cudaError_t launch_copy(const float *from, int64_t n, float *to, cudaStream_t s)
+template <typename T>
+static cudaError_t launch_copy_of(const T *from, int64_t n, T *to, cudaStream_t s)
 {
     if (n <= 0) return cudaSuccess;
     if (!aligned16(from) || !aligned16(to) || !on_current_device(from) || !on_current_device(to))
-        return cudaMemcpyAsync(to, from, (size_t)n * sizeof(float), cudaMemcpyDeviceToDevice, s);
-    const cudaError_t e = launch_overlapping_tail(copy_kernel, dim3(stream_grid(n)), dim3(kStreamThreads), 0, s, from, n, to);
+        return cudaMemcpyAsync(to, from, (size_t)n * sizeof(T), cudaMemcpyDeviceToDevice, s);
+    const cudaError_t e = launch_overlapping_tail(copy_kernel<T>, dim3(stream_grid(n * (int64_t)sizeof(T) / 4)), dim3(kStreamThreads), 0, s, from, n, to);
     if (e == cudaErrorInvalidResourceHandle) {  // another device's stream, in which the runtime copies and launches nothing
         cudaGetLastError();
-        return cudaMemcpyAsync(to, from, (size_t)n * sizeof(float), cudaMemcpyDeviceToDevice, s);
+        return cudaMemcpyAsync(to, from, (size_t)n * sizeof(T), cudaMemcpyDeviceToDevice, s);
     }
     last_launch_info().launches += e == cudaSuccess;
     return e;
 }
+
+cudaError_t launch_copy(const float *from, int64_t n, float *to, cudaStream_t s) { return launch_copy_of(from, n, to, s); }
+cudaError_t launch_copy_16(const uint16_t *from, int64_t n, uint16_t *to, cudaStream_t s) { return launch_copy_of(from, n, to, s); }
 
 cudaError_t launch_embedding(const int32_t *ids, int64_t T, const int8_t *Eq, const float *S_e, int64_t V,
                              int64_t H, float *out, int8_t *rows_q, int32_t *status, cudaStream_t s)

@@ -194,6 +194,21 @@ q8_status q8_mx4_fake_quantize(const void *X, int dtype, int64_t rows, int64_t K
     return cuda_status(launch_mx4_quantize(a, dtype, static_cast<cudaStream_t>(stream)));
 }
 
+q8_status q8_mx4_ste_backward(const void *grad_out, int dtype, int64_t numel, void *grad_in, void *stream)
+{
+    last_launch_info() = LaunchInfo();
+    if (!known_dtype(dtype)) return Q8_ERR_ARG;
+    if (numel < 0 || numel > kMaxSpan) return Q8_ERR_SHAPE;
+    if (numel == 0 || grad_in == grad_out) return Q8_OK;
+    if (!grad_out || !grad_in) return Q8_ERR_NULL;
+    const size_t size = dtype_bytes(dtype);
+    if (!aligned_to(grad_out, size) || !aligned_to(grad_in, size)) return Q8_ERR_ALIGN;
+    if (pieces_touch(grad_out, (size_t)numel * size, grad_in, (size_t)numel * size)) return Q8_ERR_ARG;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return cuda_status(size == 4 ? launch_copy(static_cast<const float *>(grad_out), numel, static_cast<float *>(grad_in), s)
+                                 : launch_copy_16(static_cast<const uint16_t *>(grad_out), numel, static_cast<uint16_t *>(grad_in), s));
+}
+
 size_t q8_mx4_linear_workspace_bytes(int64_t M, int64_t K) { return M >= 0 && K > 0 && mx4_fused_preferred(M, K) ? 0 : q8_mx4_bytes(1, M, K); }
 
 size_t q8_mx4_linear_grouped_workspace_bytes(int64_t T, int64_t experts, int64_t K)

@@ -28,7 +28,7 @@ namespace {
     X(q8_linear_workspace_bytes) X(q8_linear_q) X(q8_linear_requant) X(q8_linear_q_requant) X(q8_linear_dyn)            \
     X(q8_embedding) X(q8_add_layernorm) X(q8_add_layernorm_quant) X(q8_add_layernorm_absmax) X(q8_attention)            \
     X(q8_attention_quant) X(q8_attention_absmax) X(q8_embed_layernorm)                                                  \
-    X(q8_mx4_quantize) X(q8_mx4_dequantize) X(q8_mx4_fake_quantize) X(q8_mx4_bytes) X(q8_mx4_linear)             \
+    X(q8_mx4_quantize) X(q8_mx4_dequantize) X(q8_mx4_fake_quantize) X(q8_mx4_ste_backward) X(q8_mx4_bytes) X(q8_mx4_linear)             \
     X(q8_mx4_linear_workspace_bytes) X(q8_mx4_linear_q) X(q8_mx4_linear_grouped) X(q8_mx4_linear_grouped_workspace_bytes)
 #define Q8_DECLARE(name) decltype(&::name) p_##name = nullptr;
 Q8_CALLS(Q8_DECLARE)
@@ -637,6 +637,30 @@ PyObject *mx4_fake_quantize(Args a)
     return out.result();
 }
 
+// (grad_out, grad_in)
+PyObject *mx4_ste_backward(Args a)
+{
+    Call c;
+    const at::Tensor *t = c.tensor(a[0]);
+    if (t == nullptr || !same_device(*t) || !t->is_contiguous() || mx4_dtype(t->scalar_type()) < 0) return other_form();
+    void *o = nullptr;
+    at::Tensor made;
+    if (a[1] == Py_None) {
+        made = new_tensor(t->sizes(), t->scalar_type());
+        o = made.data_ptr();
+    } else {
+        const at::Tensor *into = c.tensor(a[1]);
+        if (into == nullptr || !same_device(*into) || !into->is_contiguous() || into->scalar_type() != t->scalar_type() || into->sizes() != t->sizes())
+            return other_form();
+        o = into->data_ptr();
+    }
+    const void *g = t->data_ptr();
+    const int dtype = mx4_dtype(t->scalar_type());
+    const int64_t n = t->numel();
+    if (!run("q8_mx4_ste_backward", [&](void *s) { return p_q8_mx4_ste_backward(g, dtype, n, o, s); })) return nullptr;
+    return a[1] == Py_None ? THPVariable_Wrap(made) : Py_NewRef(a[1]);
+}
+
 // (X, W, bias, act, Y, dtype, workspace, dev_status)
 PyObject *mx4_linear(Args a)
 {
@@ -763,6 +787,7 @@ PyMethodDef kMethods[] = {
     Q8_ENTRY("mx4_quantize", mx4_quantize, 2),
     Q8_ENTRY("mx4_dequantize", mx4_dequantize, 2),
     Q8_ENTRY("mx4_fake_quantize", mx4_fake_quantize, 3),
+    Q8_ENTRY("mx4_ste_backward", mx4_ste_backward, 2),
     Q8_ENTRY("mx4_linear", mx4_linear, 8),
     Q8_ENTRY("mx4_linear_q", mx4_linear_q, 7),
     Q8_ENTRY("mx4_linear_grouped", mx4_linear_grouped, 10),

@@ -781,3 +781,67 @@ def test_status_of_calls_without_a_word():
         with torch.cuda.stream(side):
             call(bad, None)
             assert q8.q8_mx4_status() == found
+
+
+# ---------------------------------------------------------------- the gradient in every type
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 2049, 100_003])
+def test_straight_through_gradient(n, dtype):
+    """Bit for bit the incoming one, NaN and infinities too, at any address, nothing beside it written, in place, in a graph."""
+    g = values((n,), n, dtype)
+    g[n // 2] = float("nan")
+    bits = {4: torch.int32, 2: torch.int16}[g.element_size()]
+    got = q8.q8_mx4_ste_backward(g)
+    assert q8.q8_last_launch_info()["launches"] == 1 and got.dtype == dtype and got.data_ptr() != g.data_ptr()
+    assert torch.equal(got.view(bits), g.view(bits)) and torch.equal(q8.q8_mx4_ste_backward(g, stream=torch.cuda.current_stream()).view(bits), g.view(bits))
+    assert q8.q8_mx4_ste_backward(g, g) is g
+    for off_in, off_out in ((0, 0), (1, 0), (0, 1), (2, 2), (3, 5)):
+        src, room = torch.zeros(n + 8, dtype=dtype, device="cuda"), torch.full((n + 16,), 9.0, dtype=dtype, device="cuda")
+        src[off_in:off_in + n] = g
+        q8.q8_mx4_ste_backward(src[off_in:off_in + n], room[off_out:off_out + n])
+        assert torch.equal(room[off_out:off_out + n].view(bits), g.view(bits))
+        assert (room[:off_out] == 9).all() and (room[off_out + n:] == 9).all()
+    moved, graph = torch.zeros_like(g), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        q8.q8_mx4_ste_backward(g, moved)
+    g.copy_(values((n,), n + 1, dtype))
+    graph.replay()
+    assert torch.equal(moved, g)
+    assert q8.q8_mx4_ste_backward(torch.empty(0, 5, dtype=dtype, device="cuda")).shape == (0, 5)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_training_step_in_every_type(dtype):
+    """test_training_step with leaves, rounded values and gradients in their own type, the product between them in fp32."""
+    class Rounded(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            return q8.q8_mx4_fake_quantize(x)
+
+        @staticmethod
+        def backward(ctx, g):
+            return q8.q8_mx4_ste_backward(g.contiguous())
+
+    x, w = values((48, 96), 1, dtype, 0.5).requires_grad_(), weights((80, 96), 2).to(dtype).requires_grad_()
+    g = values((48, 80), 3, spread=0.0)
+    (Rounded.apply(x).float() @ Rounded.apply(w).float().t()).backward(g)
+    x_hat, w_hat, g64 = ref.rounded(x), ref.rounded(w), ref.as_numpy(g)
+    for leaf, want, size in ((x, g64 @ w_hat, np.abs(g64) @ np.abs(w_hat)), (w, g64.T @ x_hat, np.abs(g64).T @ np.abs(x_hat))):
+        far = 100 * 2.0 ** -24 * size  # up to 96 fp32 additions
+        far = far + ref.HALF_STEP[dtype] * (np.abs(want) + far) + ref.SMALLEST[dtype]  # and the rounding to the leaf's type
+        assert leaf.grad.dtype == dtype and (np.abs(ref.as_numpy(leaf.grad) - want) <= far).all()
+
+
+def test_straight_through_gradient_refusals():
+    g = values((40,), 1, torch.bfloat16)
+    with pytest.raises(TypeError, match="float32, float16 or bfloat16"):
+        q8.q8_mx4_ste_backward(g.double())
+    with pytest.raises(TypeError):
+        q8.q8_mx4_ste_backward(g, torch.empty(40, dtype=torch.float16, device="cuda"))
+    with pytest.raises(ValueError, match="grad_in must be"):
+        q8.q8_mx4_ste_backward(g, torch.empty(39, dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(TypeError, match="contiguous"):
+        q8.q8_mx4_ste_backward(g[::2])
+    with pytest.raises(q8.Q8Error) as e:
+        q8.q8_mx4_ste_backward(g[:30], g[5:35])
+    assert e.value.status == q8.Q8_ERR_ARG

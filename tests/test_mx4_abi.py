@@ -177,3 +177,11 @@ def test_reference_on_an_example_by_hand():
     assert ref.values(code, E, 8).tolist() == [[4, 0, 2, 1, -4, 0.5, 0, 1.5]]
     assert code[0, :8].tolist() == [6, 0, 4, 2, 14, 1, 8, 3]
     assert ref.values(*ref.quantize(x * 2.0 ** -30), 8).tolist() == (ref.values(code, E, 8) * 2.0 ** -30).tolist()
+
+
+@pytest.mark.parametrize("grad_out,dtype,numel,grad_in,status", [
+    (None, 2, 8, FAR, q8.Q8_ERR_NULL), (FAKE, 2, 8, None, q8.Q8_ERR_NULL), (FAKE, 3, 8, FAR, q8.Q8_ERR_ARG), (FAKE, -1, 8, FAR, q8.Q8_ERR_ARG),
+    (FAKE, 0, -1, FAR, q8.Q8_ERR_SHAPE), (FAKE, 0, 1 << 57, FAR, q8.Q8_ERR_SHAPE), (FAKE + 2, 0, 8, FAR, q8.Q8_ERR_ALIGN), (FAKE, 1, 8, FAR + 1, q8.Q8_ERR_ALIGN),
+    (FAKE, 2, 8, FAKE + 14, q8.Q8_ERR_ARG), (FAKE, 0, 8, FAKE - 28, q8.Q8_ERR_ARG), (FAKE, 2, 0, None, q8.Q8_OK), (FAKE, 2, 8, FAKE, q8.Q8_OK)])
+def test_gradient_refusals(lib, grad_out, dtype, numel, grad_in, status):
+    assert lib.q8_mx4_ste_backward(grad_out, dtype, numel, grad_in, None) == status
