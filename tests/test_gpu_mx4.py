@@ -1,4 +1,8 @@
 """The MXFP4 operators on the GPU against their definition in 64 bits."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -845,3 +849,84 @@ def test_straight_through_gradient_refusals():
     with pytest.raises(q8.Q8Error) as e:
         q8.q8_mx4_ste_backward(g[:30], g[5:35])
     assert e.value.status == q8.Q8_ERR_ARG
+
+
+# ---------------------------------------------------------------- far offsets, streams at once, a first call that is captured
+def test_tensors_of_more_than_two_to_the_31_values():
+    rows, K = 525_000, 4100  # 2.15e9 values, rows that end inside a block and are not aligned
+    x = torch.empty(rows, K, dtype=torch.bfloat16, device="cuda")
+    part = values((1000, K), 1, torch.bfloat16)
+    for i in range(0, rows, 1000):
+        torch.mul(part, 1 + i // 1000 % 3, out=x[i:i + 1000])
+    assert x.numel() > 2 ** 31
+    want = [torch.from_numpy(ref.rounded(part * f)).to(torch.bfloat16).cuda() for f in (1, 2, 3)]
+    t = q8.q8_mx4_quantize(x)
+    for back in (lambda: q8.q8_mx4_dequantize(t, torch.bfloat16), lambda: q8.q8_mx4_fake_quantize(x, x)):
+        y = back()
+        assert all(torch.equal(y[i:i + 1000], want[i // 1000 % 3]) for i in range(0, rows, 1000))
+        del y
+
+
+@pytest.mark.parametrize("grouped", [False, True], ids=["plain", "grouped"])
+def test_outputs_of_more_than_two_to_the_31_values(grouped):
+    M, N, K = 70_000, 32_000, 64
+    x, w = values((M, K), 1, torch.bfloat16, 0.0), weights((2 if grouped else 1, N, K), 2)
+    cut = 69_900
+    if grouped:
+        Y = q8.q8_mx4_linear_grouped(x, torch.tensor([0, cut, M], dtype=torch.int32).cuda(), q8.q8_mx4_quantize(w))
+    else:
+        Y = q8.q8_mx4_linear(x, q8.q8_mx4_quantize(w[0]))
+    assert Y.numel() > 2 ** 31
+    for lo in (0, 33_000, 67_100, cut - 60, cut, M - 60):  # on both sides of value 2^31
+        ref.assert_layer(Y[lo:lo + 60], ref.rounded(x[lo:lo + 60]), ref.rounded(w[1 if grouped and lo >= cut else 0]), None, q8.Q8_ACT_NONE)
+
+
+def test_calls_on_two_streams_at_once():
+    """Products of every form on one stream while others run on a second one, each with what it gives alone."""
+    sizes = [(4096, 2400, 2100), (2, 200, 8192), (24, 1000, 4096), (1300, 1000, 96), (700, 384, 512)]
+    calls = []
+    for M, N, K in sizes:
+        x, W = values((M, K), M, torch.bfloat16), q8.q8_mx4_quantize(weights((N, K), 2))
+        calls.append(lambda word, x=x, W=W: q8.q8_mx4_linear(x, W, act=q8.Q8_ACT_GELU, dev_status=word))
+    x, W = values((500, 512), 1), q8.q8_mx4_quantize(weights((6, 300, 512), 2))
+    offsets = torch.tensor([0, 100, 100, 230, 231, 400, 500], dtype=torch.int32).cuda()
+    calls.append(lambda word: q8.q8_mx4_linear_grouped(x, offsets, W, dev_status=word))
+    word = status_word()
+    want = [c(word) for c in calls]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for i in range(120):
+        for s, stream in enumerate(streams):
+            k = (i + 3 * s) % len(calls)
+            with torch.cuda.stream(stream):
+                y = calls[k](word)
+                if i % 10 == 9:
+                    got.append((k, y))
+    torch.cuda.synchronize()
+    assert word.item() == 0
+    assert len(got) == 24 and all(torch.equal(y, want[k]) for k, y in got)
+
+
+def test_first_call_of_a_process_is_captured():
+    """What a call sets up once (function attributes, the status word's address) may be set up while a stream is captured."""
+    code = """
+import torch
+from paper_1910_06188_b200 import binding as q8
+x, w = torch.randn(600, 96, device="cuda"), torch.randn(256, 96, device="cuda")
+few, many, offsets = x[:2].clone(), w.reshape(2, 128, 96), torch.tensor([0, 10, 600], dtype=torch.int32, device="cuda")
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    W = q8.q8_mx4_quantize(w)
+    got = [q8.q8_mx4_linear(x, W), q8.q8_mx4_linear(few, W), q8.q8_mx4_linear_grouped(x, offsets, q8.q8_mx4_quantize(many)),
+           q8.q8_mx4_fake_quantize(x), q8.q8_mx4_ste_backward(x)]
+graph.replay()
+torch.cuda.synchronize()
+W = q8.q8_mx4_quantize(w)
+want = [q8.q8_mx4_linear(x, W), q8.q8_mx4_linear(few, W), q8.q8_mx4_linear_grouped(x, offsets, q8.q8_mx4_quantize(many)),
+        q8.q8_mx4_fake_quantize(x), x]
+assert all(torch.equal(a, b) for a, b in zip(got, want))
+assert q8.q8_mx4_status() == (0, 0)
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
