@@ -363,10 +363,13 @@ mx4_gemm_kernel(const __grid_constant__ Maps<CTAS> maps, Mx4GemmArgs a, Plan pla
     else asm volatile("barrier.cta.sync 1, %0;" ::"n"(C::kThreads) : "memory");
     tc_fence_after();
     const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(tmem_slot);  // (not yet there for that producer, which does not use it)
-    // The next kernel may be parked beside single CTAs with up to three rounds of tiles, as beside the 8-bit GEMM, and only once this CTA has its
-    // tensor memory, whose allocation waits without a limit.  Beside longer products and pairs nothing is parked: they let the next one start
-    // when they end.
-    if (!goes_ahead) grid_dependency_release_next(CTAS == 1 && (a.offsets != nullptr ? table.tile[a.E] : plan.tiles) <= 3 * tile_step);
+    // The next kernel is parked beside single CTAs with one tile each, or with up to three where they quantise their tokens themselves, and only once
+    // this CTA has its tensor memory, whose allocation waits without a limit.  Longer products and pairs have nothing parked beside them: they
+    // let the next one start when they end.  (Let in early / when it ends, us, replayed: 1 x 1024 -> 4096 4.1 / 5.0, 1 x 8192 -> 512 5.8 / 7.4, 1 x 1024 -> 32768 7.2 /
+    // 8.0, 1000 slots of 7 experts 8.1 / 9.7, but with two or three tiles behind a quantise pass 24 x 4096 -> 32768 18.3 / 16.4, 640 x 512 -> 4096 9.6 / 7.9, 32 slots
+    // on 64 experts 12.4 / 11.0.)
+    constexpr int kRoundsBeside = FUSED ? 3 : 1;
+    if (!goes_ahead) grid_dependency_release_next(CTAS == 1 && (a.offsets != nullptr ? table.tile[a.E] : plan.tiles) <= kRoundsBeside * tile_step);
 
     Tile tile;
     auto width_of = [&](const Tile &t) { return (t.count + kStep - 1) / kStep * kStep; };

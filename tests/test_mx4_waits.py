@@ -18,7 +18,8 @@ def kernel():
 def test_no_kernel_is_parked_beside_a_pair_or_a_long_product(kernel):
     """The next kernel's CTAs are let in early by single CTAs with few rounds of tiles only, a condition that is the same for the whole grid."""
     released = re.findall(r"grid_dependency_release_next\((.*)\);", kernel)
-    assert released == ["CTAS == 1 && (a.offsets != nullptr ? table.tile[a.E] : plan.tiles) <= 3 * tile_step"]
+    assert released == ["CTAS == 1 && (a.offsets != nullptr ? table.tile[a.E] : plan.tiles) <= kRoundsBeside * tile_step"]
+    assert "constexpr int kRoundsBeside = FUSED ? 3 : 1;" in kernel
     assert "griddepcontrol" not in kernel
 
 
