@@ -7,7 +7,7 @@
 //
 // Measured: fp32 is bound by memory (49152 x 1024 into tiles 34.6 us, DRAM 77 %; 4096 x 1024 with the gradient's copy 12.5 us = 82 % of the copy rate), 16-bit
 // values by instructions (8192 x 8192 bf16 30.9 us, ALU pipe 69 %, DRAM 56 %; in training 12288 x 4096 37 us = 5.4 TB/s).  Into tiles and
-// back, 24576 x 1024 bf16: 39 us for two passes, 89 % of the copy rate.
+// back, 24576 x 1024 fp32: 39 us for two passes, 89 % of the copy rate.
 
 #include "q8_mx4.cuh"
 

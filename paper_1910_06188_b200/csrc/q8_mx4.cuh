@@ -178,7 +178,9 @@ __device__ __forceinline__ void load16(const void *p, uint32_t *w)
 // What a lane of a warp that takes 256 columns of a row reads of its columns k0 .. k0 + 7 (k0 = 8 lane + a multiple of 256), columns at
 // and behind K being 0.  ALIGNED: rows begin at multiples of 16 (vec) or 32 bytes.  Else a lane reads the aligned 16 or 32 bytes that its
 // first value lies in, the last lane the 16 behind them too, and settle() moves the bytes to their places; what of that is not of the
-// row is not read.  (Value by value, rows of 3532 bf16 took 6 times as long as rows of 3536.)
+// row is not read.  (Value by value, rows of 3532 bf16 took 6 times as long as rows of 3536.)  Few values, the slots of experts and tokens that the
+// product quantises itself take ALIGNED at any address, value by value where vec is 0: the grouped layer on 16384 slots of 2048 bf16 97.8 us with
+// rows 2048 apart, 116 to 120 with rows 2049 apart.
 template <typename T, bool ALIGNED>
 struct Columns {
     uint32_t w[kWords<T>], behind[ALIGNED ? 1 : 4];

@@ -21,7 +21,9 @@
 // CTAS = 2 (cta_group::2): a pair of SMs shares a tile of 256 features; each loads its own 128 rows of weights, half of the tokens and the
 // scales of all of them.  A plain product is the grouped one with a single expert.  Every wait on an mbarrier is bounded: after
 // ~2 s the CTA raises Q8_ERR_TIMEOUT in the status word, all roles leave their loops, copies and products in flight are waited for
-// (bounded), TMEM is freed.  No copy is multicast.
+// (bounded), TMEM is freed.  No copy is multicast.  Without a limit are the waits for the kernel before, for the CTAs of a cluster, for the CTA's own warps
+// and for TMEM; what ends them is resident (a cluster starts as a whole) or complete before this kernel's last CTA, and no other CTA of the library that holds TMEM
+// fits beside this one's shared memory.
 //
 // Bounds: many tokens the tensor pipe (8192 x 8192 -> 8192 bf16 180 us = 6.1 PFLOP/s at 1.55 GHz, the pipe 86 % active; 4096 x 8192 -> 8192 91 to 97 us),
 // with short K or fp32 outputs the epilogue's stores (24576 x 1024 -> 4096 fp32 with GELU 83 to 87 us for 403 MB of output); few tokens the

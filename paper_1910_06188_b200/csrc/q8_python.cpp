@@ -472,7 +472,8 @@ PyObject *ste_backward(Args a)
 }
 
 // ---- MXFP4
-// A new tensor on the current device, without the way through the dispatcher (1.5 us of 6 that a small layer took).
+// A new tensor on the current device, without the way through the dispatcher (1.5 us of 6 that a small layer took).  Dispatch modes do not see it, and
+// torch's filling of new memory in deterministic mode leaves it alone.
 at::Tensor new_tensor(at::IntArrayRef shape, at::ScalarType type)
 {
     return at::detail::empty_generic(shape, c10::cuda::CUDACachingAllocator::get(), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt);
